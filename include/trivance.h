@@ -41,7 +41,13 @@ typedef enum {
                                    +3^k and +2*3^k. Congestion counting only; not executable. */
 } trivance_variant;
 
-typedef enum { TRIVANCE_F32 = 0, TRIVANCE_I32 = 1 } trivance_dtype;
+typedef enum {
+    TRIVANCE_F32 = 0,
+    TRIVANCE_I32 = 1,
+    TRIVANCE_BF16 = 2, /* the 16-bit types and 64-bit integers are for the operators around the */
+    TRIVANCE_F16 = 3,  /* AllReduce (layer norm, balance loss, orthogonalisation); an AllReduce */
+    TRIVANCE_I64 = 4   /* takes F32 and I32                                                     */
+} trivance_dtype;
 
 typedef enum {
     TRIVANCE_ROUTE_SCHEDULED = 0, /* a message travels in the direction of its offset's sign   */
@@ -372,6 +378,162 @@ int trivance_copy_device(void* dst, const void* src, int64_t bytes, void* stream
  */
 int trivance_plan_with_dispatch_limit(const trivance_plan_t* plan, int64_t work_items,
                                       trivance_plan_t** out);
+
+/*
+ * Operators around the AllReduce: what the ranks of a data-parallel training step put into the rows
+ * that the AllReduce sums, and what is done with a sum.
+ *
+ * Activations and logits are rows of `width` (or `experts`) consecutive values, one for each token
+ * of each rank: value i of token t of rank r lies at data[r * rank_stride + t * token_stride + i].
+ * Strides count elements, are not negative and need no alignment beyond an element's; rows that are
+ * written must not overlap (EINVAL). Gradients and counts are one row per rank, `*_rank_stride`
+ * elements apart, so they can be written into (and read from) slices of the buffers of
+ * trivance_allreduce_emulated. All calls are asynchronous on `stream`, enqueue kernel launches only
+ * and can be captured into a HIP graph; sums are formed in a fixed order, so a call repeated on
+ * the same inputs leaves the same bits. Workspaces are caller-owned device memory whose contents
+ * do not matter on entry and are undefined after; calls that share one race.
+ * dtype is TRIVANCE_F32, TRIVANCE_BF16 or TRIVANCE_F16.
+ */
+
+/*
+ * trivance_layernorm_forward -- y = (x - mean) rstd gamma + beta for every row, with mean the row's
+ * mean, rstd = 1 / sqrt(variance + eps) and the variance taken about the mean (divided by width).
+ *
+ *   x, y         device rows of `dtype`; y may be x (with the same strides).
+ *   gamma, beta  device arrays of `width` values of weight_dtype; NULL means ones and zeros.
+ *   mean, rstd   device fp32 arrays [ranks][tokens] for the backward pass; NULL: not written.
+ *
+ * Statistics are fp32 sums, y is rounded once. A row that holds a NaN or an infinity gives NaN.
+ * tokens == 0 does nothing.
+ * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, width outside [1, 2^24], eps negative or
+ * NaN, NULL x or y, bad strides; EHIP.
+ */
+int trivance_layernorm_forward(const void* x, const void* gamma, const void* beta, void* y,
+                               float* mean, float* rstd, int64_t ranks, int64_t tokens,
+                               int64_t width, int64_t x_rank_stride, int64_t x_token_stride,
+                               int64_t y_rank_stride, int64_t y_token_stride, double eps, int dtype,
+                               int weight_dtype, void* stream);
+
+/* Workspace bytes of trivance_layernorm_backward for these sizes, for every dtype; 0 where a rank's
+ * tokens are summed in one piece. EINVAL for sizes that the call refuses. */
+int64_t trivance_layernorm_workspace_bytes(int64_t ranks, int64_t tokens, int64_t width);
+
+/*
+ * trivance_layernorm_backward -- the gradients of trivance_layernorm_forward. With
+ * h = (x - mean) rstd and g = dy gamma:
+ *     dx = rstd (g - mean(g) - h mean(g h))       per row
+ *     dgamma_r = sum over rank r's tokens of dy h     dbeta_r = sum over rank r's tokens of dy
+ *
+ *   dy, x, dx      device rows of `dtype`; dx may be dy or x (with the same strides).
+ *   gamma          as in the forward pass (NULL: ones).
+ *   mean, rstd     what the forward pass wrote, [ranks][tokens].
+ *   dgamma, dbeta  device fp32 rows of `width` values, one per rank, both grad_rank_stride elements
+ *                  apart; either may be NULL. They are written, not added to (zeros for a rank
+ *                  without tokens). The two must not overlap.
+ *   workspace      4-byte aligned, at least trivance_layernorm_workspace_bytes (unused, and may be
+ *                  NULL, where dgamma and dbeta are both NULL).
+ *
+ * Errors: those of the forward pass, EINVAL for NULL dy, mean, rstd or dx, ESIZE for the workspace.
+ */
+int trivance_layernorm_backward(const void* dy, const void* x, const void* gamma, const float* mean,
+                                const float* rstd, void* dx, float* dgamma, float* dbeta,
+                                int64_t ranks, int64_t tokens, int64_t width, int64_t dy_rank_stride,
+                                int64_t dy_token_stride, int64_t x_rank_stride,
+                                int64_t x_token_stride, int64_t dx_rank_stride,
+                                int64_t dx_token_stride, int64_t grad_rank_stride, int dtype,
+                                int weight_dtype, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+
+/* Workspace bytes of trivance_balance_counts for these sizes, for every dtype. EINVAL or
+ * EUNSUPPORTED for sizes that the call refuses. */
+int64_t trivance_balance_workspace_bytes(int64_t ranks, int64_t tokens, int64_t experts);
+
+/*
+ * trivance_balance_counts -- what a router's balance loss needs from each rank's tokens, as rows to
+ * sum over the ranks: how many slots chose each expert, how many tokens there are, and the sum
+ * over the tokens of the experts' probabilities softmax(logits).
+ *
+ *   logits   device rows of `experts` values of `dtype`. A logit of minus infinity excludes its
+ *            expert; where it excludes all, the token's probabilities count as zero.
+ *   chosen   device array [ranks][tokens][top_k] of id_dtype (TRIVANCE_I32 or TRIVANCE_I64), the
+ *            chosen experts; a value outside [0, experts) is an empty slot.
+ *   mask     device bytes [ranks][tokens]: a token whose byte is zero is left out, and neither its
+ *            logits nor its slots matter. NULL: all tokens count.
+ *   counts   device int32 rows of experts + 1 values: the counts, then the number of tokens.
+ *   probs    device fp32 rows of `experts` values.
+ *   workspace  4-byte aligned, at least trivance_balance_workspace_bytes.
+ *
+ * Both outputs are written, not added to (zeros for a rank without tokens).
+ * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, experts < 1, top_k < 1, more than
+ * 2^31 - 1 slots over all ranks, NULL pointers, bad strides; EUNSUPPORTED for more than 4096 experts;
+ * ESIZE for the workspace; EHIP.
+ */
+int trivance_balance_counts(const void* logits, const void* chosen, const uint8_t* mask,
+                            int32_t* counts, float* probs, int64_t ranks, int64_t tokens,
+                            int64_t experts, int64_t top_k, int64_t rank_stride,
+                            int64_t token_stride, int64_t counts_rank_stride,
+                            int64_t probs_rank_stride, int dtype, int id_dtype, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/*
+ * trivance_balance_loss -- the balance loss of each rank's row of counts and sums of probabilities.
+ * With counts c_e, N tokens and sums P_e:
+ *     loss = scale experts sum over e of (c_e / (top_k N)) (P_e / N),     0 where N = 0.
+ * Rows that an AllReduce has summed give every rank the loss over the tokens of all ranks; rows as
+ * trivance_balance_counts left them give each rank its own. loss: device fp32 [ranks].
+ * Errors: as trivance_balance_counts.
+ */
+int trivance_balance_loss(const int32_t* counts, const float* probs, float* loss, int64_t ranks,
+                          int64_t experts, int64_t top_k, int64_t counts_rank_stride,
+                          int64_t probs_rank_stride, double scale, void* stream);
+
+/*
+ * trivance_balance_backward -- the gradient of that loss with respect to each rank's logits, from
+ * the same counts (which have no gradient):
+ *     dlogit_tj = p_tj (w_j - sum over e of w_e p_te),   w_e = dloss scale experts c_e / (top_k N^2).
+ *
+ *   logits, mask  as in trivance_balance_counts; a masked token's gradient is zero.
+ *   dloss         device fp32 [ranks], the gradient of the loss; NULL: ones.
+ *   dlogits       device rows of `dtype`; may be logits (with the same strides).
+ *
+ * Errors: as trivance_balance_counts.
+ */
+int trivance_balance_backward(const void* logits, const int32_t* counts, const uint8_t* mask,
+                              const float* dloss, void* dlogits, int64_t ranks, int64_t tokens,
+                              int64_t experts, int64_t top_k, int64_t rank_stride,
+                              int64_t token_stride, int64_t d_rank_stride, int64_t d_token_stride,
+                              int64_t counts_rank_stride, double scale, int dtype, void* stream);
+
+/* Workspace bytes of trivance_orthogonalize for these sizes, for every dtype. EINVAL or EUNSUPPORTED for
+ * sizes that the call refuses. */
+int64_t trivance_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols);
+
+/*
+ * trivance_orthogonalize -- pushes the singular values of matrices towards one by Newton-Schulz
+ * products, as optimisers do with a summed gradient or its momentum before they apply it (the
+ * norm divides out, so a sum over ranks serves as well as a mean). For each matrix G:
+ *     X = G / (|G| + eps) with the Frobenius norm, then for each step (a, b, c) of `coefficients`
+ *     X <- a X + (b A + c A A) X with A = X X' (on the smaller side of G), and out = scale X.
+ *
+ *   x, out        device matrices [batch][rows][cols] of `dtype`, rows of consecutive values,
+ *                 strides in elements; out may be x (with the same strides).
+ *   coefficients  host array [steps][3].
+ *   workspace     at least trivance_orthogonalize_workspace_bytes.
+ *
+ * The norm is a 64-bit sum. Matrices are held in 22 bits and products summed in fp32 for every
+ * dtype: accuracy is that of fp32 products, and out is rounded once. Entries below 2^-36 of the norm
+ * are lost. A zero matrix gives zeros, one that holds a NaN or an infinity gives NaN throughout.
+ * batch, rows or cols == 0 does nothing.
+ * Errors: EINVAL for unknown types, negative sizes, steps < 1, NULL pointers, eps negative or NaN, scale
+ * not finite, bad strides; EUNSUPPORTED for sides above 65536, more than 65535 matrices or 64 steps,
+ * and coefficients that take a singular value in [0, 1] beyond 3.9 or a step's factor
+ * a + b s^2 + c s^4 beyond 15 in size; ESIZE for the workspace; EHIP.
+ */
+int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows, int64_t cols,
+                           int64_t x_batch_stride, int64_t x_row_stride, int64_t out_batch_stride,
+                           int64_t out_row_stride, const float* coefficients, int steps, double scale,
+                           double eps, int dtype, void* workspace, int64_t workspace_bytes,
+                           void* stream);
 
 /* Static description of a status code. */
 const char* trivance_strerror(int status);

@@ -18,7 +18,7 @@ import numpy as np
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtrivance.so")
 
 LATENCY_OPT, BANDWIDTH_OPT, BRUCK_REF = 0, 1, 2
-F32, I32 = 0, 1
+F32, I32, BF16, F16, I64 = 0, 1, 2, 3, 4
 ROUTE_SCHEDULED, ROUTE_SHORTEST = 0, 1
 PHASE_LATENCY, PHASE_REDUCE_SCATTER, PHASE_ALLGATHER = 0, 1, 2
 MAX_DIMS = 8
@@ -94,6 +94,21 @@ def _lib():
         "trivance_cost_model": (ctypes.c_int, [P, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                                ctypes.POINTER(ctypes.c_double), ctypes.c_int,
                                                ctypes.POINTER(CostResult)]),
+        "trivance_layernorm_forward": (ctypes.c_int, [P] * 6 + [i64] * 7 +
+                                       [ctypes.c_double, ctypes.c_int, ctypes.c_int, P]),
+        "trivance_layernorm_workspace_bytes": (i64, [i64] * 3),
+        "trivance_layernorm_backward": (ctypes.c_int, [P] * 8 + [i64] * 10 +
+                                        [ctypes.c_int, ctypes.c_int, P, i64, P]),
+        "trivance_balance_workspace_bytes": (i64, [i64] * 3),
+        "trivance_balance_counts": (ctypes.c_int, [P] * 5 + [i64] * 8 +
+                                    [ctypes.c_int, ctypes.c_int, P, i64, P]),
+        "trivance_balance_loss": (ctypes.c_int, [P] * 3 + [i64] * 5 + [ctypes.c_double, P]),
+        "trivance_balance_backward": (ctypes.c_int, [P] * 5 + [i64] * 9 +
+                                      [ctypes.c_double, ctypes.c_int, P]),
+        "trivance_orthogonalize_workspace_bytes": (i64, [i64] * 3),
+        "trivance_orthogonalize": (ctypes.c_int, [P] * 2 + [i64] * 7 +
+                                   [ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_double,
+                                    ctypes.c_double, ctypes.c_int, P, i64, P]),
         "trivance_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     }
     for name, (res, args) in sig.items():
@@ -115,7 +130,11 @@ def exported_symbols() -> list:
              "trivance_allreduce_emulated_ws", "trivance_allreduce_emulated_steps_ws",
              "trivance_congestion",
              "trivance_congestion_device", "trivance_congestion_noalloc", "trivance_fill_hash_uniform",
-             "trivance_copy_device", "trivance_cost_model", "trivance_strerror"]
+             "trivance_copy_device", "trivance_cost_model", "trivance_strerror",
+             "trivance_layernorm_forward", "trivance_layernorm_workspace_bytes",
+             "trivance_layernorm_backward", "trivance_balance_workspace_bytes",
+             "trivance_balance_counts", "trivance_balance_loss", "trivance_balance_backward",
+             "trivance_orthogonalize_workspace_bytes", "trivance_orthogonalize"]
     return [n for n in names if hasattr(lib, n)]
 
 
@@ -208,6 +227,8 @@ def trivance_pass_bytes(plan: Plan, elems: int, pass_index: int, dtype: int = F3
 
 _TORCH = None
 _DTYPES = {}
+_FLOATS = {}  # the element types of activations, logits, weights and matrices
+_IDS = {}  # of expert numbers
 
 
 def _torch():
@@ -217,6 +238,8 @@ def _torch():
         import torch
 
         _DTYPES.update({torch.float32: F32, torch.int32: I32})
+        _FLOATS.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _IDS.update({torch.int32: I32, torch.int64: I64})
         _TORCH = torch
     return _TORCH
 
@@ -382,3 +405,216 @@ def trivance_cost_model(plan: Plan, bytes_per_rank: float, alpha: float = 0.0,
                                       peaks, max(P, 1), ctypes.byref(res)), "trivance_cost_model")
     return {"total": res.total, "latency": res.latency, "transmission": res.transmission,
             "theta": res.theta, "passes": res.passes, "pass_link_bytes": list(peaks)[:P]}
+
+
+# The operators around the AllReduce. Tensors of activations and logits are [ranks, tokens, width], any
+# strides with the last dimension's values consecutive; gradients, counts and sums are one row per
+# rank and may be slices of a buffer that an AllReduce sums.
+
+
+def _rows(t, name, shape=None):
+    """(pointer, rank stride, token stride, type) of a [ranks, tokens, width] tensor."""
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
+    dt = _FLOATS.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16")
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be {'three-dimensional' if shape is None else tuple(shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and t.shape[2] > 1:
+        raise ValueError(f"the values of a row of {name} must be consecutive")
+    return t.data_ptr(), s0, s1, dt
+
+
+def _same_type(t, name, x, x_name):
+    if t.dtype != x.dtype or t.device != x.device:
+        raise TypeError(f"{name} must have the type and device of {x_name}")
+
+
+def _array(t, name, shape, dtype, device):
+    """Pointer of a contiguous tensor, None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, _TORCH.Tensor) or t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on {device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor")
+    return t.data_ptr()
+
+
+def _rank_rows(t, name, ranks, width, dtype, device):
+    """(pointer, stride) of one row of `width` values per rank, (None, None) for None."""
+    if t is None:
+        return None, None
+    if not isinstance(t, _TORCH.Tensor) or t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on {device}")
+    if t.dim() != 2 or t.shape[0] != ranks or t.shape[1] != width or \
+            (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{ranks}, {width}] with consecutive values in a row")
+    # the stride of a single row does not matter, and torch may give any
+    return t.data_ptr(), t.stride(0) if ranks > 1 else width
+
+
+def _weights(gamma, beta, width, device):
+    """Pointers and the one type of the weights."""
+    w = gamma if gamma is not None else beta
+    if w is None:
+        return None, None, F32
+    dt = _FLOATS.get(w.dtype)
+    if dt is None:
+        raise TypeError("weights must be float32, bfloat16 or float16")
+    return (_array(gamma, "gamma", (width,), w.dtype, device),
+            _array(beta, "beta", (width,), w.dtype, device), dt)
+
+
+def trivance_layernorm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5,
+                               stream=None) -> None:
+    """y = layer norm of the rows of x [ranks, tokens, width], times gamma plus beta (either may be
+    None); mean and rstd [ranks, tokens] receive the statistics for the backward pass."""
+    xp, xr, xt, dt = _rows(x, "x")
+    yp, yr, yt, _ = _rows(y, "y", x.shape)
+    _same_type(y, "y", x, "x")
+    ranks, tokens, width = x.shape
+    f32 = _TORCH.float32
+    gp, bp, wt = _weights(gamma, beta, width, x.device)
+    mp = _array(mean, "mean", (ranks, tokens), f32, x.device)
+    sp = _array(rstd, "rstd", (ranks, tokens), f32, x.device)
+    _check(_lib().trivance_layernorm_forward(xp, gp, bp, yp, mp, sp, ranks, tokens, width, xr, xt, yr,
+                                             yt, eps, dt, wt, _stream_ptr(stream)),
+           "trivance_layernorm_forward")
+
+
+def trivance_layernorm_workspace_bytes(ranks: int, tokens: int, width: int) -> int:
+    return _check(_lib().trivance_layernorm_workspace_bytes(ranks, tokens, width),
+                  "trivance_layernorm_workspace_bytes")
+
+
+def trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None,
+                                stream=None) -> None:
+    """dx, and each rank's dgamma and dbeta [ranks, width] (fp32 rows, equally far apart; either may be
+    None), from dy and what the forward pass read and wrote."""
+    xp, xr, xt, dt = _rows(x, "x")
+    dyp, dyr, dyt, _ = _rows(dy, "dy", x.shape)
+    dxp, dxr, dxt, _ = _rows(dx, "dx", x.shape)
+    _same_type(dy, "dy", x, "x")
+    _same_type(dx, "dx", x, "x")
+    ranks, tokens, width = x.shape
+    f32 = _TORCH.float32
+    gp, _, wt = _weights(gamma, None, width, x.device)
+    mp = _array(mean, "mean", (ranks, tokens), f32, x.device)
+    sp = _array(rstd, "rstd", (ranks, tokens), f32, x.device)
+    dgp, dgs = _rank_rows(dgamma, "dgamma", ranks, width, f32, x.device)
+    dbp, dbs = _rank_rows(dbeta, "dbeta", ranks, width, f32, x.device)
+    if dgs is not None and dbs is not None and dgs != dbs:
+        raise ValueError("the rows of dgamma and dbeta must be equally far apart")
+    wp, wb = _workspace_args(workspace)
+    _check(_lib().trivance_layernorm_backward(dyp, xp, gp, mp, sp, dxp, dgp, dbp, ranks, tokens, width,
+                                              dyr, dyt, xr, xt, dxr, dxt,
+                                              dgs if dgs is not None else dbs or 0, dt, wt, wp, wb,
+                                              _stream_ptr(stream)),
+           "trivance_layernorm_backward")
+
+
+def trivance_balance_workspace_bytes(ranks: int, tokens: int, experts: int) -> int:
+    return _check(_lib().trivance_balance_workspace_bytes(ranks, tokens, experts),
+                  "trivance_balance_workspace_bytes")
+
+
+def _mask(mask, shape, device):
+    if mask is not None and mask.dtype == _TORCH.uint8:
+        return _array(mask, "mask", shape, _TORCH.uint8, device)
+    return _array(mask, "mask", shape, _TORCH.bool, device)
+
+
+def trivance_balance_counts(logits, chosen, counts, probs, workspace=None, mask=None,
+                            stream=None) -> None:
+    """Each rank's expert counts and number of tokens, counts [ranks, experts + 1] (int32), and sums of
+    probabilities, probs [ranks, experts] (float32), from the router's logits [ranks, tokens,
+    experts], the experts chosen [ranks, tokens, top_k] (int32 or int64; negative: an empty slot)
+    and an optional mask [ranks, tokens] of the tokens that count (bool or uint8)."""
+    lp, lr, lt, dt = _rows(logits, "logits")
+    ranks, tokens, experts = logits.shape
+    it = _IDS.get(getattr(chosen, "dtype", None))
+    if it is None:
+        raise TypeError("chosen must be an int32 or int64 tensor")
+    if chosen.dim() != 3:
+        raise ValueError("chosen must be [ranks, tokens, top_k]")
+    k = chosen.shape[2]
+    ip = _array(chosen, "chosen", (ranks, tokens, k), chosen.dtype, logits.device)
+    mp = _mask(mask, (ranks, tokens), logits.device)
+    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, logits.device)
+    pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, logits.device)
+    wp, wb = _workspace_args(workspace)
+    _check(_lib().trivance_balance_counts(lp, ip, mp, cp, pp, ranks, tokens, experts, k, lr, lt,
+                                          cs or 0, ps or 0, dt, it, wp, wb, _stream_ptr(stream)),
+           "trivance_balance_counts")
+
+
+def trivance_balance_loss(counts, probs, top_k: int, loss, scale=1.0, stream=None) -> None:
+    """loss [ranks]: the balance loss of every rank's row of counts and probs."""
+    if not isinstance(probs, _torch().Tensor) or not probs.is_cuda or probs.dim() != 2:
+        raise TypeError("probs must be a two-dimensional CUDA (HIP) torch tensor")
+    ranks, experts = probs.shape
+    pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, probs.device)
+    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, probs.device)
+    op = _array(loss, "loss", (ranks,), _TORCH.float32, probs.device)
+    _check(_lib().trivance_balance_loss(cp, pp, op, ranks, experts, top_k, cs or 0, ps, scale,
+                                        _stream_ptr(stream)), "trivance_balance_loss")
+
+
+def trivance_balance_backward(logits, counts, top_k: int, dlogits, mask=None, scale=1.0, dloss=None,
+                              stream=None) -> None:
+    """dlogits: the gradient of the balance loss of `counts`, times dloss [ranks] (None: ones)."""
+    lp, lr, lt, dt = _rows(logits, "logits")
+    dp, dr, dts, _ = _rows(dlogits, "dlogits", logits.shape)
+    _same_type(dlogits, "dlogits", logits, "logits")
+    ranks, tokens, experts = logits.shape
+    mp = _mask(mask, (ranks, tokens), logits.device)
+    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, logits.device)
+    gp = _array(dloss, "dloss", (ranks,), _TORCH.float32, logits.device)
+    _check(_lib().trivance_balance_backward(lp, cp, mp, gp, dp, ranks, tokens, experts, top_k, lr, lt,
+                                            dr, dts, cs or 0, scale, dt, _stream_ptr(stream)),
+           "trivance_balance_backward")
+
+
+def trivance_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    return _check(_lib().trivance_orthogonalize_workspace_bytes(batch, rows, cols),
+                  "trivance_orthogonalize_workspace_bytes")
+
+
+# a, b, c of five steps that bring singular values from [0.003, 1] to about [0.7, 1.2]
+QUINTIC_5 = ((3.4445, -4.7750, 2.0315),) * 5
+_HOST_COEFFICIENTS = {}
+
+
+def _coefficients(steps):
+    """The steps' coefficients as a host array (made once for each tuple of tuples)."""
+    key = steps if isinstance(steps, tuple) else None
+    try:
+        got = _HOST_COEFFICIENTS.get(key) if key is not None else None
+    except TypeError:  # a tuple of lists
+        key = got = None
+    if got is None:
+        flat = [float(v) for abc in steps for v in abc]
+        if len(flat) != 3 * len(steps):
+            raise ValueError("coefficients must be three numbers for each step")
+        got = (ctypes.c_float * max(len(flat), 1))(*flat), len(steps)
+        if key is not None and len(_HOST_COEFFICIENTS) < 64:
+            _HOST_COEFFICIENTS[key] = got
+    return got
+
+
+def trivance_orthogonalize(x, out, workspace, coefficients=QUINTIC_5, scale=1.0, eps=1e-7,
+                           stream=None) -> None:
+    """out = scale times x [batch, rows, cols] with the singular values of each matrix pushed towards
+    one: X = x / (norm + eps), then X <- a X + (b A + c A A) X, A = X X', for each (a, b, c)."""
+    xp, xb, xr, dt = _rows(x, "x")
+    op, ob, orow, _ = _rows(out, "out", x.shape)
+    _same_type(out, "out", x, "x")
+    batch, rows, cols = x.shape
+    k, steps = _coefficients(coefficients)
+    wp, wb = _workspace_args(workspace)
+    _check(_lib().trivance_orthogonalize(xp, op, batch, rows, cols, xb, xr, ob, orow, k, steps, scale,
+                                         eps, dt, wp, wb, _stream_ptr(stream)),
+           "trivance_orthogonalize")
