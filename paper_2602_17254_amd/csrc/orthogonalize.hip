@@ -14,6 +14,7 @@
 // is 2^-36. G enters scaled by a power of two, exactly where it has 16 bits; the rest of the norm goes into
 // the first step's coefficients.
 //
+// What bounds it: the MFMA rate, for matrices of some hundred rows and more.
 // Layout. X is kept both ways round, so that both operands of every product have their summed index
 // contiguous; sides are padded with zeros to whole tiles. A and A A are symmetric: only tiles on and
 // above the diagonal are computed and each is written to both places.
@@ -22,6 +23,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "device.h"
 #include "operators.h"
 
 namespace trivance {
@@ -32,8 +34,6 @@ constexpr int kScaleExp = 12;
 constexpr int kMaxSteps = 64;
 constexpr int64_t kMaxSide = 1 << 16;
 constexpr int kNormParts = 256;  // partial sums of a matrix's norm
-constexpr int kTile = 64;
-constexpr int kDepth = 32;  // of one stage of a product
 
 typedef f16 half8 __attribute__((ext_vector_type(8)));
 typedef f16 half4 __attribute__((ext_vector_type(4)));
@@ -120,8 +120,11 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
     for (int q = threadIdx.x / 64; q < 64; q += 4) {
         const int64_t at = b * x.batch + (int64_t)(i0 + q) * x.ld + j0 + lane;
         const int64_t att = b * xt.batch + (int64_t)(j0 + q) * xt.ld + i0 + lane;
-        split(tile[q][lane], x.hi[at], x.lo[at]);
-        split(tile[lane][q], xt.hi[att], xt.lo[att]);
+        f16 lo;
+        split(tile[q][lane], x.hi[at], lo);
+        if (sizeof(T) > 2) x.lo[at] = lo;  // zero otherwise, and not read in the first step
+        split(tile[lane][q], xt.hi[att], lo);
+        if (sizeof(T) > 2) xt.lo[att] = lo;
     }
 }
 
@@ -135,64 +138,156 @@ struct Output {
     float scale;
 };
 
-// One stage of an operand: kTile rows of kDepth values in 16-byte pieces. The piece of row r and
-// index p lies at piece p ^ (r / 4 % 4), so that 16 rows' pieces of one index fall into 16
-// different groups of banks.
-__device__ __forceinline__ int piece(int row, int p) { return row * (kDepth / 8) + (p ^ (row / 4 % 4)); }
+// How a square tile of a product is computed: the rows and columns of waves that share it, and the
+// values of the summed index in one stage of local memory (two stages: 64, 128 and 128 KiB). Rates
+// measured with both operands in two planes, on 2048 x 8192 from 2048 and on 2048 x 2048 from
+// 2048: tiles of 256 1125 and 370 TFLOP/s (64 tiles for 256 CUs), of 128 860 and 860, of 64 530 and
+// 574. Larger tiles read less of the operands again; a stage of 64 halves the barriers, and tiles of 256
+// have no room for it.
+template <int TILE>
+struct Shape;
+template <>
+struct Shape<256> {
+    static constexpr int kRows = 2, kCols = 4, kDepth = 32;
+};
+template <>
+struct Shape<128> {
+    static constexpr int kRows = 2, kCols = 2, kDepth = 64;
+};
+template <>
+struct Shape<64> {
+    static constexpr int kRows = 2, kCols = 2, kDepth = 64;
+};
 
-// C = L R' over `depth` (whole stages): L's rows are C's rows and R's rows C's columns. One workgroup of
-// four waves a tile, each wave a quarter.
-template <Product KIND, typename T>
-__global__ __launch_bounds__(256) void product_kernel(Planes l, Planes r, int depth, Planes c, Planes ct,
-                                                      Planes a, Coefficients k,
-                                                      const Coefficients* first, Output<T> out) {
+// Where a stage holds 16-byte piece p of a row of DEPTH values: pieces are permuted within their row so
+// that the 16 lanes that read one piece of 16 rows, and any 8 of them in order, meet different banks.
+template <int DEPTH>
+__device__ __forceinline__ int piece_of(int row, int p) {
+    if constexpr (DEPTH == 32) return p ^ ((row >> 1 & 3) ^ (row >> 3 & 1));
+    return p ^ ((row & 7) ^ (row >> 3 & 1));
+}
+
+// 16 bytes a lane straight from memory to local memory, a wave's lanes one after another.
+__device__ __forceinline__ void copy_to_local(const f16* from, half8* to) {
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)from,
+        (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+struct Operands {
+    Planes l, r;     // C = L R': L's rows are C's rows, R's rows its columns
+    int depth;       // the summed index, a multiple of 64
+    int rows, cols;  // tiles of C
+    Planes c, ct;    // C and its transpose
+    Planes a;        // of the polynomial
+    Coefficients k;
+    const Coefficients* first;  // in place of k, for each matrix
+};
+
+// C = L R'. LP and RP: the planes that are not zero. While the waves multiply one stage of the
+// operands the next one is on its way into the other half of local memory, so a stage has one barrier.
+template <Product KIND, int TILE, int LP, int RP, typename T>
+__global__ __launch_bounds__(Shape<TILE>::kRows * Shape<TILE>::kCols * 64, TILE == 64 ? 2 : 1) void product_kernel(
+    Operands o, Output<T> out) {
+    using S = Shape<TILE>;
     constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
-    if (kSymmetric && blockIdx.x < blockIdx.y) return;
-    __shared__ half8 stage[4][kTile * kDepth / 8];
+    constexpr int kThreads = S::kRows * S::kCols * 64, kDepth = S::kDepth, kPieces = kDepth / 8;
+    constexpr int WM = TILE / S::kRows, WN = TILE / S::kCols, MI = WM / 16, NI = WN / 16;
+    constexpr int kPlane = TILE * kPieces, kStage = (LP + RP) * kPlane;
+    extern __shared__ half8 stages[];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t b = blockIdx.z;
-    const int i0 = blockIdx.y * kTile, j0 = blockIdx.x * kTile;
-    const f16* src[4] = {l.hi + b * l.batch + (int64_t)i0 * l.ld, l.lo + b * l.batch + (int64_t)i0 * l.ld,
-                         r.hi + b * r.batch + (int64_t)j0 * r.ld, r.lo + b * r.batch + (int64_t)j0 * r.ld};
-    const int wi = wave / 2 * 32, wj = wave % 2 * 32;
-    float4v acc[2][2] = {};
-    const int row = threadIdx.x / 4, p = threadIdx.x % 4;
-    for (int d = 0; d < depth; d += kDepth) {
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            stage[q][piece(row, p)] =
-                *reinterpret_cast<const half8*>(src[q] + (int64_t)row * (q < 2 ? l.ld : r.ld) + d + p * 8);
-        __syncthreads();
-        half8 f[4][2];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                f[q][s] = stage[q][piece((q < 2 ? wi : wj) + s * 16 + lane % 16, lane / 16)];
-        // R first: a lane then holds four consecutive columns of one row
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[3][y], f[0][x], acc[x][y], 0, 0, 0);
-                acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[2][y], f[1][x], acc[x][y], 0, 0, 0);
-                acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[2][y], f[0][x], acc[x][y], 0, 0, 0);
-            }
+    // one XCD's workgroups take neighbouring tiles: all rows of some columns
+    const int tiles = kSymmetric ? o.rows * (o.rows + 1) / 2 : o.rows * o.cols;
+    const int all = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int64_t b = all / tiles;
+    const int tile = all % tiles;
+    int ti, tj;
+    if constexpr (kSymmetric) {  // ti <= tj
+        tj = (int)((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
+        while ((tj + 1) * (tj + 2) / 2 <= tile) ++tj;
+        while (tj * (tj + 1) / 2 > tile) --tj;
+        ti = tile - tj * (tj + 1) / 2;
+    } else {
+        ti = tile % o.rows;
+        tj = tile / o.rows;
     }
-    if (KIND == Product::kPolynomial && first) k = first[b];
+    const int i0 = ti * TILE, j0 = tj * TILE;
+    const int wi = wave / S::kCols * WM, wj = wave % S::kCols * WN;
+    const f16* lsrc[2] = {o.l.hi + b * o.l.batch + (int64_t)i0 * o.l.ld,
+                          o.l.lo + b * o.l.batch + (int64_t)i0 * o.l.ld};
+    const f16* rsrc[2] = {o.r.hi + b * o.r.batch + (int64_t)j0 * o.r.ld,
+                          o.r.lo + b * o.r.batch + (int64_t)j0 * o.r.ld};
+    const auto load = [&](int d, half8* stage) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+        for (int p = 0; p < LP + RP; ++p) {
+            const bool left = p < LP;
+            const f16* src = left ? lsrc[p] : rsrc[p - LP];
+            const int64_t ld = left ? o.l.ld : o.r.ld;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
+            for (int q0 = 0; q0 < kPlane; q0 += kThreads) {
+                const int q = q0 + threadIdx.x, row = q / kPieces;
+                copy_to_local(src + row * ld + d + piece_of<kDepth>(row, q % kPieces) * 8,
+                              stage + p * kPlane + q0 + wave * 64);
+            }
+        }
+    };
+    float4v acc[MI][NI] = {};
+    load(0, stages);
+    for (int d = 0, turn = 0; d < o.depth; d += kDepth, turn ^= 1) {
+        // this stage has arrived, and every wave has read the other half
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (d + kDepth < o.depth) load(d + kDepth, stages + (turn ^ 1) * kStage);
+        const half8* stage = stages + turn * kStage;
+#pragma unroll
+        for (int kk = 0; kk < kPieces / 4; ++kk) {
+            half8 l[LP][MI], r[RP][NI];
+#pragma unroll
+            for (int p = 0; p < LP; ++p)
+#pragma unroll
+                for (int x = 0; x < MI; ++x) {
+                    const int row = wi + x * 16 + lane % 16;
+                    l[p][x] = stage[p * kPlane + row * kPieces + piece_of<kDepth>(row, kk * 4 + lane / 16)];
+                }
+#pragma unroll
+            for (int p = 0; p < RP; ++p)
+#pragma unroll
+                for (int y = 0; y < NI; ++y) {
+                    const int row = wj + y * 16 + lane % 16;
+                    r[p][y] = stage[(LP + p) * kPlane + row * kPieces +
+                                    piece_of<kDepth>(row, kk * 4 + lane / 16)];
+                }
+            // R first: a lane then holds four consecutive columns of one row
+#pragma unroll
+            for (int pl = 0; pl < LP; ++pl)
+#pragma unroll
+                for (int pr = 0; pr < (pl ? 1 : RP); ++pr)
+#pragma unroll
+                    for (int x = 0; x < MI; ++x)
+#pragma unroll
+                        for (int y = 0; y < NI; ++y)
+                            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[pr][y], l[pl][x],
+                                                                               acc[x][y], 0, 0, 0);
+        }
+    }
+    Coefficients k = o.k;
+    if (KIND == Product::kPolynomial && o.first) k = o.first[b];
+#pragma unroll
+    for (int x = 0; x < MI; ++x)
+#pragma unroll
+        for (int y = 0; y < NI; ++y) {
             const int i = i0 + wi + x * 16 + lane % 16, j = j0 + wj + y * 16 + lane / 16 * 4;
             float v[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = acc[x][y][q] * (1.0f / kScale);
             if constexpr (KIND == Product::kPolynomial) {
-                const int64_t at = b * a.batch + (int64_t)i * a.ld + j;
-                const half4 h = *reinterpret_cast<const half4*>(a.hi + at);
-                const half4 w = *reinterpret_cast<const half4*>(a.lo + at);
+                const int64_t at = b * o.a.batch + (int64_t)i * o.a.ld + j;
+                const half4 h = *reinterpret_cast<const half4*>(o.a.hi + at);
+                const half4 w = *reinterpret_cast<const half4*>(o.a.lo + at);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     v[q] = k.b * ((float)h[q] + (float)w[q]) + k.c * v[q] + (i == j + q ? k.a * kScale : 0.0f);
@@ -212,33 +307,65 @@ __global__ __launch_bounds__(256) void product_kernel(Planes l, Planes r, int de
                     h[q] = hi;
                     w[q] = lo;
                 }
-                const int64_t at = b * c.batch + (int64_t)i * c.ld + j;
-                *reinterpret_cast<half4*>(c.hi + at) = h;
-                *reinterpret_cast<half4*>(c.lo + at) = w;
-                if (!kSymmetric || blockIdx.x != blockIdx.y) {
+                const int64_t at = b * o.c.batch + (int64_t)i * o.c.ld + j;
+                *reinterpret_cast<half4*>(o.c.hi + at) = h;
+                *reinterpret_cast<half4*>(o.c.lo + at) = w;
+                if (!kSymmetric || ti != tj) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int64_t att = b * ct.batch + (int64_t)(j + q) * ct.ld + i;
-                        ct.hi[att] = h[q];
-                        ct.lo[att] = w[q];
+                        const int64_t att = b * o.ct.batch + (int64_t)(j + q) * o.ct.ld + i;
+                        o.ct.hi[att] = h[q];
+                        o.ct.lo[att] = w[q];
                     }
                 }
             }
         }
 }
 
-int pad(int64_t side) { return (int)((side + kTile - 1) / kTile * kTile); }
+// The tiles of a call: of the symmetric products and of the others. Sides are padded to the larger.
+struct Tiles {
+    int symmetric, update;
+    int pad() const { return symmetric > update ? symmetric : update; }
+};
+
+int64_t padded(int64_t side, int tile) { return (side + tile - 1) / tile * tile; }
+
+// The pair that takes the least time by the measured rates, counting whole rounds of the 256 CUs and the
+// padding.
+Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
+    const auto cost = [&](int tile, int64_t tiles, int64_t depth) {
+        const double rate = tile == 256 ? 1.0 : tile == 128 ? 0.76 : 0.5;
+        return (double)((batch * tiles + 255) / 256) * tile * tile * depth / rate;
+    };
+    Tiles best{64, 64};
+    double least = INFINITY;
+    for (const int s : {64, 128})
+        for (const int u : {64, 128, 256}) {
+            const Tiles t{s, u};
+            const int64_t pm = padded(m, t.pad()), pn = padded(n, t.pad());
+            const int64_t ms = pm / s;
+            const double c = cost(s, ms * (ms + 1) / 2, pn + pm) + cost(u, pm / u * (pn / u), pm);
+            if (c < least) {
+                least = c;
+                best = t;
+            }
+        }
+    return best;
+}
 
 // The workspace: norm parts and first coefficients, then the planes of X and X' twice, A and P.
 struct Layout {
     int64_t parts, first, x[2], xt[2], a, p, bytes;  // byte offsets
+    Tiles tiles;
     int m, n;
 };
 
 Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     Layout w;
-    w.m = pad(rows < cols ? rows : cols);
-    w.n = pad(rows < cols ? cols : rows);
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    w.tiles = tiles_of(batch, m, n);
+    w.m = (int)padded(m, w.tiles.pad());
+    w.n = (int)padded(n, w.tiles.pad());
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -257,6 +384,42 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     w.p = take(as);
     w.bytes = at + 256;
     return w;
+}
+
+template <Product KIND, int TILE, int LP, int RP, typename T>
+int launch_product(const Operands& o, const Output<T>& out, int64_t batch, hipStream_t stream) {
+    using S = Shape<TILE>;
+    constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
+    constexpr size_t local = (size_t)2 * (LP + RP) * TILE * S::kDepth * sizeof(f16);
+    const auto kernel = product_kernel<KIND, TILE, LP, RP, T>;
+    if (local > 65536 &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)local) != hipSuccess)
+        return TRIVANCE_EHIP;
+    const int64_t tiles = kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols;
+    kernel<<<(unsigned)(tiles * batch), S::kRows * S::kCols * 64, local, stream>>>(o, out);
+    return launch_status();
+}
+
+// A product by the call's tiles. `exact`: X0 has one plane.
+template <Product KIND, typename T>
+int product(Operands o, const Output<T>& out, int64_t batch, int tile, bool exact, hipStream_t stream) {
+    o.rows = o.rows / tile;
+    o.cols = o.cols / tile;
+    // in a first step from 16 bits the lower plane of X is zero: both operands of the Gram matrix, the
+    // right one of the update
+    constexpr int LP = KIND == Product::kGram ? 1 : 2;
+#define LAUNCH(TILE)                                                                                 \
+    if (tile == TILE) {                                                                              \
+        if constexpr (KIND != Product::kPolynomial)                                                  \
+            if (exact) return launch_product<KIND, TILE, LP, 1>(o, out, batch, stream);              \
+        return launch_product<KIND, TILE, 2, 2>(o, out, batch, stream);                              \
+    }
+    if constexpr (KIND == Product::kUpdate || KIND == Product::kLast) LAUNCH(256)
+    LAUNCH(128)
+    LAUNCH(64)
+#undef LAUNCH
+    return TRIVANCE_EINVAL;
 }
 
 template <typename T>
@@ -281,21 +444,23 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
     norm_parts_kernel<T><<<dim3(nparts, nb), 256, 0, stream>>>(in, parts);
     split_kernel<T><<<dim3(w.n / 64, w.m / 64, nb), 256, 0, stream>>>(
         in, parts, nparts, x[0], xt[0], Coefficients{k[0], k[1], k[2]}, eps, first);
-    const dim3 square(w.m / kTile, w.m / kTile, nb), wide(w.n / kTile, w.m / kTile, nb);
-    for (int s = 0; s < steps; ++s) {
+    int rc = launch_status();
+    for (int s = 0; s < steps && !rc; ++s) {
         const Coefficients c{k[3 * s], k[3 * s + 1], k[3 * s + 2]};
         const int q = s % 2;
-        product_kernel<Product::kGram, T><<<square, 256, 0, stream>>>(x[q], x[q], w.n, a, a, a, c, nullptr, out);
-        product_kernel<Product::kPolynomial, T><<<square, 256, 0, stream>>>(
-            a, a, w.m, p, p, a, c, s == 0 ? first : nullptr, out);
-        if (s + 1 < steps)
-            product_kernel<Product::kUpdate, T><<<wide, 256, 0, stream>>>(p, xt[q], w.m, x[1 - q], xt[1 - q],
-                                                                          a, c, nullptr, out);
-        else
-            product_kernel<Product::kLast, T><<<wide, 256, 0, stream>>>(p, xt[q], w.m, x[q], xt[q], a, c,
-                                                                        nullptr, out);
+        const bool exact = s == 0 && sizeof(T) == 2;
+        const Output<f16> none{};
+        rc = product<Product::kGram>({x[q], x[q], w.n, w.m, w.m, a, a, a, c, nullptr}, none, batch,
+                                     w.tiles.symmetric, exact, stream);
+        if (rc) break;
+        rc = product<Product::kPolynomial>({a, a, w.m, w.m, w.m, p, p, a, c, s == 0 ? first : nullptr}, none,
+                                           batch, w.tiles.symmetric, false, stream);
+        if (rc) break;
+        const Operands update{p, xt[q], w.m, w.m, w.n, x[1 - q], xt[1 - q], a, c, nullptr};
+        rc = s + 1 < steps ? product<Product::kUpdate>(update, none, batch, w.tiles.update, exact, stream)
+                           : product<Product::kLast>(update, out, batch, w.tiles.update, exact, stream);
     }
-    return launch_status();
+    return rc;
 }
 
 // Whether the stored numbers stay in fp16's range for every singular value in [0, 1]: step by step, the
