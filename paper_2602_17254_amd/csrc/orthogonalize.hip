@@ -33,7 +33,7 @@ constexpr float kScale = 4096.0f;  // 2^12, of every stored matrix
 constexpr int kScaleExp = 12;
 constexpr int kMaxSteps = 64;
 constexpr int64_t kMaxSide = 1 << 16;
-constexpr int kNormParts = 256;  // partial sums of a matrix's norm
+constexpr int kNormParts = 1024;  // most partial sums of a matrix's norm
 
 typedef f16 half8 __attribute__((ext_vector_type(8)));
 typedef f16 half4 __attribute__((ext_vector_type(4)));
@@ -64,26 +64,41 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
 }
 
 // Partial sums of squares in 64 bits, so that no finite matrix overflows. Rows of the input as it lies in
-// memory: its contiguous index runs over the lanes.
+// memory, in pieces of 256 vectors.
 template <typename T>
 __global__ __launch_bounds__(256) void norm_parts_kernel(Input<T> in, double* parts) {
+    constexpr int V = kVec<T>;
     __shared__ double sums[4];
     const bool tall = in.sj != 1;
     const int rows = tall ? in.n : in.m, cols = tall ? in.m : in.n;
     const int64_t stride = tall ? in.sj : in.si;
     const T* x = in.x + blockIdx.y * in.batch;
+    const int pieces = (cols + 256 * V - 1) / (256 * V);
     double s = 0.0;
-    for (int i = blockIdx.x; i < rows; i += gridDim.x)
-        for (int j = threadIdx.x; j < cols; j += 256) {
-            const double v = (float)x[i * stride + j];
-            s += v * v;
-        }
+    for (int64_t u = blockIdx.x; u < (int64_t)rows * pieces; u += gridDim.x) {
+        float v[V];
+        load_row<T>(x + u / pieces * stride, (u % pieces * 256 + threadIdx.x) * V, cols, 0.0f, v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += (double)v[k] * (double)v[k];
+    }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
     if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
     __syncthreads();
     if (threadIdx.x == 0)
         parts[blockIdx.y * kNormParts + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+// The power of two 2^e below the norm, and the first step's coefficients, which hold what is left of it:
+// zeros for a zero matrix, not a number where the norm is none.
+__device__ __forceinline__ void scale_of(double squares, Coefficients c, float eps, int& e, Coefficients& first) {
+    const double norm = sqrt(squares);
+    e = norm > 0.0 && norm < __builtin_inf() ? ilogb(norm) : 0;
+    const double alpha = norm == 0.0 ? 0.0
+                         : norm < __builtin_inf() ? ldexp(1.0, e) / (norm + eps)
+                                                  : __builtin_nan("");
+    const double cube = alpha * alpha * alpha;
+    first = {(float)(c.a * alpha), (float)(c.b * cube), (float)(c.c * (cube * alpha * alpha))};
 }
 
 // X both ways round, scaled by 2^12 over the power of two below the norm and padded with zeros, and the
@@ -98,15 +113,11 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
     for (int i = threadIdx.x % 64; i < nparts; i += 64) sum += parts[b * kNormParts + i];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    const double norm = sqrt(sum);
-    int e = 0;
-    if (norm > 0.0 && norm < __builtin_inf()) e = ilogb(norm);
-    // zero for a zero matrix; not a number where the norm is none
-    const double alpha = norm == 0.0 ? 0.0 : (norm < __builtin_inf() ? ldexp(1.0, e) / (norm + eps) : __builtin_nan(""));
+    int e;
+    Coefficients mine;
+    scale_of(sum, c, eps, e, mine);
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-    if (i0 == 0 && j0 == 0 && threadIdx.x == 0)
-        first[b] = {(float)(c.a * alpha), (float)(c.b * (alpha * alpha * alpha)),
-                    (float)(c.c * (alpha * alpha * alpha * alpha * alpha))};
+    if (i0 == 0 && j0 == 0 && threadIdx.x == 0) first[b] = mine;
     const T* g = in.x + b * in.batch;
     const bool tall = in.sj != 1;
     const int lane = threadIdx.x % 64;
@@ -138,26 +149,30 @@ struct Output {
     float scale;
 };
 
-// How a square tile of a product is computed: the rows and columns of waves that share it, and the
-// values of the summed index in one stage of local memory (two stages: 64, 128 and 128 KiB). Rates
-// measured with both operands in two planes, on 2048 x 8192 from 2048 and on 2048 x 2048 from
-// 2048: tiles of 256 1125 and 370 TFLOP/s (64 tiles for 256 CUs), of 128 860 and 860, of 64 530 and
-// 574. Larger tiles read less of the operands again; a stage of 64 halves the barriers, and tiles of 256
-// have no room for it.
+// How a square tile of a product is computed: the rows and columns of waves that share it, the values
+// of the summed index in one stage of local memory, and the stages. Rates measured
+// with both operands in two planes, on 2048 x 8192 from 2048 and on 2048 x 2048 from 2048: tiles of 256
+// 1125 and 370 TFLOP/s (64 tiles for 256 CUs), of 128 860 and 860, of 64 530 and 574 with two stages.
+// Larger tiles read less of the operands again; a stage of 64 halves the barriers, and tiles of 256
+// have no room for it. Tiles of 64 serve products too small to fill the GPU; there stages of 32 or 128
+// values, three or four stages, and 8 or 16 waves all measured within 15% of this one (135 tiles from
+// 768, 351 from 576).
 template <int TILE>
 struct Shape;
 template <>
 struct Shape<256> {
-    static constexpr int kRows = 2, kCols = 4, kDepth = 32;
+    static constexpr int kRows = 2, kCols = 4, kDepth = 32, kStages = 2;
 };
 template <>
 struct Shape<128> {
-    static constexpr int kRows = 2, kCols = 2, kDepth = 64;
+    static constexpr int kRows = 2, kCols = 2, kDepth = 64, kStages = 2;
 };
 template <>
 struct Shape<64> {
-    static constexpr int kRows = 2, kCols = 2, kDepth = 64;
+    static constexpr int kRows = 2, kCols = 2, kDepth = 64, kStages = 2;
 };
+template <int TILE>
+constexpr int kThreadsOf = Shape<TILE>::kRows * Shape<TILE>::kCols * 64;
 
 // Where a stage holds 16-byte piece p of a row of DEPTH values: pieces are permuted within their row so
 // that the 16 lanes that read one piece of 16 rows, and any 8 of them in order, meet different banks.
@@ -184,40 +199,32 @@ struct Operands {
     const Coefficients* first;  // in place of k, for each matrix
 };
 
-// C = L R'. LP and RP: the planes that are not zero. While the waves multiply one stage of the
-// operands the next one is on its way into the other half of local memory, so a stage has one barrier.
-template <Product KIND, int TILE, int LP, int RP, typename T>
-__global__ __launch_bounds__(Shape<TILE>::kRows * Shape<TILE>::kCols * 64, TILE == 64 ? 2 : 1) void product_kernel(
-    Operands o, Output<T> out) {
+// Waits until at most `n` of the wave's loads are on their way and its reads of local memory have arrived.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64, "vmcnt has six bits");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
+}
+
+// A workgroup's tile: the sums over values d0 .. d1 (whole stages) of the summed index of rows i0 of L and
+// j0 of R. LP and RP: the planes that are not zero. While the waves multiply one stage of the
+// operands the next ones are on their way into the other parts of local memory, so a stage has one
+// barrier.
+template <int TILE, int LP, int RP, int MI, int NI>
+__device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
+                                         half8* stages, float4v (&acc)[MI][NI]) {
     using S = Shape<TILE>;
-    constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
-    constexpr int kThreads = S::kRows * S::kCols * 64, kDepth = S::kDepth, kPieces = kDepth / 8;
-    constexpr int WM = TILE / S::kRows, WN = TILE / S::kCols, MI = WM / 16, NI = WN / 16;
+    constexpr int kThreads = kThreadsOf<TILE>, kDepth = S::kDepth, kPieces = kDepth / 8;
     constexpr int kPlane = TILE * kPieces, kStage = (LP + RP) * kPlane;
-    extern __shared__ half8 stages[];
+    constexpr int kLoads = kStage / kThreads;  // of a thread for a stage
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    // one XCD's workgroups take neighbouring tiles: all rows of some columns
-    const int tiles = kSymmetric ? o.rows * (o.rows + 1) / 2 : o.rows * o.cols;
-    const int all = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int64_t b = all / tiles;
-    const int tile = all % tiles;
-    int ti, tj;
-    if constexpr (kSymmetric) {  // ti <= tj
-        tj = (int)((sqrtf(8.0f * tile + 1.0f) - 1.0f) * 0.5f);
-        while ((tj + 1) * (tj + 2) / 2 <= tile) ++tj;
-        while (tj * (tj + 1) / 2 > tile) --tj;
-        ti = tile - tj * (tj + 1) / 2;
-    } else {
-        ti = tile % o.rows;
-        tj = tile / o.rows;
-    }
-    const int i0 = ti * TILE, j0 = tj * TILE;
-    const int wi = wave / S::kCols * WM, wj = wave % S::kCols * WN;
+    const int wi = wave / S::kCols * (MI * 16), wj = wave % S::kCols * (NI * 16);
     const f16* lsrc[2] = {o.l.hi + b * o.l.batch + (int64_t)i0 * o.l.ld,
                           o.l.lo + b * o.l.batch + (int64_t)i0 * o.l.ld};
     const f16* rsrc[2] = {o.r.hi + b * o.r.batch + (int64_t)j0 * o.r.ld,
                           o.r.lo + b * o.r.batch + (int64_t)j0 * o.r.ld};
-    const auto load = [&](int d, half8* stage) {
+    const auto load = [&](int d, int part) {
+        half8* stage = stages + part * kStage;
 #pragma unroll
         for (int p = 0; p < LP + RP; ++p) {
             const bool left = p < LP;
@@ -231,18 +238,22 @@ __global__ __launch_bounds__(Shape<TILE>::kRows * Shape<TILE>::kCols * 64, TILE 
             }
         }
     };
-    float4v acc[MI][NI] = {};
-    load(0, stages);
-    for (int d = 0, turn = 0; d < o.depth; d += kDepth, turn ^= 1) {
-        // this stage has arrived, and every wave has read the other half
+#pragma unroll
+    for (int s = 0; s + 1 < S::kStages; ++s)
+        if (d0 + s * kDepth < d1) load(d0 + s * kDepth, s);
+    for (int d = d0, part = 0; d < d1; d += kDepth) {
+        // this stage has arrived, and every wave has read the one before, whose place is taken next
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+        if (d + (S::kStages - 2) * kDepth < d1) wait_loads<kLoads * (S::kStages - 2)>();
+        else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (d + kDepth < o.depth) load(d + kDepth, stages + (turn ^ 1) * kStage);
-        const half8* stage = stages + turn * kStage;
+        const int ahead = part == 0 ? S::kStages - 1 : part - 1;
+        if (d + (S::kStages - 1) * kDepth < d1) load(d + (S::kStages - 1) * kDepth, ahead);
+        const half8* stage = stages + part * kStage;
+        part = part + 1 == S::kStages ? 0 : part + 1;
 #pragma unroll
         for (int kk = 0; kk < kPieces / 4; ++kk) {
             half8 l[LP][MI], r[RP][NI];
@@ -274,52 +285,349 @@ __global__ __launch_bounds__(Shape<TILE>::kRows * Shape<TILE>::kCols * 64, TILE 
                                                                                acc[x][y], 0, 0, 0);
         }
     }
+}
+
+// Four consecutive values of row i of C from column j on: what the product is for, and its places.
+// `mirrored`: in C's transpose too.
+template <Product KIND, typename T>
+__device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, int64_t b, Coefficients k,
+                                       int i, int j, bool mirrored, float4v sum) {
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = sum[q] * (1.0f / kScale);
+    if constexpr (KIND == Product::kPolynomial) {
+        const int64_t at = b * o.a.batch + (int64_t)i * o.a.ld + j;
+        const half4 h = *reinterpret_cast<const half4*>(o.a.hi + at);
+        const half4 w = *reinterpret_cast<const half4*>(o.a.lo + at);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            v[q] = k.b * ((float)h[q] + (float)w[q]) + k.c * v[q] + (i == j + q ? k.a * kScale : 0.0f);
+    }
+    if constexpr (KIND == Product::kLast) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (i < out.m && j + q < out.n)
+                out.x[b * out.batch + i * out.si + (j + q) * out.sj] = (T)(v[q] * (out.scale / kScale));
+    } else {
+        half4 h, w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f16 hi, lo;
+            split(v[q], hi, lo);
+            h[q] = hi;
+            w[q] = lo;
+        }
+        const int64_t at = b * o.c.batch + (int64_t)i * o.c.ld + j;
+        *reinterpret_cast<half4*>(o.c.hi + at) = h;
+        *reinterpret_cast<half4*>(o.c.lo + at) = w;
+        if (mirrored) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t att = b * o.ct.batch + (int64_t)(j + q) * o.ct.ld + i;
+                o.ct.hi[att] = h[q];
+                o.ct.lo[att] = w[q];
+            }
+        }
+    }
+}
+
+// Tile t of the tiles on and above the diagonal, column by column: its row is ti <= tj.
+__device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
+    tj = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while ((tj + 1) * (tj + 2) / 2 <= t) ++tj;
+    while (tj * (tj + 1) / 2 > t) --tj;
+    ti = t - tj * (tj + 1) / 2;
+}
+
+// C = L R', a workgroup a tile.
+template <Product KIND, int TILE, int LP, int RP, typename T>
+__global__ __launch_bounds__(kThreadsOf<TILE>, 1) void product_kernel(Operands o, Output<T> out) {
+    using S = Shape<TILE>;
+    constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
+    constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16;
+    extern __shared__ half8 stages[];
+    // one XCD's workgroups take neighbouring tiles: all rows of some columns
+    const int tiles = kSymmetric ? o.rows * (o.rows + 1) / 2 : o.rows * o.cols;
+    const int all = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int64_t b = all / tiles;
+    const int tile = all % tiles;
+    int ti = tile % o.rows, tj = tile / o.rows;
+    if constexpr (kSymmetric) triangle(tile, ti, tj);
+    float4v acc[MI][NI] = {};
+    multiply<TILE, LP, RP>(o, b, ti * TILE, tj * TILE, 0, o.depth, stages, acc);
     Coefficients k = o.k;
     if (KIND == Product::kPolynomial && o.first) k = o.first[b];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int i = ti * TILE + wave / S::kCols * (MI * 16) + lane % 16;
+    const int j = tj * TILE + wave % S::kCols * (NI * 16) + lane / 16 * 4;
 #pragma unroll
     for (int x = 0; x < MI; ++x)
 #pragma unroll
-        for (int y = 0; y < NI; ++y) {
-            const int i = i0 + wi + x * 16 + lane % 16, j = j0 + wj + y * 16 + lane / 16 * 4;
-            float v[4];
+        for (int y = 0; y < NI; ++y)
+            finish<KIND, T>(o, out, b, k, i + x * 16, j + y * 16, !kSymmetric || ti != tj, acc[x][y]);
+}
+
+// A symmetric product whose tiles fill the GPU badly: kWorkers workgroups share all stages of all
+// tiles evenly, in order, and leave each part of a tile's sum in memory, in the order of the registers; the
+// part of worker w in tile t is part t + w.
+constexpr int kWorkers = 256;
+
+struct Shares {
+    float* parts;
+    int64_t stages;  // of all tiles
+    int depth;       // stages of a tile
+    __device__ __forceinline__ int64_t begin(int64_t w) const { return w * stages / kWorkers; }
+};
+
+template <int TILE, int LP, int RP>
+__global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Operands o, Shares s) {
+    using S = Shape<TILE>;
+    constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
+    extern __shared__ half8 stages[];
+    const int tiles = o.rows * (o.rows + 1) / 2;
+    const int64_t w = xcd_contiguous(blockIdx.x, kWorkers);
+    const int64_t end = s.begin(w + 1);
+    for (int64_t at = s.begin(w); at < end;) {
+        const int64_t t = at / s.depth;
+        const int64_t stop = (t + 1) * s.depth < end ? (t + 1) * s.depth : end;
+        int ti, tj;
+        triangle((int)(t % tiles), ti, tj);
+        float4v acc[MI][NI] = {};
+        multiply<TILE, LP, RP>(o, t / tiles, ti * TILE, tj * TILE, (int)(at - t * s.depth) * S::kDepth,
+                               (int)(stop - t * s.depth) * S::kDepth, stages, acc);
+        float* part = s.parts + (t + w) * (TILE * TILE) + threadIdx.x * 4;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = acc[x][y][q] * (1.0f / kScale);
-            if constexpr (KIND == Product::kPolynomial) {
-                const int64_t at = b * o.a.batch + (int64_t)i * o.a.ld + j;
-                const half4 h = *reinterpret_cast<const half4*>(o.a.hi + at);
-                const half4 w = *reinterpret_cast<const half4*>(o.a.lo + at);
+        for (int x = 0; x < MI; ++x)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    v[q] = k.b * ((float)h[q] + (float)w[q]) + k.c * v[q] + (i == j + q ? k.a * kScale : 0.0f);
-            }
-            if constexpr (KIND == Product::kLast) {
+            for (int y = 0; y < NI; ++y)
+                *reinterpret_cast<float4v*>(part + (x * NI + y) * (kThreads * 4)) = acc[x][y];
+        at = stop;
+        __syncthreads();  // every wave has read the last stage
+    }
+}
+
+// The parts of a tile, added in the workers' order; a workgroup takes kJoin of its 16 x 16 pieces a wave.
+constexpr int kJoin = 2;
+
+template <Product KIND, int TILE>
+__global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands o, Shares s) {
+    using S = Shape<TILE>;
+    constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
+    constexpr int kGroups = MI * NI / kJoin;
+    const int tiles = o.rows * (o.rows + 1) / 2;
+    const int64_t t = blockIdx.x / kGroups;
+    const int piece = blockIdx.x % kGroups * kJoin;
+    const int64_t b = t / tiles;
+    int ti, tj;
+    triangle((int)(t % tiles), ti, tj);
+    // the workers that hold the tile's first and last stage
+    const int64_t first = t * s.depth, last = first + s.depth - 1;
+    int64_t w0 = first * kWorkers / s.stages, w1 = last * kWorkers / s.stages;
+    while (s.begin(w0 + 1) <= first) ++w0;
+    while (s.begin(w1 + 1) <= last) ++w1;
+    float4v sum[kJoin] = {};
+    for (int64_t w = w0; w <= w1; ++w) {
+        if (s.begin(w) == s.begin(w + 1)) continue;  // a worker without a stage
+        const float* part = s.parts + (t + w) * (TILE * TILE) + threadIdx.x * 4;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (i < out.m && j + q < out.n)
-                        out.x[b * out.batch + i * out.si + (j + q) * out.sj] =
-                            (T)(v[q] * (out.scale / kScale));
-            } else {
-                half4 h, w;
+        for (int q = 0; q < kJoin; ++q)
+            sum[q] += *reinterpret_cast<const float4v*>(part + (piece + q) * (kThreads * 4));
+    }
+    Coefficients k = o.k;
+    if (KIND == Product::kPolynomial && o.first) k = o.first[b];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int i = ti * TILE + wave / S::kCols * (MI * 16) + lane % 16;
+    const int j = tj * TILE + wave % S::kCols * (NI * 16) + lane / 16 * 4;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    f16 hi, lo;
-                    split(v[q], hi, lo);
-                    h[q] = hi;
-                    w[q] = lo;
+    for (int q = 0; q < kJoin; ++q)
+        finish<KIND>(o, Output<f16>{}, b, k, i + (piece + q) / NI * 16, j + (piece + q) % NI * 16, ti != tj,
+                     sum[q]);
+}
+
+// Whole matrices of up to 64 x 256 in one workgroup each, with everything in local memory: X both ways
+// round, A and P, 160 KiB at the largest. The product kernels would take three launches a step of 4 us each,
+// whatever they compute. Instructions bound it, so a lane's places in the permuted rows are worked out
+// once: rows of a tile start at multiples of 16, and what a permutation takes from them is the lane's own.
+constexpr int kSmallSide = 64, kSmallLong = 256, kSmallThreads = 1024;
+
+struct SmallSteps {
+    int steps;
+    Coefficients k[kMaxSteps];
+};
+
+// Matrices in local memory lie in panels of 64 columns: 8 pieces a row, permuted as a stage's.
+struct LocalPlanes {
+    half8 *hi, *lo;
+    int panel;  // pieces from one panel to the next
+};
+
+__device__ __forceinline__ int permuted(int row, int p) { return piece_of<64>(row, p); }
+
+// A lane's operands of a tile: its row's piece of each half of a panel, from the tile's first row on.
+struct LaneOffsets {
+    int half[2];    // operands
+    int row, flip;  // a value's row and its permutation, as C holds it: four columns of one row
+    int column;     // of the first of the four, 0 to 12
+    __device__ __forceinline__ explicit LaneOffsets(int lane) {
+        const int r = lane % 16;
+        half[0] = r * 8 + permuted(r, lane / 16);
+        half[1] = r * 8 + permuted(r, 4 + lane / 16);
+        row = r;
+        flip = permuted(r, 0);
+        column = lane / 16 * 4;
+    }
+};
+
+// acc += the 16 x 16 tiles of L R' for NL tiles of rows from L's row i on (every 16) and R's 16 rows from j on,
+// over one panel.
+template <int NL>
+__device__ __forceinline__ void local_product(LocalPlanes l, int i, LocalPlanes r, int j, int panel,
+                                              const LaneOffsets& at, float4v (&acc)[NL]) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+        const int rr = panel * r.panel + j * 8 + at.half[kk];
+        const half8 rh = r.hi[rr], rl = r.lo[rr];
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+            const int ll = panel * l.panel + (i + x * 16) * 8 + at.half[kk];
+            const half8 lh = l.hi[ll], lw = l.lo[ll];
+            acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rh, lh, acc[x], 0, 0, 0);
+            acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rl, lh, acc[x], 0, 0, 0);
+            acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rh, lw, acc[x], 0, 0, 0);
+        }
+    }
+}
+
+// The tile at row i and column j (multiples of 16) of a matrix, and with `t` of its transpose.
+__device__ __forceinline__ void local_store(LocalPlanes m, const LocalPlanes* t, int i, int j,
+                                            const LaneOffsets& at, const float (&v)[4]) {
+    half4 h, w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        f16 hi, lo;
+        split(v[q], hi, lo);
+        h[q] = hi;
+        w[q] = lo;
+    }
+    const int to = (j / 64 * m.panel + (i + at.row) * 8 + ((j % 64 + at.column) / 8 ^ at.flip)) * 8 + at.column % 8;
+    *reinterpret_cast<half4*>(reinterpret_cast<f16*>(m.hi) + to) = h;
+    *reinterpret_cast<half4*>(reinterpret_cast<f16*>(m.lo) + to) = w;
+    if (t) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int r = at.column + q;
+            const int too = ((j + r) * 8 + ((i + at.row) / 8 ^ permuted(r, 0))) * 8 + at.row % 8;
+            reinterpret_cast<f16*>(t->hi)[too] = h[q];
+            reinterpret_cast<f16*>(t->lo)[too] = w[q];
+        }
+    }
+}
+
+// pieces of X (either way round) and of A or P in one plane
+__host__ __device__ constexpr int small_x(int n) { return kSmallSide * n / 8; }
+constexpr int kSmallA = kSmallSide * kSmallSide / 8;
+
+// n: X's columns padded to whole panels.
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Output<T> out, int n, SmallSteps s,
+                                                              float eps) {
+    extern __shared__ half8 local[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    constexpr int kWaves = kSmallThreads / 64, kTiles = kSmallSide / 16;
+    static_assert(kTiles * kTiles == kWaves && kSmallLong / 16 == kWaves, "a tile of A, a column of X a wave");
+    const int xs = small_x(n);
+    const LocalPlanes x{local, local + xs, kSmallA}, xt{local + 2 * xs, local + 3 * xs, 0};
+    const LocalPlanes a{local + 4 * xs, local + 4 * xs + kSmallA, 0};
+    const LocalPlanes p{local + 4 * xs + 2 * kSmallA, local + 4 * xs + 3 * kSmallA, 0};
+    const LaneOffsets at(lane);
+
+    // G once, in registers; its contiguous index over the lanes
+    constexpr int kMine = kSmallSide * kSmallLong / kSmallThreads;
+    const T* g = in.x + blockIdx.x * in.batch;
+    const bool tall = in.sj != 1;
+    float v[kMine];
+    double sum = 0.0;
+    const auto place = [&](int q, int& i, int& j) {
+        i = tall ? threadIdx.x % kSmallSide : q * (kSmallThreads / kSmallLong) + threadIdx.x / kSmallLong;
+        j = tall ? q * (kSmallThreads / kSmallSide) + threadIdx.x / kSmallSide : threadIdx.x % kSmallLong;
+    };
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+        int i, j;
+        place(q, i, j);
+        v[q] = i < in.m && j < in.n ? (float)g[i * in.si + j * in.sj] : 0.0f;
+        sum += (double)v[q] * (double)v[q];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    double* sums = reinterpret_cast<double*>(p.hi);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += sums[w];
+    int e;
+    Coefficients first;
+    scale_of(sum, s.k[0], eps, e, first);
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+        int i, j;
+        place(q, i, j);
+        if (j >= n) continue;
+        f16 hi, lo;
+        split(ldexpf(v[q], kScaleExp - e), hi, lo);
+        const int to = (j / 64 * kSmallA + i * 8 + permuted(i, j % 64 / 8)) * 8 + j % 8;
+        const int too = (j * 8 + permuted(j, i / 8)) * 8 + i % 8;
+        reinterpret_cast<f16*>(x.hi)[to] = hi;
+        reinterpret_cast<f16*>(x.lo)[to] = lo;
+        reinterpret_cast<f16*>(xt.hi)[too] = hi;
+        reinterpret_cast<f16*>(xt.lo)[too] = lo;
+    }
+    __syncthreads();
+
+    const int ti = wave / kTiles * 16, tj = wave % kTiles * 16;  // the wave's tile of A and P
+    const int col = wave * 16;                                   // and its columns of X
+    for (int step = 0; step < s.steps; ++step) {
+        const Coefficients k = step == 0 ? first : s.k[step];
+        float4v acc[1] = {};
+        for (int q = 0; q < n / 64; ++q) local_product<1>(x, ti, x, tj, q, at, acc);
+        float gram[4], poly[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) gram[c] = acc[0][c] * (1.0f / kScale);
+        local_store(a, nullptr, ti, tj, at, gram);
+        __syncthreads();
+        acc[0] = float4v{};
+        local_product<1>(a, ti, a, tj, 0, at, acc);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            poly[c] = k.b * gram[c] + k.c * (acc[0][c] * (1.0f / kScale)) +
+                      (ti + at.row == tj + at.column + c ? k.a * kScale : 0.0f);
+        local_store(p, nullptr, ti, tj, at, poly);
+        __syncthreads();
+        float4v next[kTiles] = {};
+        if (col < n) local_product<kTiles>(p, 0, xt, col, 0, at, next);
+        const bool last = step + 1 == s.steps;
+        __syncthreads();
+        if (col < n) {
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y) {
+                float w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[c] = next[y][c] * (1.0f / kScale);
+                if (!last) {
+                    local_store(x, &xt, y * 16, col, at, w);
+                    continue;
                 }
-                const int64_t at = b * o.c.batch + (int64_t)i * o.c.ld + j;
-                *reinterpret_cast<half4*>(o.c.hi + at) = h;
-                *reinterpret_cast<half4*>(o.c.lo + at) = w;
-                if (!kSymmetric || ti != tj) {
+                const int i = y * 16 + at.row, j = col + at.column;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int64_t att = b * o.ct.batch + (int64_t)(j + q) * o.ct.ld + i;
-                        o.ct.hi[att] = h[q];
-                        o.ct.lo[att] = w[q];
-                    }
-                }
+                for (int c = 0; c < 4; ++c)
+                    if (i < out.m && j + c < out.n)
+                        out.x[blockIdx.x * out.batch + i * out.si + (j + c) * out.sj] =
+                            (T)(w[c] * (out.scale / kScale));
             }
         }
+        __syncthreads();
+    }
 }
 
 // The tiles of a call: of the symmetric products and of the others. Sides are padded to the larger.
@@ -330,12 +638,26 @@ struct Tiles {
 
 int64_t padded(int64_t side, int tile) { return (side + tile - 1) / tile * tile; }
 
+// Whether a symmetric product's stages are shared out evenly. It leaves no CU idle in the last round, and
+// costs a launch and the parts' way through memory, about 10 us: a round of tiles of 128 takes 30 us for
+// 1000 values of the summed index. 136 tiles from 2048 measured 60 us as they are and 43 shared out,
+// from 8192 200 and 117.
+bool shared(int tile, int64_t tiles, int64_t depth) {
+    if (tile != 128) return false;
+    const double rounds = tiles / 256.0, idle = std::ceil(rounds) - rounds;
+    return idle * depth >= 512.0;
+}
+
 // The pair that takes the least time by the measured rates, counting whole rounds of the 256 CUs and the
 // padding.
 Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
-    const auto cost = [&](int tile, int64_t tiles, int64_t depth) {
+    const auto cost = [&](int tile, int64_t tiles, int64_t depth, bool symmetric) {
         const double rate = tile == 256 ? 1.0 : tile == 128 ? 0.76 : 0.5;
-        return (double)((batch * tiles + 255) / 256) * tile * tile * depth / rate;
+        const double rounds = symmetric && shared(tile, batch * tiles, depth)
+                                  ? batch * tiles / 256.0
+                                  : (double)((batch * tiles + 255) / 256);
+        // in units of 1/720000 us; the second launch of shared products takes 10 us
+        return rounds * tile * tile * depth / rate + (symmetric && shared(tile, batch * tiles, depth) ? 7.2e6 : 0.0);
     };
     Tiles best{64, 64};
     double least = INFINITY;
@@ -344,7 +666,8 @@ Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
             const Tiles t{s, u};
             const int64_t pm = padded(m, t.pad()), pn = padded(n, t.pad());
             const int64_t ms = pm / s;
-            const double c = cost(s, ms * (ms + 1) / 2, pn + pm) + cost(u, pm / u * (pn / u), pm);
+            const double c = cost(s, ms * (ms + 1) / 2, pn, true) + cost(s, ms * (ms + 1) / 2, pm, true) +
+                             cost(u, pm / u * (pn / u), pm, false);
             if (c < least) {
                 least = c;
                 best = t;
@@ -355,14 +678,22 @@ Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
 
 // The workspace: norm parts and first coefficients, then the planes of X and X' twice, A and P.
 struct Layout {
-    int64_t parts, first, x[2], xt[2], a, p, bytes;  // byte offsets
+    int64_t parts, first, x[2], xt[2], a, p, shares, bytes;  // byte offsets
     Tiles tiles;
     int m, n;
+    bool small;  // nothing else then
 };
 
 Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     Layout w;
     const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    w.small = m <= kSmallSide && n <= kSmallLong;
+    if (w.small) {
+        w.m = kSmallSide;
+        w.n = (int)padded(n, 64);
+        w.bytes = 0;
+        return w;
+    }
     w.tiles = tiles_of(batch, m, n);
     w.m = (int)padded(m, w.tiles.pad());
     w.n = (int)padded(n, w.tiles.pad());
@@ -382,28 +713,47 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     }
     w.a = take(as);
     w.p = take(as);
+    const int64_t ms = w.m / w.tiles.symmetric, tiles = batch * ms * (ms + 1) / 2;
+    const bool any = shared(w.tiles.symmetric, tiles, w.n) || shared(w.tiles.symmetric, tiles, w.m);
+    w.shares = take(any ? (tiles + kWorkers) * w.tiles.symmetric * w.tiles.symmetric * (int64_t)sizeof(float) : 0);
     w.bytes = at + 256;
     return w;
 }
 
+template <typename K>
+bool allow_local(K kernel, size_t local) {
+    return local <= 65536 ||
+           hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)local) == hipSuccess;
+}
+
 template <Product KIND, int TILE, int LP, int RP, typename T>
-int launch_product(const Operands& o, const Output<T>& out, int64_t batch, hipStream_t stream) {
+int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float* parts, hipStream_t stream) {
     using S = Shape<TILE>;
     constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
-    constexpr size_t local = (size_t)2 * (LP + RP) * TILE * S::kDepth * sizeof(f16);
+    constexpr size_t local = (size_t)S::kStages * (LP + RP) * TILE * S::kDepth * sizeof(f16);
+    const int64_t tiles = batch * (kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols);
+    if constexpr (kSymmetric && TILE == 128) {
+        if (shared(TILE, tiles, o.depth)) {
+            const auto kernel = shared_product_kernel<TILE, LP, RP>;
+            if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
+            const Shares s{parts, tiles * (o.depth / S::kDepth), o.depth / S::kDepth};
+            kernel<<<kWorkers, kThreadsOf<TILE>, local, stream>>>(o, s);
+            constexpr int kGroups = TILE / S::kRows / 16 * (TILE / S::kCols / 16) / kJoin;
+            join_product_kernel<KIND, TILE><<<(unsigned)(tiles * kGroups), kThreadsOf<TILE>, 0, stream>>>(o, s);
+            return launch_status();
+        }
+    }
     const auto kernel = product_kernel<KIND, TILE, LP, RP, T>;
-    if (local > 65536 &&
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)local) != hipSuccess)
-        return TRIVANCE_EHIP;
-    const int64_t tiles = kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols;
-    kernel<<<(unsigned)(tiles * batch), S::kRows * S::kCols * 64, local, stream>>>(o, out);
+    if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
+    kernel<<<(unsigned)tiles, kThreadsOf<TILE>, local, stream>>>(o, out);
     return launch_status();
 }
 
 // A product by the call's tiles. `exact`: X0 has one plane.
 template <Product KIND, typename T>
-int product(Operands o, const Output<T>& out, int64_t batch, int tile, bool exact, hipStream_t stream) {
+int product(Operands o, const Output<T>& out, int64_t batch, int tile, bool exact, float* parts,
+            hipStream_t stream) {
     o.rows = o.rows / tile;
     o.cols = o.cols / tile;
     // in a first step from 16 bits the lower plane of X is zero: both operands of the Gram matrix, the
@@ -412,8 +762,8 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, bool exac
 #define LAUNCH(TILE)                                                                                 \
     if (tile == TILE) {                                                                              \
         if constexpr (KIND != Product::kPolynomial)                                                  \
-            if (exact) return launch_product<KIND, TILE, LP, 1>(o, out, batch, stream);              \
-        return launch_product<KIND, TILE, 2, 2>(o, out, batch, stream);                              \
+            if (exact) return launch_product<KIND, TILE, LP, 1>(o, out, batch, parts, stream);       \
+        return launch_product<KIND, TILE, 2, 2>(o, out, batch, parts, stream);                       \
     }
     if constexpr (KIND == Product::kUpdate || KIND == Product::kLast) LAUNCH(256)
     LAUNCH(128)
@@ -425,6 +775,15 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, bool exac
 template <typename T>
 int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, float eps, const Layout& w,
         void* workspace, hipStream_t stream) {
+    if (w.small) {
+        SmallSteps s;
+        s.steps = steps;
+        for (int i = 0; i < steps; ++i) s.k[i] = {k[3 * i], k[3 * i + 1], k[3 * i + 2]};
+        const size_t local = sizeof(half8) * (4 * small_x(w.n) + 4 * kSmallA);
+        if (!allow_local(&small_kernel<T>, local)) return TRIVANCE_EHIP;
+        small_kernel<T><<<(unsigned)batch, kSmallThreads, local, stream>>>(in, out, w.n, s, eps);
+        return launch_status();
+    }
     char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
     const auto planes = [&](int64_t offset, int rows, int ld) {
         f16* hi = reinterpret_cast<f16*>(base + offset);
@@ -432,6 +791,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
     };
     double* parts = reinterpret_cast<double*>(base + w.parts);
     Coefficients* first = reinterpret_cast<Coefficients*>(base + w.first);
+    float* shares = reinterpret_cast<float*>(base + w.shares);
     Planes x[2], xt[2];
     for (int i = 0; i < 2; ++i) {
         x[i] = planes(w.x[i], w.m, w.n);
@@ -439,7 +799,8 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
     }
     const Planes a = planes(w.a, w.m, w.m), p = planes(w.p, w.m, w.m);
     const int rows = in.sj != 1 ? in.n : in.m;
-    const int nparts = rows < kNormParts ? rows : kNormParts;
+    const int64_t pieces = (int64_t)rows * (((rows == in.n ? in.m : in.n) + 256 * kVec<T> - 1) / (256 * kVec<T>));
+    const int nparts = (int)(pieces < kNormParts ? pieces : kNormParts);
     const unsigned nb = (unsigned)batch;
     norm_parts_kernel<T><<<dim3(nparts, nb), 256, 0, stream>>>(in, parts);
     split_kernel<T><<<dim3(w.n / 64, w.m / 64, nb), 256, 0, stream>>>(
@@ -451,14 +812,14 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
         const bool exact = s == 0 && sizeof(T) == 2;
         const Output<f16> none{};
         rc = product<Product::kGram>({x[q], x[q], w.n, w.m, w.m, a, a, a, c, nullptr}, none, batch,
-                                     w.tiles.symmetric, exact, stream);
+                                     w.tiles.symmetric, exact, shares, stream);
         if (rc) break;
         rc = product<Product::kPolynomial>({a, a, w.m, w.m, w.m, p, p, a, c, s == 0 ? first : nullptr}, none,
-                                           batch, w.tiles.symmetric, false, stream);
+                                           batch, w.tiles.symmetric, false, shares, stream);
         if (rc) break;
         const Operands update{p, xt[q], w.m, w.m, w.n, x[1 - q], xt[1 - q], a, c, nullptr};
-        rc = s + 1 < steps ? product<Product::kUpdate>(update, none, batch, w.tiles.update, exact, stream)
-                           : product<Product::kLast>(update, out, batch, w.tiles.update, exact, stream);
+        rc = s + 1 < steps ? product<Product::kUpdate>(update, none, batch, w.tiles.update, exact, shares, stream)
+                           : product<Product::kLast>(update, out, batch, w.tiles.update, exact, shares, stream);
     }
     return rc;
 }
@@ -506,12 +867,12 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
     const int64_t need = trivance_orthogonalize_workspace_bytes(batch, rows, cols);
     if (need < 0) return (int)need;
     if (steps > kMaxSteps || !coefficients_ok(coefficients, steps)) return TRIVANCE_EUNSUPPORTED;
-    if (need == 0) return TRIVANCE_OK;
+    if (batch == 0 || rows == 0 || cols == 0) return TRIVANCE_OK;
     if (!x || !out || !rows_fit(batch, rows, cols, x_batch_stride, x_row_stride) ||
         !rows_fit(batch, rows, cols, out_batch_stride, out_row_stride) ||
         !rows_distinct(batch, rows, cols, out_batch_stride, out_row_stride))
         return TRIVANCE_EINVAL;
-    if (workspace_bytes < need || !workspace) return TRIVANCE_ESIZE;
+    if (workspace_bytes < need || (need > 0 && !workspace)) return TRIVANCE_ESIZE;
     const Layout w = layout_of(batch, rows, cols);
     const bool tall = rows > cols;
     const int m = (int)(tall ? cols : rows), n = (int)(tall ? rows : cols);
