@@ -17,7 +17,10 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "device.h"
 #include "operators.h"
+
+#pragma clang fp contract(fast)
 
 namespace trivance {
 namespace {
@@ -27,12 +30,14 @@ constexpr int kMaxExperts = 4096;
 constexpr int64_t kMaxGridX = 1 << 20;
 constexpr int64_t kMaxGridY = 65535;
 
-// exp(x - max) of a row's values in place, and one over their sum; the maximum is -inf where every
-// expert is excluded: all probabilities are zero then.
+// A row's logits, as fp32, become exp(x - max); returns their maximum's place in it, minus infinity where every
+// expert is excluded (all are zero then). Exponents are taken to base two: one multiplication and the
+// hardware's instruction, which is good to a unit in the last place.
 template <typename T, int L, int NV>
-__device__ __forceinline__ float row_exp(float (&v)[NV][kVec<T>]) {
+__device__ __forceinline__ void row_exp(float (&v)[NV][kVec<T>]) {
     constexpr int V = kVec<T>;
-    float m = -__builtin_inff(), s = 0.0f;
+    constexpr float kLog2E = 1.44269504088896340736f;
+    float m = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -42,13 +47,29 @@ __device__ __forceinline__ float row_exp(float (&v)[NV][kVec<T>]) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            v[j][k] = expf(v[j][k] - m);
-            s += v[j][k];
-        }
-    s = lanes_sum<L>(s);
-    return s == 0.0f ? 0.0f : 1.0f / s;
+        for (int k = 0; k < V; ++k) v[j][k] = __builtin_amdgcn_exp2f((v[j][k] - m) * kLog2E);
 }
+
+// One over a sum of exponentials; zero for the sum of none.
+__device__ __forceinline__ float over(float s) { return s == 0.0f ? 0.0f : 1.0f / s; }
+
+// A lane's part of every row: NV vectors, one every L vectors. What lies beyond the row's end is
+// minus infinity: an excluded expert.
+template <typename T, int L, int NV>
+struct Row {
+    typename Packed<T>::type v[NV];
+    __device__ __forceinline__ void fetch(const T* x, int lane, int experts) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            v[j] = load_packed<T>(x, (j * L + lane) * kVec<T>, experts, (T)-__builtin_inff());
+    }
+    __device__ __forceinline__ void values(float (&out)[NV][kVec<T>]) const {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int k = 0; k < kVec<T>; ++k) out[j][k] = (float)v[j][k];
+    }
+};
 
 template <typename T>
 struct Counts {
@@ -61,6 +82,7 @@ struct Counts {
     float* part_probs;  // [ranks][chunks][experts]
     int64_t ranks, tokens, rank_stride, token_stride, counts_rank, probs_rank, chunks, per;
     int experts, top_k, wide_ids;
+    FastDiv32 by_top_k;
 };
 
 template <typename T, int L, int NV>
@@ -77,23 +99,37 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
         __syncthreads();
         for (int e = threadIdx.x; e <= a.experts; e += kThreads) hist[e] = 0;
         __syncthreads();
+        // the logits first, so that they are on their way during the counting
+        Row<T, L, NV> next;
+        const T* x = a.logits + r * a.rank_stride;
+        int64_t t = t1 + group;
+        bool used = t < t2 && (!mask || mask[t]);
+        if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
         const int64_t first = (r * a.tokens + t1) * a.top_k;
-        for (int64_t i = threadIdx.x; i < (t2 - t1) * a.top_k; i += kThreads) {
-            if (mask && !mask[t1 + i / a.top_k]) continue;
+        const int slots = (int)(t2 - t1) * a.top_k;
+        for (int i = threadIdx.x; i < slots; i += kThreads) {
+            if (mask && !mask[t1 + fdiv32(i, a.by_top_k)]) continue;
             const int64_t e = a.wide_ids ? static_cast<const int64_t*>(a.ids)[first + i]
                                          : static_cast<const int*>(a.ids)[first + i];
             if (e >= 0 && e < a.experts) atomicAdd(&hist[e], 1);
         }
         float sum[NV][V] = {};
         int live = 0;
-        for (int64_t t = t1 + group; t < t2; t += G) {
-            if (mask && !mask[t]) continue;
-            const T* x = a.logits + r * a.rank_stride + t * a.token_stride;
+        while (t < t2) {
+            const bool use = used;
             float v[NV][V];
+            next.values(v);
+            t += G;
+            used = t < t2 && (!mask || mask[t]);
+            if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
+            if (!use) continue;
+            row_exp<T, L, NV>(v);
+            float s = 0.0f;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                load_row<T>(x, (int64_t)(j * L + lane) * V, a.experts, -__builtin_inff(), v[j]);
-            const float inv = row_exp<T, L, NV>(v);
+#pragma unroll
+                for (int k = 0; k < V; ++k) s += v[j][k];
+            const float inv = over(lanes_sum<L>(s));
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -205,33 +241,41 @@ __global__ __launch_bounds__(kThreads) void balance_gradient_kernel(Gradient<T> 
                 const int e = (j * L + lane) * V + k;
                 w[j][k] = e < a.experts ? (float)(f * counts[e]) : 0.0f;
             }
-        for (int64_t t = (int64_t)blockIdx.x * G + group; t < a.tokens; t += (int64_t)gridDim.x * G) {
+        const int64_t step = (int64_t)gridDim.x * G;
+        Row<T, L, NV> next;
+        const T* x = a.logits + r * a.rank_stride;
+        int64_t t = (int64_t)blockIdx.x * G + group;
+        bool used = t < a.tokens && (!mask || mask[t]);
+        if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
+        while (t < a.tokens) {
+            const bool use = used;
             T* d = a.dlogits + r * a.d_rank + t * a.d_token;
             float v[NV][V];
-            if (mask && !mask[t]) {  // what lies there is not read
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int k = 0; k < V; ++k) v[j][k] = 0.0f;
-            } else {
-                const T* x = a.logits + r * a.rank_stride + t * a.token_stride;
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    load_row<T>(x, (int64_t)(j * L + lane) * V, a.experts, -__builtin_inff(), v[j]);
-                const float inv = row_exp<T, L, NV>(v);
-                float s = 0.0f;
+            next.values(v);
+            t += step;
+            used = t < a.tokens && (!mask || mask[t]);
+            if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
+            if (use) {
+                row_exp<T, L, NV>(v);
+                float s = 0.0f, q = 0.0f;
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
-                        v[j][k] *= inv;
-                        s += v[j][k] * w[j][k];
+                        s += v[j][k];
+                        q += v[j][k] * w[j][k];
                     }
-                s = lanes_sum<L>(s);
+                const float inv = over(lanes_sum<L>(s));
+                q = lanes_sum<L>(q) * inv;
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
-                    for (int k = 0; k < V; ++k) v[j][k] *= w[j][k] - s;
+                    for (int k = 0; k < V; ++k) v[j][k] = v[j][k] * inv * (w[j][k] - q);
+            } else {  // what lies there is not read
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int k = 0; k < V; ++k) v[j][k] = 0.0f;
             }
 #pragma unroll
             for (int j = 0; j < NV; ++j)
@@ -300,8 +344,10 @@ int run_counts(const Counts<T>& a, hipStream_t stream) {
 template <typename T>
 int run_gradient(const Gradient<T>& a, hipStream_t stream) {
     const int rows = kThreads / row_lanes(a.experts, kVec<T>);
-    const dim3 grid((unsigned)imin((a.tokens + rows - 1) / rows, kMaxGridX),
-                    (unsigned)imin(a.ranks, kMaxGridY));
+    // as many workgroups as the GPU holds, with the same number of rows each
+    const int64_t units = (a.tokens + rows - 1) / rows, most = imax(1, 256 * 8 / a.ranks);
+    const int64_t each = (units + most - 1) / most;
+    const dim3 grid((unsigned)((units + each - 1) / each), (unsigned)imin(a.ranks, kMaxGridY));
     with_shape<T>(a.experts, [&](auto l, auto nv) {
         balance_gradient_kernel<T, l(), nv()><<<grid, kThreads, 0, stream>>>(a);
     });
@@ -364,7 +410,8 @@ int trivance_balance_counts(const void* logits, const void* chosen, const uint8_
             Counts<T>{static_cast<const T*>(logits), chosen, mask, counts, probs, part,
                       reinterpret_cast<float*>(part + ranks * chunks * (experts + 1)), ranks, tokens,
                       rank_stride, token_stride, counts_rank_stride, probs_rank_stride, chunks, per,
-                      (int)experts, (int)top_k, id_dtype == TRIVANCE_I64},
+                      (int)experts, (int)top_k, id_dtype == TRIVANCE_I64,
+                      make_fastdiv32((uint32_t)top_k)},
             s);
     };
     return dtype == TRIVANCE_F32 ? run(float{}) : dtype == TRIVANCE_BF16 ? run(bf16{}) : run(f16{});

@@ -18,12 +18,14 @@
 
 #include "operators.h"
 
+#pragma clang fp contract(fast)
+
 namespace trivance {
 namespace {
 
 constexpr int kThreads = 256;      // lanes of a workgroup whose rows take fewer
 constexpr int kWide = 1024;        // lanes of the widest rows' groups
-constexpr int64_t kMaxGridX = 1 << 20;
+constexpr int64_t kBlocks = 8;     // of that many lanes, of the forward pass on one CU
 constexpr int64_t kMaxGridY = 65535;
 
 template <int LANES>
@@ -63,6 +65,46 @@ __device__ __forceinline__ void row_sums(float& x, float& y, float2* slots) {
     }
 }
 
+// A lane's part of every row: NV vectors of V values, one every LANES vectors. Rows that do not end with a
+// vector lend the last lane values of the one before: it reads and writes them as well, the same bits,
+// and leaves them out of its sums. So a row needs no path for its end; rows shorter than a vector
+// take V = 1.
+template <int V, int LANES, int NV>
+struct Columns {
+    int first[NV];  // of the lane's values
+    int skip[NV];   // those that count for another lane; V: the lane has none
+    __device__ __forceinline__ Columns(int lane, int width) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = (j * LANES + lane) * V;
+            first[j] = i + V <= width ? i : width - V;
+            skip[j] = i < width ? i - first[j] : V;
+        }
+    }
+    // The sum of f(j, k) over the values that count.
+    template <typename F>
+    __device__ __forceinline__ float sum(F f) const {
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float part = 0.0f;
+            if (skip[j] == 0) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) part += f(j, k);
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (k >= skip[j]) part += f(j, k);
+            }
+            s += part;
+        }
+        return s;
+    }
+};
+
+template <typename T, int V>
+using Some = T __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+
 template <typename T>
 struct Forward {
     const T* x;
@@ -74,51 +116,61 @@ struct Forward {
     int weight_type;
 };
 
-template <typename T, int LANES, int NV>
+// The group of lanes of a row: known to be the same in a whole wave where a row takes one or more.
+template <int LANES>
+__device__ __forceinline__ int group_of_lane() {
+    if constexpr (LANES > 64) return 0;
+    const int g = threadIdx.x / LANES;
+    if constexpr (LANES == 64) return __builtin_amdgcn_readfirstlane(g);
+    return g;
+}
+
+template <typename T, int V, int LANES, int NV>
 __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> a) {
-    constexpr int V = kVec<T>, G = kBlock<LANES> / LANES;
+    constexpr int G = kBlock<LANES> / LANES;
     __shared__ float slots[2][kWide / 64];
-    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES, group = group_of_lane<LANES>();
+    const Columns<V, LANES, NV> own(lane, (int)a.width);
     const float inv = 1.0f / (float)a.width;
     float gamma[NV][V], beta[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int64_t i = (int64_t)(j * LANES + lane) * V;
-        load_weights<V>(a.gamma, a.weight_type, i, a.width, 1.0f, gamma[j]);
-        load_weights<V>(a.beta, a.weight_type, i, a.width, 0.0f, beta[j]);
+        load_weights<V>(a.gamma, a.weight_type, own.first[j], a.width, 1.0f, gamma[j]);
+        load_weights<V>(a.beta, a.weight_type, own.first[j], a.width, 0.0f, beta[j]);
     }
+    Some<T, V> next[NV];
+    const auto fetch = [&](int64_t r, int64_t t) {
+        const T* x = a.x + r * a.x_rank + t * a.x_token;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (own.skip[j] < V) next[j] = *reinterpret_cast<const Some<T, V>*>(x + own.first[j]);
+    };
+    const int64_t step = (int64_t)gridDim.x * G;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
-        for (int64_t t0 = (int64_t)blockIdx.x * G; t0 < a.tokens; t0 += (int64_t)gridDim.x * G) {
-            const int64_t t = t0 + group;
-            if (G > 1 && t >= a.tokens) continue;  // whole groups of lanes, never a workgroup's row
-            const T* x = a.x + r * a.x_rank + t * a.x_token;
-            float v[NV][V], s = 0.0f;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-                load_row<T>(x, (int64_t)(j * LANES + lane) * V, a.width, 0.0f, v[j]);
+        int64_t t = (int64_t)blockIdx.x * G + group;
+        if (t < a.tokens) fetch(r, t);
+        for (; t < a.tokens; t += step) {  // whole groups of lanes, whole workgroups where a row takes one
+            float v[NV][V];
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int k = 0; k < V; ++k) s += v[j][k];
-            const float mean = row_sum<LANES>(s, slots[0]) * inv;
-            float q = 0.0f;
+                for (int k = 0; k < V; ++k) v[j][k] = (float)next[j][k];
+            if (t + step < a.tokens) fetch(r, t + step);  // on its way during this row's sums
+            const float mean = row_sum<LANES>(own.sum([&](int j, int k) { return v[j][k]; }), slots[0]) * inv;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int64_t i = (int64_t)(j * LANES + lane) * V;
+            for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    v[j][k] -= mean;
-                    if (i + k < a.width) q += v[j][k] * v[j][k];
-                }
-            }
-            const float rstd = 1.0f / sqrtf(row_sum<LANES>(q, slots[1]) * inv + a.eps);
+                for (int k = 0; k < V; ++k) v[j][k] -= mean;
+            const float square =
+                row_sum<LANES>(own.sum([&](int j, int k) { return v[j][k] * v[j][k]; }), slots[1]);
+            const float rstd = 1.0f / sqrtf(square * inv + a.eps);
             T* y = a.y + r * a.y_rank + t * a.y_token;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float o[V];
+                Some<T, V> o;
 #pragma unroll
-                for (int k = 0; k < V; ++k) o[k] = v[j][k] * rstd * gamma[j][k] + beta[j][k];
-                store_row<T, V>(y, (int64_t)(j * LANES + lane) * V, a.width, o);
+                for (int k = 0; k < V; ++k) o[k] = (T)(v[j][k] * rstd * gamma[j][k] + beta[j][k]);
+                if (own.skip[j] < V) *reinterpret_cast<Some<T, V>*>(y + own.first[j]) = o;
             }
             if (lane == 0) {
                 if (a.mean) a.mean[r * a.tokens + t] = mean;
@@ -191,58 +243,69 @@ __device__ __forceinline__ float* sums_of(const Backward<T>& a, int64_t r, int64
     return d ? d + r * a.grad_rank : nullptr;
 }
 
-template <typename T, int LANES, int NV>
+template <typename T, int V, int LANES, int NV>
 __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T> a) {
-    constexpr int V = kVec<T>, G = kBlock<LANES> / LANES;
+    constexpr int G = kBlock<LANES> / LANES;
     __shared__ float2 slots[2][kWide / 64];
     __shared__ float join[G > 1 ? kThreads * NV * V : 1];
-    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES, group = group_of_lane<LANES>();
+    const Columns<V, LANES, NV> own(lane, (int)a.width);
     const float inv = 1.0f / (float)a.width;
     float gamma[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        load_weights<V>(a.gamma, a.weight_type, (int64_t)(j * LANES + lane) * V, a.width, 1.0f,
-                        gamma[j]);
+        load_weights<V>(a.gamma, a.weight_type, own.first[j], a.width, 1.0f, gamma[j]);
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         const int64_t c = blockIdx.x, t1 = c * a.per;
         const int64_t t2 = t1 + a.per < a.tokens ? t1 + a.per : a.tokens;
         float dg[NV][V] = {}, db[NV][V] = {};
         int turn = 0;
-        for (int64_t t0 = t1; t0 < t2; t0 += G) {
-            const int64_t t = t0 + group;
-            if (G > 1 && t >= t2) continue;
+        Some<T, V> nx[NV], ndy[NV];
+        float nmean = 0.0f, nrstd = 0.0f;
+        const auto fetch = [&](int64_t t) {
             const T* x = a.x + r * a.x_rank + t * a.x_token;
             const T* dy = a.dy + r * a.dy_rank + t * a.dy_token;
-            const float mean = a.mean[r * a.tokens + t], rstd = a.rstd[r * a.tokens + t];
-            float h[NV][V], g[NV][V], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int64_t i = (int64_t)(j * LANES + lane) * V;
-                load_row<T>(x, i, a.width, 0.0f, h[j]);
-                load_row<T>(dy, i, a.width, 0.0f, g[j]);
-            }
+            for (int j = 0; j < NV; ++j)
+                if (own.skip[j] < V) {
+                    nx[j] = *reinterpret_cast<const Some<T, V>*>(x + own.first[j]);
+                    ndy[j] = *reinterpret_cast<const Some<T, V>*>(dy + own.first[j]);
+                }
+            nmean = a.mean[r * a.tokens + t];
+            nrstd = a.rstd[r * a.tokens + t];
+        };
+        // the next row is on its way during this row's sums, where there are registers for both
+        constexpr bool kAhead = NV * V * sizeof(T) <= 64;
+        int64_t t = t1 + group;
+        if (kAhead && t < t2) fetch(t);
+        for (; t < t2; t += G) {
+            if (!kAhead) fetch(t);
+            const float mean = nmean, rstd = nrstd;
+            float h[NV][V], g[NV][V];
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
+            for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
-                    h[j][k] = (h[j][k] - mean) * rstd;
+                    h[j][k] = ((float)nx[j][k] - mean) * rstd;
+                    g[j][k] = (float)ndy[j][k];
                     dg[j][k] += g[j][k] * h[j][k];
                     db[j][k] += g[j][k];
-                    g[j][k] *= gamma[j][k];  // zero beyond the row's end, where dy was filled so
-                    s1 += g[j][k];
-                    s2 += g[j][k] * h[j][k];
+                    g[j][k] *= gamma[j][k];
                 }
-            }
+            if (kAhead && t + G < t2) fetch(t + G);
+            float s1 = own.sum([&](int j, int k) { return g[j][k]; });
+            float s2 = own.sum([&](int j, int k) { return g[j][k] * h[j][k]; });
             row_sums<LANES>(s1, s2, slots[turn]);
             turn ^= 1;
+            s1 *= inv;
+            s2 *= inv;
             T* dx = a.dx + r * a.dx_rank + t * a.dx_token;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float o[V];
+                Some<T, V> o;
 #pragma unroll
-                for (int k = 0; k < V; ++k)
-                    o[k] = rstd * (g[j][k] - s1 * inv - h[j][k] * (s2 * inv));
-                store_row<T, V>(dx, (int64_t)(j * LANES + lane) * V, a.width, o);
+                for (int k = 0; k < V; ++k) o[k] = (T)(rstd * (g[j][k] - s1 - h[j][k] * s2));
+                if (own.skip[j] < V) *reinterpret_cast<Some<T, V>*>(dx + own.first[j]) = o;
             }
         }
 #pragma unroll
@@ -251,9 +314,12 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T
             if (!out) continue;
             if constexpr (G == 1) {
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    store_row<float, V>(out, (int64_t)(j * LANES + lane) * V, a.width,
-                                        which ? db[j] : dg[j]);
+                for (int j = 0; j < NV; ++j) {
+                    Some<float, V> o;
+#pragma unroll
+                    for (int k = 0; k < V; ++k) o[k] = which ? db[j][k] : dg[j][k];
+                    if (own.skip[j] < V) *reinterpret_cast<Some<float, V>*>(out + own.first[j]) = o;
+                }
             } else {
                 // the groups' sums, in the groups' order
                 constexpr int N = LANES * NV * V;
@@ -262,7 +328,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
                     for (int k = 0; k < V; ++k)
-                        join[group * N + (j * LANES + lane) * V + k] = which ? db[j][k] : dg[j][k];
+                        if (own.skip[j] < V) join[group * N + own.first[j] + k] = which ? db[j][k] : dg[j][k];
                 __syncthreads();
                 for (int i = threadIdx.x; i < N && i < a.width; i += kThreads) {
                     float s = 0.0f;
@@ -369,32 +435,38 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks_kernel(
 }
 
 // How a row lies in lanes: groups of 8 to 64 lanes with one vector each, then waves and larger groups
-// with up to 16 values a lane. kLong: in none.
-enum class Shape { k8, k16, k32, k64, k64x2, k64x4, k256x2, k256x4, k512x2, k512x4, k1024x2, k1024x4, kLong };
+// with 16 values a lane; 32 for the widest, whose workgroups would need more registers with 1024 lanes
+// than those have. kTiny: shorter than a vector; kLong: in no workgroup's registers.
+enum class Shape { kTiny, k8, k16, k32, k64, k64x2, k64x4, k256x2, k256x4, k512x2, k512x4, k512x8, kLong };
 
 template <typename T>
 Shape shape_of(int64_t width) {
     constexpr int V = kVec<T>;
     const int64_t n = (width + V - 1) / V;
+    if (width < V) return Shape::kTiny;
     if (n <= 8) return Shape::k8;
     if (n <= 16) return Shape::k16;
     if (n <= 32) return Shape::k32;
     if (n <= 64) return Shape::k64;
     if (n <= 128) return Shape::k64x2;
-    if (V == 4 && n <= 256) return Shape::k64x4;
+    if (V == 4) {
+        if (n <= 256) return Shape::k64x4;
+        if (n <= 512) return Shape::k256x2;
+        if (n <= 1024) return Shape::k256x4;
+        if (n <= 2048) return Shape::k512x4;
+        if (n <= 4096) return Shape::k512x8;
+        return Shape::kLong;
+    }
     if (n <= 512) return Shape::k256x2;
-    if (V == 4 && n <= 1024) return Shape::k256x4;
     if (n <= 1024) return Shape::k512x2;
-    if (V == 4 && n <= 2048) return Shape::k512x4;
-    if (n <= 2048) return Shape::k1024x2;
-    if (V == 4 && n <= 4096) return Shape::k1024x4;
+    if (n <= 2048) return Shape::k512x4;
     return Shape::kLong;
 }
 
 // The rows that a workgroup takes at a time, and its lanes.
 int group_rows(Shape s) {
     switch (s) {
-        case Shape::k8: return kThreads / 8;
+        case Shape::kTiny: case Shape::k8: return kThreads / 8;
         case Shape::k16: return kThreads / 16;
         case Shape::k32: return kThreads / 32;
         case Shape::k64: case Shape::k64x2: case Shape::k64x4: return kThreads / 64;
@@ -404,8 +476,8 @@ int group_rows(Shape s) {
 
 int block_lanes(Shape s) {
     switch (s) {
-        case Shape::k512x2: case Shape::k512x4: return 512;
-        case Shape::k1024x2: case Shape::k1024x4: case Shape::kLong: return kWide;
+        case Shape::k512x2: case Shape::k512x4: case Shape::k512x8: return 512;
+        case Shape::kLong: return kWide;
         default: return kThreads;
     }
 }
@@ -423,30 +495,38 @@ int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
     return imax(rows, (per + rows - 1) / rows * rows);
 }
 
-#define TRIVANCE_NORM_SHAPES(RUN, RUN_LONG)                                      \
-    switch (shape) {                                                             \
-        case Shape::k8: RUN(8, 1); break;                                        \
-        case Shape::k16: RUN(16, 1); break;                                      \
-        case Shape::k32: RUN(32, 1); break;                                      \
-        case Shape::k64: RUN(64, 1); break;                                      \
-        case Shape::k64x2: RUN(64, 2); break;                                    \
-        case Shape::k64x4: if constexpr (kVec<T> == 4) RUN(64, 4); break;        \
-        case Shape::k256x2: RUN(256, 2); break;                                  \
-        case Shape::k256x4: if constexpr (kVec<T> == 4) RUN(256, 4); break;      \
-        case Shape::k512x2: RUN(512, 2); break;                                  \
-        case Shape::k512x4: if constexpr (kVec<T> == 4) RUN(512, 4); break;      \
-        case Shape::k1024x2: RUN(1024, 2); break;                                \
-        case Shape::k1024x4: if constexpr (kVec<T> == 4) RUN(1024, 4); break;    \
-        case Shape::kLong: RUN_LONG(); break;                                    \
+#define TRIVANCE_NORM_SHAPES(RUN, RUN_LONG)                                                   \
+    constexpr int V = kVec<T>;                                                                \
+    switch (shape) {                                                                          \
+        case Shape::kTiny: RUN(1, 8, 1); break;                                               \
+        case Shape::k8: RUN(V, 8, 1); break;                                                  \
+        case Shape::k16: RUN(V, 16, 1); break;                                                \
+        case Shape::k32: RUN(V, 32, 1); break;                                                \
+        case Shape::k64: RUN(V, 64, 1); break;                                                \
+        case Shape::k64x2: RUN(V, 64, 2); break;                                              \
+        case Shape::k64x4: if constexpr (V == 4) RUN(V, 64, 4); break;                        \
+        case Shape::k256x2: RUN(V, 256, 2); break;                                            \
+        case Shape::k256x4: if constexpr (V == 4) RUN(V, 256, 4); break;                      \
+        case Shape::k512x2: if constexpr (V == 8) RUN(V, 512, 2); break;                      \
+        case Shape::k512x4: RUN(V, 512, 4); break;                                            \
+        case Shape::k512x8: if constexpr (V == 4) RUN(V, 512, 8); break;                      \
+        case Shape::kLong: RUN_LONG(); break;                                                 \
     }
 
+// Workgroups of the forward pass: as many as the GPU holds, with the same number of rows each, so that
+// the weights are loaded once for all of them and a row's load overlaps the one before.
 template <typename T>
-int run_forward(const Forward<T>& a, hipStream_t stream) {
+int run_forward(Forward<T> a, hipStream_t stream) {
+    if (a.x_rank == a.tokens * a.x_token && a.y_rank == a.tokens * a.y_token) {  // rank after rank
+        a.tokens *= a.ranks;
+        a.ranks = 1;
+    }
     const Shape shape = shape_of<T>(a.width);
-    const int64_t rows = group_rows(shape);
-    const dim3 grid((unsigned)imin((a.tokens + rows - 1) / rows, kMaxGridX),
-                    (unsigned)imin(a.ranks, kMaxGridY));
-#define RUN(L, N) norm_forward_kernel<T, L, N><<<grid, kBlock<L>, 0, stream>>>(a)
+    const int64_t units = (a.tokens + group_rows(shape) - 1) / group_rows(shape);
+    const int64_t most = imax(1, 256 * kBlocks * kThreads / block_lanes(shape) / a.ranks);
+    const int64_t each = (units + most - 1) / most;
+    const dim3 grid((unsigned)((units + each - 1) / each), (unsigned)imin(a.ranks, kMaxGridY));
+#define RUN(V, L, N) norm_forward_kernel<T, V, L, N><<<grid, kBlock<L>, 0, stream>>>(a)
 #define RUN_LONG() norm_forward_long_kernel<T><<<grid, kWide, 0, stream>>>(a)
     TRIVANCE_NORM_SHAPES(RUN, RUN_LONG)
 #undef RUN
@@ -458,7 +538,7 @@ template <typename T>
 int run_backward(const Backward<T>& a, hipStream_t stream) {
     const Shape shape = shape_of<T>(a.width);
     const dim3 grid((unsigned)a.chunks, (unsigned)imin(a.ranks, kMaxGridY));
-#define RUN(L, N) norm_backward_kernel<T, L, N><<<grid, kBlock<L>, 0, stream>>>(a)
+#define RUN(V, L, N) norm_backward_kernel<T, V, L, N><<<grid, kBlock<L>, 0, stream>>>(a)
 #define RUN_LONG() norm_backward_long_kernel<T><<<grid, kWide, 0, stream>>>(a)
     TRIVANCE_NORM_SHAPES(RUN, RUN_LONG)
 #undef RUN

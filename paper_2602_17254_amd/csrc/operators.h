@@ -23,20 +23,32 @@ struct Packed {
     typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
-// Values i .. i + VEC of a row of `width` values as fp32; `fill` beyond the row's end.
+// A lane's vector of a row as it lies in memory, values i .. i + VEC; `fill` beyond the row's end.
+template <typename T>
+__device__ __forceinline__ typename Packed<T>::type load_packed(const T* row, int64_t i, int64_t width, T fill) {
+    constexpr int V = kVec<T>;
+    typename Packed<T>::type x;
+    if (i + V <= width) {
+        x = *reinterpret_cast<const typename Packed<T>::type*>(row + i);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = fill;
+        if (i < width) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (i + k < width) x[k] = row[i + k];
+        }
+    }
+    return x;
+}
+
+// The same as fp32.
 template <typename T>
 __device__ __forceinline__ void load_row(const T* row, int64_t i, int64_t width, float fill,
                                          float (&out)[kVec<T>]) {
-    constexpr int V = kVec<T>;
-    if (i + V <= width) {
-        const typename Packed<T>::type x =
-            *reinterpret_cast<const typename Packed<T>::type*>(row + i);
+    const typename Packed<T>::type x = load_packed<T>(row, i, width, (T)fill);
 #pragma unroll
-        for (int k = 0; k < V; ++k) out[k] = (float)x[k];
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) out[k] = i + k < width ? (float)row[i + k] : fill;
-    }
+    for (int k = 0; k < kVec<T>; ++k) out[k] = (float)x[k];
 }
 
 // V values of weights, whose type is known at run time (the branch is uniform and taken once a row
@@ -87,19 +99,44 @@ __device__ __forceinline__ void store_row(T* row, int64_t i, int64_t width, cons
 }
 
 // Sum and maximum over the L lanes (a power of two up to 64, aligned) that hold one row; every lane
-// gets the result, the same bits in all of them.
-template <int L>
-__device__ __forceinline__ float lanes_sum(float x) {
-#pragma unroll
-    for (int d = 1; d < L; d *= 2) x += __shfl_xor(x, d);
+// gets the result, the same bits in all of them. The partner of a step differs in one bit of the lane up to
+// 2; then mirroring 8 and 16 lanes and exchanging halves of 32 and 64 bring together what
+// the steps before have made equal. One instruction a step, and none of local memory's latency.
+template <int CONTROL>
+__device__ __forceinline__ float from_lane(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+
+template <int L, typename OP>
+__device__ __forceinline__ float over_lanes(float x, OP op) {
+    if constexpr (L >= 2) x = op(x, from_lane<0xB1>(x));    // quads 1 0 3 2
+    if constexpr (L >= 4) x = op(x, from_lane<0x4E>(x));    // quads 2 3 0 1
+    if constexpr (L >= 8) x = op(x, from_lane<0x141>(x));   // halves of 16 mirrored
+    if constexpr (L >= 16) x = op(x, from_lane<0x140>(x));  // 16 mirrored
+    // v_permlaneN_swap exchanges the odd rows of N lanes of its first register with the even rows of its
+    // second: of two copies, each lane then holds the pair's values. (The builtins of this compiler
+    // return the first register for both; two wait states stand between the copies and the exchange.)
+    if constexpr (L >= 32) {
+        float y = x;
+        asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+        x = op(x, y);
+    }
+    if constexpr (L >= 64) {
+        float y = x;
+        asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+        x = op(x, y);
+    }
     return x;
 }
 
 template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+    return over_lanes<L>(x, [](float a, float b) { return a + b; });
+}
+
+template <int L>
 __device__ __forceinline__ float lanes_max(float x) {
-#pragma unroll
-    for (int d = 1; d < L; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+    return over_lanes<L>(x, [](float a, float b) { return fmaxf(a, b); });
 }
 
 inline bool is_float_type(int dtype) {
