@@ -103,15 +103,25 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
         Row<T, L, NV> next;
         const T* x = a.logits + r * a.rank_stride;
         int64_t t = t1 + group;
-        bool used = t < t2 && (!mask || mask[t]);
+        const auto counted = [&](int64_t t) { return t < t2 && (!mask || mask[t]); };
+        bool used = counted(t), after = counted(t + G);  // a token's mask is known before its row is fetched
         if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
         const int64_t first = (r * a.tokens + t1) * a.top_k;
         const int slots = (int)(t2 - t1) * a.top_k;
-        for (int i = threadIdx.x; i < slots; i += kThreads) {
-            if (mask && !mask[t1 + fdiv32(i, a.by_top_k)]) continue;
-            const int64_t e = a.wide_ids ? static_cast<const int64_t*>(a.ids)[first + i]
-                                         : static_cast<const int*>(a.ids)[first + i];
-            if (e >= 0 && e < a.experts) atomicAdd(&hist[e], 1);
+        constexpr int kIds = 4;  // of a lane on their way at once
+        for (int i0 = threadIdx.x; i0 < slots; i0 += kIds * kThreads) {
+            int64_t id[kIds];
+#pragma unroll
+            for (int q = 0; q < kIds; ++q) {
+                const int i = i0 + q * kThreads;
+                id[q] = -1;
+                if (i < slots && (!mask || mask[t1 + fdiv32(i, a.by_top_k)]))
+                    id[q] = a.wide_ids ? static_cast<const int64_t*>(a.ids)[first + i]
+                                       : static_cast<const int*>(a.ids)[first + i];
+            }
+#pragma unroll
+            for (int q = 0; q < kIds; ++q)
+                if (id[q] >= 0 && id[q] < a.experts) atomicAdd(&hist[id[q]], 1);
         }
         float sum[NV][V] = {};
         int live = 0;
@@ -120,8 +130,9 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
             float v[NV][V];
             next.values(v);
             t += G;
-            used = t < t2 && (!mask || mask[t]);
+            used = after;
             if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
+            after = counted(t + G);
             if (!use) continue;
             row_exp<T, L, NV>(v);
             float s = 0.0f;
@@ -173,9 +184,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void balance_join_kernel(
         double s = 0.0;  // exact for the counts
         if (col < experts) {
             const float* p = part_probs + r * chunks * experts + col;
+#pragma unroll 8
             for (int64_t c = wave; c < chunks; c += kJoinWaves) s += p[c * experts];
         } else if (col < 2 * experts + 1) {
             const int* p = part_counts + r * chunks * (experts + 1) + (col - experts);
+#pragma unroll 8
             for (int64_t c = wave; c < chunks; c += kJoinWaves) s += p[c * (experts + 1)];
         }
         sums[wave][lane] = s;
@@ -231,30 +244,32 @@ __global__ __launch_bounds__(kThreads) void balance_gradient_kernel(Gradient<T> 
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         const int* counts = a.counts + r * a.counts_rank;
         const uint8_t* mask = a.mask ? a.mask + r * a.tokens : nullptr;
-        const double f = count_weight(counts[a.experts], a.experts, a.top_k, a.scale) *
-                         (a.dloss ? (double)a.dloss[r] : 1.0);
+        const int64_t step = (int64_t)gridDim.x * G;
+        Row<T, L, NV> next;
+        const T* x = a.logits + r * a.rank_stride;
+        int64_t t = (int64_t)blockIdx.x * G + group;
+        const auto counted = [&](int64_t t) { return t < a.tokens && (!mask || mask[t]); };
+        bool used = counted(t), after = counted(t + step);  // a token's mask is known before its row is fetched
+        if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
+        const float f = (float)(count_weight(counts[a.experts], a.experts, a.top_k, a.scale) *
+                                (a.dloss ? (double)a.dloss[r] : 1.0));
         float w[NV][V];
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int e = (j * L + lane) * V + k;
-                w[j][k] = e < a.experts ? (float)(f * counts[e]) : 0.0f;
+                w[j][k] = e < a.experts ? f * (float)counts[e] : 0.0f;
             }
-        const int64_t step = (int64_t)gridDim.x * G;
-        Row<T, L, NV> next;
-        const T* x = a.logits + r * a.rank_stride;
-        int64_t t = (int64_t)blockIdx.x * G + group;
-        bool used = t < a.tokens && (!mask || mask[t]);
-        if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
         while (t < a.tokens) {
             const bool use = used;
             T* d = a.dlogits + r * a.d_rank + t * a.d_token;
             float v[NV][V];
             next.values(v);
             t += step;
-            used = t < a.tokens && (!mask || mask[t]);
+            used = after;
             if (used) next.fetch(x + t * a.token_stride, lane, a.experts);
+            after = counted(t + step);
             if (use) {
                 row_exp<T, L, NV>(v);
                 float s = 0.0f, q = 0.0f;
@@ -299,7 +314,7 @@ int row_lanes(int experts, int vec) {
 // so few that a chunk's slots are counted in 31 bits.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, int lanes) {
     const int64_t rows = kThreads / lanes;
-    const int64_t chunks = imax(1, imin((1024 + ranks - 1) / ranks, tokens / (4 * rows)));
+    const int64_t chunks = imax(1, imin((2048 + ranks - 1) / ranks, tokens / (4 * rows)));
     const int64_t per = (tokens + chunks - 1) / chunks;
     return imax(rows, (per + rows - 1) / rows * rows);
 }
@@ -345,7 +360,7 @@ template <typename T>
 int run_gradient(const Gradient<T>& a, hipStream_t stream) {
     const int rows = kThreads / row_lanes(a.experts, kVec<T>);
     // as many workgroups as the GPU holds, with the same number of rows each
-    const int64_t units = (a.tokens + rows - 1) / rows, most = imax(1, 256 * 8 / a.ranks);
+    const int64_t units = (a.tokens + rows - 1) / rows, most = imax(1, 256 * 64 / a.ranks);
     const int64_t each = (units + most - 1) / most;
     const dim3 grid((unsigned)((units + each - 1) / each), (unsigned)imin(a.ranks, kMaxGridY));
     with_shape<T>(a.experts, [&](auto l, auto nv) {

@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kThreads = 256;      // lanes of a workgroup whose rows take fewer
 constexpr int kWide = 1024;        // lanes of the widest rows' groups
-constexpr int64_t kBlocks = 8;     // of that many lanes, of the forward pass on one CU
+constexpr int64_t kBlocks = 32;    // of that many lanes, of the forward pass on one CU
 constexpr int64_t kMaxGridY = 65535;
 
 template <int LANES>
@@ -114,6 +114,7 @@ struct Forward {
     int64_t ranks, tokens, width, x_rank, x_token, y_rank, y_token;
     float eps;
     int weight_type;
+    bool stream;  // the tensors are larger than the caches
 };
 
 // The group of lanes of a row: known to be the same in a whole wave where a row takes one or more.
@@ -125,7 +126,7 @@ __device__ __forceinline__ int group_of_lane() {
     return g;
 }
 
-template <typename T, int V, int LANES, int NV>
+template <typename T, int V, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> a) {
     constexpr int G = kBlock<LANES> / LANES;
     __shared__ float slots[2][kWide / 64];
@@ -138,24 +139,25 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> 
         load_weights<V>(a.gamma, a.weight_type, own.first[j], a.width, 1.0f, gamma[j]);
         load_weights<V>(a.beta, a.weight_type, own.first[j], a.width, 0.0f, beta[j]);
     }
-    Some<T, V> next[NV];
-    const auto fetch = [&](int64_t r, int64_t t) {
+    const auto fetch = [&](int64_t r, int64_t t, Some<T, V>(&to)[NV]) {
         const T* x = a.x + r * a.x_rank + t * a.x_token;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (own.skip[j] < V) next[j] = *reinterpret_cast<const Some<T, V>*>(x + own.first[j]);
+            if (own.skip[j] < V)
+                to[j] = load_vector<STREAM>(reinterpret_cast<const Some<T, V>*>(x + own.first[j]));
     };
     const int64_t step = (int64_t)gridDim.x * G;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
+        Some<T, V> next[NV];
         int64_t t = (int64_t)blockIdx.x * G + group;
-        if (t < a.tokens) fetch(r, t);
+        if (t < a.tokens) fetch(r, t, next);
         for (; t < a.tokens; t += step) {  // whole groups of lanes, whole workgroups where a row takes one
             float v[NV][V];
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int k = 0; k < V; ++k) v[j][k] = (float)next[j][k];
-            if (t + step < a.tokens) fetch(r, t + step);  // on its way during this row's sums
+            if (t + step < a.tokens) fetch(r, t + step, next);  // on its way during this row's sums
             const float mean = row_sum<LANES>(own.sum([&](int j, int k) { return v[j][k]; }), slots[0]) * inv;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> 
                 Some<T, V> o;
 #pragma unroll
                 for (int k = 0; k < V; ++k) o[k] = (T)(v[j][k] * rstd * gamma[j][k] + beta[j][k]);
-                if (own.skip[j] < V) *reinterpret_cast<Some<T, V>*>(y + own.first[j]) = o;
+                if (own.skip[j] < V) store_vector<STREAM>(reinterpret_cast<Some<T, V>*>(y + own.first[j]), o);
             }
             if (lane == 0) {
                 if (a.mean) a.mean[r * a.tokens + t] = mean;
@@ -232,6 +234,7 @@ struct Backward {
     int64_t ranks, tokens, width, dy_rank, dy_token, x_rank, x_token, dx_rank, dx_token, grad_rank;
     int64_t chunks, per;    // chunks of a rank's tokens, and the tokens of one
     int weight_type;
+    bool stream;  // the tensors are larger than the caches
 };
 
 // Where a chunk's sums go, if anywhere: the rank's own gradients where it is the only one.
@@ -243,7 +246,7 @@ __device__ __forceinline__ float* sums_of(const Backward<T>& a, int64_t r, int64
     return d ? d + r * a.grad_rank : nullptr;
 }
 
-template <typename T, int V, int LANES, int NV>
+template <typename T, int V, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T> a) {
     constexpr int G = kBlock<LANES> / LANES;
     __shared__ float2 slots[2][kWide / 64];
@@ -260,39 +263,39 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T
         const int64_t t2 = t1 + a.per < a.tokens ? t1 + a.per : a.tokens;
         float dg[NV][V] = {}, db[NV][V] = {};
         int turn = 0;
-        Some<T, V> nx[NV], ndy[NV];
-        float nmean = 0.0f, nrstd = 0.0f;
-        const auto fetch = [&](int64_t t) {
+        struct Ahead {
+            Some<T, V> x[NV], dy[NV];
+            float mean, rstd;
+        };
+        const auto fetch = [&](int64_t t, Ahead& to) {
             const T* x = a.x + r * a.x_rank + t * a.x_token;
             const T* dy = a.dy + r * a.dy_rank + t * a.dy_token;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (own.skip[j] < V) {
-                    nx[j] = *reinterpret_cast<const Some<T, V>*>(x + own.first[j]);
-                    ndy[j] = *reinterpret_cast<const Some<T, V>*>(dy + own.first[j]);
+                    to.x[j] = load_vector<STREAM>(reinterpret_cast<const Some<T, V>*>(x + own.first[j]));
+                    to.dy[j] = load_vector<STREAM>(reinterpret_cast<const Some<T, V>*>(dy + own.first[j]));
                 }
-            nmean = a.mean[r * a.tokens + t];
-            nrstd = a.rstd[r * a.tokens + t];
+            to.mean = a.mean[r * a.tokens + t];
+            to.rstd = a.rstd[r * a.tokens + t];
         };
         // the next row is on its way during this row's sums, where there are registers for both
         constexpr bool kAhead = NV * V * sizeof(T) <= 64;
-        int64_t t = t1 + group;
-        if (kAhead && t < t2) fetch(t);
-        for (; t < t2; t += G) {
-            if (!kAhead) fetch(t);
-            const float mean = nmean, rstd = nrstd;
+        const auto row = [&](int64_t t, Ahead& next) {
+            if (!kAhead) fetch(t, next);
+            const float mean = next.mean, rstd = next.rstd;
             float h[NV][V], g[NV][V];
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
-                    h[j][k] = ((float)nx[j][k] - mean) * rstd;
-                    g[j][k] = (float)ndy[j][k];
+                    h[j][k] = ((float)next.x[j][k] - mean) * rstd;
+                    g[j][k] = (float)next.dy[j][k];
                     dg[j][k] += g[j][k] * h[j][k];
                     db[j][k] += g[j][k];
                     g[j][k] *= gamma[j][k];
                 }
-            if (kAhead && t + G < t2) fetch(t + G);
+            if (kAhead && t + G < t2) fetch(t + G, next);
             float s1 = own.sum([&](int j, int k) { return g[j][k]; });
             float s2 = own.sum([&](int j, int k) { return g[j][k] * h[j][k]; });
             row_sums<LANES>(s1, s2, slots[turn]);
@@ -305,9 +308,13 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T
                 Some<T, V> o;
 #pragma unroll
                 for (int k = 0; k < V; ++k) o[k] = (T)(rstd * (g[j][k] - s1 - h[j][k] * s2));
-                if (own.skip[j] < V) *reinterpret_cast<Some<T, V>*>(dx + own.first[j]) = o;
+                if (own.skip[j] < V) store_vector<STREAM>(reinterpret_cast<Some<T, V>*>(dx + own.first[j]), o);
             }
-        }
+        };
+        Ahead next;
+        int64_t t = t1 + group;
+        if (kAhead && t < t2) fetch(t, next);
+        for (; t < t2; t += G) row(t, next);
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             float* out = sums_of(a, r, c, which);
@@ -420,6 +427,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks_kernel(
         double s = 0.0;
         if (col < 2 * width) {
             const float* p = parts + r * chunks * 2 * width + col;
+#pragma unroll 8
             for (int64_t c = wave; c < chunks; c += kJoinWaves) s += p[c * 2 * width];
         }
         sums[wave][lane] = s;
@@ -489,7 +497,7 @@ int64_t imax(int64_t a, int64_t b) { return a > b ? a : b; }
 // least for each group of lanes.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
     const int64_t rows = group_rows(s);
-    const int64_t blocks = 1024 * kThreads / block_lanes(s);
+    const int64_t blocks = 512 * kThreads / block_lanes(s);
     const int64_t chunks = imax(1, imin((blocks + ranks - 1) / ranks, tokens / (4 * rows)));
     const int64_t per = (tokens + chunks - 1) / chunks;
     return imax(rows, (per + rows - 1) / rows * rows);
@@ -504,12 +512,12 @@ int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
         case Shape::k32: RUN(V, 32, 1); break;                                                \
         case Shape::k64: RUN(V, 64, 1); break;                                                \
         case Shape::k64x2: RUN(V, 64, 2); break;                                              \
-        case Shape::k64x4: if constexpr (V == 4) RUN(V, 64, 4); break;                        \
+        case Shape::k64x4: if constexpr (V == 4) { RUN(V, 64, 4); } break;                        \
         case Shape::k256x2: RUN(V, 256, 2); break;                                            \
-        case Shape::k256x4: if constexpr (V == 4) RUN(V, 256, 4); break;                      \
-        case Shape::k512x2: if constexpr (V == 8) RUN(V, 512, 2); break;                      \
+        case Shape::k256x4: if constexpr (V == 4) { RUN(V, 256, 4); } break;                      \
+        case Shape::k512x2: if constexpr (V == 8) { RUN(V, 512, 2); } break;                      \
         case Shape::k512x4: RUN(V, 512, 4); break;                                            \
-        case Shape::k512x8: if constexpr (V == 4) RUN(V, 512, 8); break;                      \
+        case Shape::k512x8: if constexpr (V == 4) { RUN(V, 512, 8); } break;                      \
         case Shape::kLong: RUN_LONG(); break;                                                 \
     }
 
@@ -526,7 +534,9 @@ int run_forward(Forward<T> a, hipStream_t stream) {
     const int64_t most = imax(1, 256 * kBlocks * kThreads / block_lanes(shape) / a.ranks);
     const int64_t each = (units + most - 1) / most;
     const dim3 grid((unsigned)((units + each - 1) / each), (unsigned)imin(a.ranks, kMaxGridY));
-#define RUN(V, L, N) norm_forward_kernel<T, V, L, N><<<grid, kBlock<L>, 0, stream>>>(a)
+#define RUN(V, L, N)                                                                      \
+    if (a.stream) norm_forward_kernel<T, V, L, N, true><<<grid, kBlock<L>, 0, stream>>>(a); \
+    else norm_forward_kernel<T, V, L, N, false><<<grid, kBlock<L>, 0, stream>>>(a)
 #define RUN_LONG() norm_forward_long_kernel<T><<<grid, kWide, 0, stream>>>(a)
     TRIVANCE_NORM_SHAPES(RUN, RUN_LONG)
 #undef RUN
@@ -538,7 +548,9 @@ template <typename T>
 int run_backward(const Backward<T>& a, hipStream_t stream) {
     const Shape shape = shape_of<T>(a.width);
     const dim3 grid((unsigned)a.chunks, (unsigned)imin(a.ranks, kMaxGridY));
-#define RUN(V, L, N) norm_backward_kernel<T, V, L, N><<<grid, kBlock<L>, 0, stream>>>(a)
+#define RUN(V, L, N)                                                                       \
+    if (a.stream) norm_backward_kernel<T, V, L, N, true><<<grid, kBlock<L>, 0, stream>>>(a); \
+    else norm_backward_kernel<T, V, L, N, false><<<grid, kBlock<L>, 0, stream>>>(a)
 #define RUN_LONG() norm_backward_long_kernel<T><<<grid, kWide, 0, stream>>>(a)
     TRIVANCE_NORM_SHAPES(RUN, RUN_LONG)
 #undef RUN
@@ -585,7 +597,8 @@ int trivance_layernorm_forward(const void* x, const void* gamma, const void* bet
         using T = decltype(type);
         return run_forward(Forward<T>{static_cast<const T*>(x), static_cast<T*>(y), gamma, beta, mean,
                                       rstd, ranks, tokens, width, x_rank_stride, x_token_stride,
-                                      y_rank_stride, y_token_stride, (float)eps, weight_dtype},
+                                      y_rank_stride, y_token_stride, (float)eps, weight_dtype,
+                                      ranks * tokens * width * (int64_t)sizeof(T) > kStreamBytes},
                            s);
     };
     return dtype == TRIVANCE_F32 ? run(float{}) : dtype == TRIVANCE_BF16 ? run(bf16{}) : run(f16{});
@@ -635,7 +648,7 @@ int trivance_layernorm_backward(const void* dy, const void* x, const void* gamma
                         mean, rstd, dgamma, dbeta, static_cast<float*>(workspace), ranks, tokens, width,
                         dy_rank_stride, dy_token_stride, x_rank_stride, x_token_stride, dx_rank_stride,
                         dx_token_stride, grad_rank_stride, imax(1, (tokens + per - 1) / per), per,
-                        weight_dtype},
+                        weight_dtype, ranks * tokens * width * (int64_t)sizeof(T) > kStreamBytes},
             s);
     };
     return dtype == TRIVANCE_F32 ? run(float{}) : dtype == TRIVANCE_BF16 ? run(bf16{}) : run(f16{});

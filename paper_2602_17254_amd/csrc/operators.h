@@ -51,6 +51,22 @@ __device__ __forceinline__ void load_row(const T* row, int64_t i, int64_t width,
     for (int k = 0; k < kVec<T>; ++k) out[k] = (float)x[k];
 }
 
+// A vector load or store that, where STREAM, does not stay in the caches: of tensors beyond kStreamBytes,
+// the L2 caches together, which would drop it before its next reader.
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load_vector(const V* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    return *p;
+}
+
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_vector(V* p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // V values of weights, whose type is known at run time (the branch is uniform and taken once a row
 // or less); `fill` everywhere where there are none.
 template <typename T, int V>
