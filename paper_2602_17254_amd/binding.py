@@ -412,45 +412,51 @@ def trivance_cost_model(plan: Plan, bytes_per_rank: float, alpha: float = 0.0,
 # rank and may be slices of a buffer that an AllReduce sums.
 
 
-def _rows(t, name, shape=None):
-    """(pointer, rank stride, token stride, type) of a [ranks, tokens, width] tensor."""
+def _rows(t, name):
+    """(pointer, rank stride, token stride, type, device) of a [ranks, tokens, width] tensor."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
     dt = _FLOATS.get(t.dtype)
     if dt is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16")
-    if t.dim() != 3 or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name} must be {'three-dimensional' if shape is None else tuple(shape)}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be three-dimensional")
     s0, s1, s2 = t.stride()
     if s2 != 1 and t.shape[2] > 1:
         raise ValueError(f"the values of a row of {name} must be consecutive")
-    return t.data_ptr(), s0, s1, dt
+    return t.data_ptr(), s0, s1, dt, t.get_device()
 
 
-def _same_type(t, name, x, x_name):
-    if t.dtype != x.dtype or t.device != x.device:
-        raise TypeError(f"{name} must have the type and device of {x_name}")
+def _rows_like(t, name, shape, dtype, device):
+    """(pointer, rank stride, token stride) of a tensor like another one."""
+    if not isinstance(t, _TORCH.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on GPU {device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and shape[2] > 1:
+        raise ValueError(f"the values of a row of {name} must be consecutive")
+    return t.data_ptr(), s0, s1
 
 
 def _array(t, name, shape, dtype, device):
     """Pointer of a contiguous tensor, None for None."""
     if t is None:
         return None
-    if not isinstance(t, _TORCH.Tensor) or t.dtype != dtype or t.device != device:
-        raise TypeError(f"{name} must be a {dtype} tensor on {device}")
+    if not isinstance(t, _TORCH.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on GPU {device}")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor")
     return t.data_ptr()
 
 
 def _rank_rows(t, name, ranks, width, dtype, device):
-    """(pointer, stride) of one row of `width` values per rank, (None, None) for None."""
+    """(pointer, stride) of one row of `width` values per rank, (None, 0) for None."""
     if t is None:
-        return None, None
-    if not isinstance(t, _TORCH.Tensor) or t.dtype != dtype or t.device != device:
-        raise TypeError(f"{name} must be a {dtype} tensor on {device}")
-    if t.dim() != 2 or t.shape[0] != ranks or t.shape[1] != width or \
-            (width > 1 and t.stride(1) != 1):
+        return None, 0
+    if not isinstance(t, _TORCH.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a {dtype} tensor on GPU {device}")
+    if t.shape != (ranks, width) or (width > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be [{ranks}, {width}] with consecutive values in a row")
     # the stride of a single row does not matter, and torch may give any
     return t.data_ptr(), t.stride(0) if ranks > 1 else width
@@ -461,25 +467,26 @@ def _weights(gamma, beta, width, device):
     w = gamma if gamma is not None else beta
     if w is None:
         return None, None, F32
-    dt = _FLOATS.get(w.dtype)
+    dtype = getattr(w, "dtype", None)
+    dt = _FLOATS.get(dtype)
     if dt is None:
-        raise TypeError("weights must be float32, bfloat16 or float16")
-    return (_array(gamma, "gamma", (width,), w.dtype, device),
-            _array(beta, "beta", (width,), w.dtype, device), dt)
+        raise TypeError("weights must be float32, bfloat16 or float16 tensors")
+    shape = (width,)
+    return (_array(gamma, "gamma", shape, dtype, device), _array(beta, "beta", shape, dtype, device), dt)
 
 
 def trivance_layernorm_forward(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5,
                                stream=None) -> None:
     """y = layer norm of the rows of x [ranks, tokens, width], times gamma plus beta (either may be
     None); mean and rstd [ranks, tokens] receive the statistics for the backward pass."""
-    xp, xr, xt, dt = _rows(x, "x")
-    yp, yr, yt, _ = _rows(y, "y", x.shape)
-    _same_type(y, "y", x, "x")
-    ranks, tokens, width = x.shape
+    xp, xr, xt, dt, dev = _rows(x, "x")
+    shape = x.shape
+    yp, yr, yt = _rows_like(y, "y", shape, x.dtype, dev)
+    ranks, tokens, width = shape
     f32 = _TORCH.float32
-    gp, bp, wt = _weights(gamma, beta, width, x.device)
-    mp = _array(mean, "mean", (ranks, tokens), f32, x.device)
-    sp = _array(rstd, "rstd", (ranks, tokens), f32, x.device)
+    gp, bp, wt = _weights(gamma, beta, width, dev)
+    mp = _array(mean, "mean", (ranks, tokens), f32, dev)
+    sp = _array(rstd, "rstd", (ranks, tokens), f32, dev)
     _check(_lib().trivance_layernorm_forward(xp, gp, bp, yp, mp, sp, ranks, tokens, width, xr, xt, yr,
                                              yt, eps, dt, wt, _stream_ptr(stream)),
            "trivance_layernorm_forward")
@@ -494,24 +501,23 @@ def trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, wor
                                 stream=None) -> None:
     """dx, and each rank's dgamma and dbeta [ranks, width] (fp32 rows, equally far apart; either may be
     None), from dy and what the forward pass read and wrote."""
-    xp, xr, xt, dt = _rows(x, "x")
-    dyp, dyr, dyt, _ = _rows(dy, "dy", x.shape)
-    dxp, dxr, dxt, _ = _rows(dx, "dx", x.shape)
-    _same_type(dy, "dy", x, "x")
-    _same_type(dx, "dx", x, "x")
-    ranks, tokens, width = x.shape
+    xp, xr, xt, dt, dev = _rows(x, "x")
+    shape, dtype = x.shape, x.dtype
+    dyp, dyr, dyt = _rows_like(dy, "dy", shape, dtype, dev)
+    dxp, dxr, dxt = _rows_like(dx, "dx", shape, dtype, dev)
+    ranks, tokens, width = shape
     f32 = _TORCH.float32
-    gp, _, wt = _weights(gamma, None, width, x.device)
-    mp = _array(mean, "mean", (ranks, tokens), f32, x.device)
-    sp = _array(rstd, "rstd", (ranks, tokens), f32, x.device)
-    dgp, dgs = _rank_rows(dgamma, "dgamma", ranks, width, f32, x.device)
-    dbp, dbs = _rank_rows(dbeta, "dbeta", ranks, width, f32, x.device)
-    if dgs is not None and dbs is not None and dgs != dbs:
+    gp, _, wt = _weights(gamma, None, width, dev)
+    mp = _array(mean, "mean", (ranks, tokens), f32, dev)
+    sp = _array(rstd, "rstd", (ranks, tokens), f32, dev)
+    dgp, dgs = _rank_rows(dgamma, "dgamma", ranks, width, f32, dev)
+    dbp, dbs = _rank_rows(dbeta, "dbeta", ranks, width, f32, dev)
+    if dgs and dbs and dgs != dbs:
         raise ValueError("the rows of dgamma and dbeta must be equally far apart")
     wp, wb = _workspace_args(workspace)
     _check(_lib().trivance_layernorm_backward(dyp, xp, gp, mp, sp, dxp, dgp, dbp, ranks, tokens, width,
                                               dyr, dyt, xr, xt, dxr, dxt,
-                                              dgs if dgs is not None else dbs or 0, dt, wt, wp, wb,
+                                              dgs or dbs, dt, wt, wp, wb,
                                               _stream_ptr(stream)),
            "trivance_layernorm_backward")
 
@@ -522,9 +528,11 @@ def trivance_balance_workspace_bytes(ranks: int, tokens: int, experts: int) -> i
 
 
 def _mask(mask, shape, device):
-    if mask is not None and mask.dtype == _TORCH.uint8:
-        return _array(mask, "mask", shape, _TORCH.uint8, device)
-    return _array(mask, "mask", shape, _TORCH.bool, device)
+    """Pointer of a mask of bools or bytes, None for None."""
+    if mask is None:
+        return None
+    dtype = _TORCH.uint8 if getattr(mask, "dtype", None) is _TORCH.uint8 else _TORCH.bool
+    return _array(mask, "mask", shape, dtype, device)
 
 
 def trivance_balance_counts(logits, chosen, counts, probs, workspace=None, mask=None,
@@ -533,7 +541,7 @@ def trivance_balance_counts(logits, chosen, counts, probs, workspace=None, mask=
     probabilities, probs [ranks, experts] (float32), from the router's logits [ranks, tokens,
     experts], the experts chosen [ranks, tokens, top_k] (int32 or int64; negative: an empty slot)
     and an optional mask [ranks, tokens] of the tokens that count (bool or uint8)."""
-    lp, lr, lt, dt = _rows(logits, "logits")
+    lp, lr, lt, dt, dev = _rows(logits, "logits")
     ranks, tokens, experts = logits.shape
     it = _IDS.get(getattr(chosen, "dtype", None))
     if it is None:
@@ -541,13 +549,13 @@ def trivance_balance_counts(logits, chosen, counts, probs, workspace=None, mask=
     if chosen.dim() != 3:
         raise ValueError("chosen must be [ranks, tokens, top_k]")
     k = chosen.shape[2]
-    ip = _array(chosen, "chosen", (ranks, tokens, k), chosen.dtype, logits.device)
-    mp = _mask(mask, (ranks, tokens), logits.device)
-    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, logits.device)
-    pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, logits.device)
+    ip = _array(chosen, "chosen", (ranks, tokens, k), chosen.dtype, dev)
+    mp = _mask(mask, (ranks, tokens), dev)
+    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, dev)
+    pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, dev)
     wp, wb = _workspace_args(workspace)
     _check(_lib().trivance_balance_counts(lp, ip, mp, cp, pp, ranks, tokens, experts, k, lr, lt,
-                                          cs or 0, ps or 0, dt, it, wp, wb, _stream_ptr(stream)),
+                                          cs, ps, dt, it, wp, wb, _stream_ptr(stream)),
            "trivance_balance_counts")
 
 
@@ -556,25 +564,25 @@ def trivance_balance_loss(counts, probs, top_k: int, loss, scale=1.0, stream=Non
     if not isinstance(probs, _torch().Tensor) or not probs.is_cuda or probs.dim() != 2:
         raise TypeError("probs must be a two-dimensional CUDA (HIP) torch tensor")
     ranks, experts = probs.shape
-    pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, probs.device)
-    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, probs.device)
-    op = _array(loss, "loss", (ranks,), _TORCH.float32, probs.device)
-    _check(_lib().trivance_balance_loss(cp, pp, op, ranks, experts, top_k, cs or 0, ps, scale,
+    dev = probs.get_device()
+    pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, dev)
+    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, dev)
+    op = _array(loss, "loss", (ranks,), _TORCH.float32, dev)
+    _check(_lib().trivance_balance_loss(cp, pp, op, ranks, experts, top_k, cs, ps, scale,
                                         _stream_ptr(stream)), "trivance_balance_loss")
 
 
 def trivance_balance_backward(logits, counts, top_k: int, dlogits, mask=None, scale=1.0, dloss=None,
                               stream=None) -> None:
     """dlogits: the gradient of the balance loss of `counts`, times dloss [ranks] (None: ones)."""
-    lp, lr, lt, dt = _rows(logits, "logits")
-    dp, dr, dts, _ = _rows(dlogits, "dlogits", logits.shape)
-    _same_type(dlogits, "dlogits", logits, "logits")
+    lp, lr, lt, dt, dev = _rows(logits, "logits")
+    dp, dr, dts = _rows_like(dlogits, "dlogits", logits.shape, logits.dtype, dev)
     ranks, tokens, experts = logits.shape
-    mp = _mask(mask, (ranks, tokens), logits.device)
-    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, logits.device)
-    gp = _array(dloss, "dloss", (ranks,), _TORCH.float32, logits.device)
+    mp = _mask(mask, (ranks, tokens), dev)
+    cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, dev)
+    gp = _array(dloss, "dloss", (ranks,), _TORCH.float32, dev)
     _check(_lib().trivance_balance_backward(lp, cp, mp, gp, dp, ranks, tokens, experts, top_k, lr, lt,
-                                            dr, dts, cs or 0, scale, dt, _stream_ptr(stream)),
+                                            dr, dts, cs, scale, dt, _stream_ptr(stream)),
            "trivance_balance_backward")
 
 
@@ -609,9 +617,8 @@ def trivance_orthogonalize(x, out, workspace, coefficients=QUINTIC_5, scale=1.0,
                            stream=None) -> None:
     """out = scale times x [batch, rows, cols] with the singular values of each matrix pushed towards
     one: X = x / (norm + eps), then X <- a X + (b A + c A A) X, A = X X', for each (a, b, c)."""
-    xp, xb, xr, dt = _rows(x, "x")
-    op, ob, orow, _ = _rows(out, "out", x.shape)
-    _same_type(out, "out", x, "x")
+    xp, xb, xr, dt, dev = _rows(x, "x")
+    op, ob, orow = _rows_like(out, "out", x.shape, x.dtype, dev)
     batch, rows, cols = x.shape
     k, steps = _coefficients(coefficients)
     wp, wb = _workspace_args(workspace)

@@ -92,9 +92,13 @@ struct Columns {
 #pragma unroll
                 for (int k = 0; k < V; ++k) part += f(j, k);
             } else {
+                // few lanes come here: without the barrier to the compiler, it works out the V
+                // comparisons before a kernel's loop and has no registers left for them
+                int from = skip[j];
+                asm volatile("" : "+v"(from));
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    if (k >= skip[j]) part += f(j, k);
+                    if (k >= from) part += f(j, k);
             }
             s += part;
         }
@@ -246,18 +250,31 @@ __device__ __forceinline__ float* sums_of(const Backward<T>& a, int64_t r, int64
     return d ? d + r * a.grad_rank : nullptr;
 }
 
+// Whether gamma stays in local memory, so that the registers suffice for two workgroups on a CU: one goes on
+// while the other waits for its row's sums.
+template <int V, int LANES, int NV>
+constexpr bool kLocalGamma = LANES == 512 && V == 8 && NV == 2;
+
 template <typename T, int V, int LANES, int NV, bool STREAM>
-__global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T> a) {
+__global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1)) void norm_backward_kernel(Backward<T> a) {
     constexpr int G = kBlock<LANES> / LANES;
     __shared__ float2 slots[2][kWide / 64];
     __shared__ float join[G > 1 ? kThreads * NV * V : 1];
     const int lane = threadIdx.x % LANES, group = group_of_lane<LANES>();
     const Columns<V, LANES, NV> own(lane, (int)a.width);
     const float inv = 1.0f / (float)a.width;
+    constexpr bool kLocal = kLocalGamma<V, LANES, NV>;
+    __shared__ float gammas[kLocal ? LANES * NV * V : 1];
     float gamma[NV][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
         load_weights<V>(a.gamma, a.weight_type, own.first[j], a.width, 1.0f, gamma[j]);
+    if constexpr (kLocal) {  // each lane reads only what it wrote
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int k = 0; k < V; ++k) gammas[(j * LANES + lane) * V + k] = gamma[j][k];
+    }
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         const int64_t c = blockIdx.x, t1 = c * a.per;
         const int64_t t2 = t1 + a.per < a.tokens ? t1 + a.per : a.tokens;
@@ -283,7 +300,11 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T
         constexpr bool kAhead = NV * V * sizeof(T) <= 64;
         const auto row = [&](int64_t t, Ahead& next) {
             if (!kAhead) fetch(t, next);
-            const float mean = next.mean, rstd = next.rstd;
+            float mean = next.mean, rstd = next.rstd;
+            if constexpr (LANES >= 64) {  // the same in a wave: in scalar registers
+                mean = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, mean)));
+                rstd = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, rstd)));
+            }
             float h[NV][V], g[NV][V];
 #pragma unroll
             for (int j = 0; j < NV; ++j)
@@ -293,7 +314,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_backward_kernel(Backward<T
                     g[j][k] = (float)next.dy[j][k];
                     dg[j][k] += g[j][k] * h[j][k];
                     db[j][k] += g[j][k];
-                    g[j][k] *= gamma[j][k];
+                    g[j][k] *= kLocal ? gammas[(j * LANES + lane) * V + k] : gamma[j][k];
                 }
             if (kAhead && t + G < t2) fetch(t + G, next);
             float s1 = own.sum([&](int j, int k) { return g[j][k]; });
@@ -493,12 +514,15 @@ int block_lanes(Shape s) {
 int64_t imin(int64_t a, int64_t b) { return a < b ? a : b; }
 int64_t imax(int64_t a, int64_t b) { return a > b ? a : b; }
 
-// The tokens that a chunk of the backward pass takes. Enough chunks to fill the GPU, but four rows at
-// least for each group of lanes.
+// The tokens that a chunk of the backward pass takes. Two workgroups a CU (512; one where a row takes 512
+// lanes), of four rows at least for each group of lanes, so that few tokens still spread over the GPU;
+// four a CU where each then has 16 rows or more, as each chunk's sums take a way through memory. A few
+// workgroups above a multiple of the CUs cost a round: 9 x 1001 x 2051 fp16 measured 37 us with 504
+// workgroups, 42 with 531, 58 with 252.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
-    const int64_t rows = group_rows(s);
-    const int64_t blocks = 512 * kThreads / block_lanes(s);
-    const int64_t chunks = imax(1, imin((blocks + ranks - 1) / ranks, tokens / (4 * rows)));
+    const int64_t rows = group_rows(s), wide = block_lanes(s) / kThreads;
+    const int64_t many = imax(1, 1024 / ranks), few = imax(1, 512 / wide / ranks);
+    const int64_t chunks = imax(1, many * 16 * rows <= tokens ? many : imin(few, tokens / (4 * rows)));
     const int64_t per = (tokens + chunks - 1) / chunks;
     return imax(rows, (per + rows - 1) / rows * rows);
 }

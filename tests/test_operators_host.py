@@ -53,7 +53,7 @@ def gradient(**kw):
 
 def orthogonalize(k=((3.4445, -4.7750, 2.0315),) * 5, **kw):
     flat = [v for abc in k for v in abc]
-    a = dict(x=P, out=P, batch=2, rows=4, cols=8, xb=32, xr=8, ob=32, orow=8,
+    a = dict(x=P, out=P, batch=2, rows=70, cols=80, xb=5600, xr=80, ob=5600, orow=80,
              k=(ctypes.c_float * max(1, len(flat)))(*flat), steps=len(k), scale=1.0, eps=1e-7,
              dtype=T.F32, ws=P, wsb=1 << 40, stream=None)
     a.update(kw)
@@ -109,8 +109,8 @@ def test_balance_backward_refuses(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=T.I32), EINVAL), (dict(batch=-1), EINVAL), (dict(rows=-1), EINVAL), (dict(k=()), EINVAL),
     (dict(x=None), EINVAL), (dict(out=None), EINVAL), (dict(eps=-1.0), EINVAL), (dict(scale=math.inf), EINVAL),
-    (dict(orow=7), EINVAL), (dict(ob=31), EINVAL), (dict(xr=-8), EINVAL), (dict(wsb=64), ESIZE),
-    (dict(ws=None), ESIZE), (dict(rows=1 << 17, xb=1 << 20, ob=1 << 20), EUNSUPPORTED),
+    (dict(orow=79), EINVAL), (dict(ob=5599), EINVAL), (dict(xr=-80), EINVAL), (dict(wsb=64), ESIZE),
+    (dict(ws=None), ESIZE), (dict(rows=1 << 17, xb=1 << 24, ob=1 << 24), EUNSUPPORTED),
     (dict(batch=1 << 16), EUNSUPPORTED), (dict(k=((1.0, 0.0, 0.0),) * 65), EUNSUPPORTED),
     (dict(k=((16.0, 0.0, 0.0),)), EUNSUPPORTED), (dict(k=((2.0, 0.0, 0.0),) * 3), EUNSUPPORTED),
     (dict(k=((math.nan, 0.0, 0.0),)), EUNSUPPORTED)], ids=str)
