@@ -139,14 +139,19 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
     }
 }
 
-enum class Product { kGram, kPolynomial, kUpdate, kLast };
+// Symmetric: A = X X', the polynomial in A, products of such matrices. The others: X times one of them, and the
+// last of these, which goes to the caller.
+enum class Product { kGram, kPolynomial, kSquare, kUpdate, kLast };
+
+constexpr bool is_symmetric(Product p) {
+    return p == Product::kGram || p == Product::kPolynomial || p == Product::kSquare;
+}
 
 template <typename T>
 struct Output {
     T* x;
     int64_t batch, si, sj;
     int m, n;
-    float scale;
 };
 
 // How a square tile of a product is computed: the rows and columns of waves that share it, the values
@@ -194,6 +199,7 @@ struct Operands {
     int depth;       // the summed index, a multiple of 64
     int rows, cols;  // tiles of C
     Planes c, ct;    // C and its transpose
+    float factor;    // of the sums, which carry the scales of both operands
     Planes a;        // of the polynomial
     Coefficients k;
     const Coefficients* first;  // in place of k, for each matrix
@@ -287,46 +293,91 @@ __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, i
     }
 }
 
-// Four consecutive values of row i of C from column j on: what the product is for, and its places.
-// `mirrored`: in C's transpose too.
-template <Product KIND, typename T>
+// Tells the compiler that local memory was written for other lanes of the wave, whose accesses the
+// hardware keeps in order.
+__device__ __forceinline__ void wave_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Local memory of a wave in which 16 columns of its part of C turn round: 16 rows of both planes.
+template <int MI>
+constexpr int kTurnRow = MI * 16 + 8;  // values; the 8 shift the rows' banks
+template <int MI>
+constexpr int kTurn = 2 * 16 * kTurnRow<MI>;
+
+// MI tiles of 16 x 16 one below the other, from row i (the lane's own) and column j (its first of four) on: what
+// the product is for, and its places. `mirrored`: in C's transpose too, through the wave's `turn`.
+template <Product KIND, int MI, typename T>
 __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, int64_t b, Coefficients k,
-                                       int i, int j, bool mirrored, float4v sum) {
-    float v[4];
+                                       int i, int j, bool mirrored, const float4v (&sum)[MI], f16* turn) {
+    const int lane = threadIdx.x % 64;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = sum[q] * (1.0f / kScale);
-    if constexpr (KIND == Product::kPolynomial) {
-        const int64_t at = b * o.a.batch + (int64_t)i * o.a.ld + j;
-        const half4 h = *reinterpret_cast<const half4*>(o.a.hi + at);
-        const half4 w = *reinterpret_cast<const half4*>(o.a.lo + at);
+    for (int x = 0; x < MI; ++x) {
+        const int row = i + x * 16;
+        float v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            v[q] = k.b * ((float)h[q] + (float)w[q]) + k.c * v[q] + (i == j + q ? k.a * kScale : 0.0f);
-    }
-    if constexpr (KIND == Product::kLast) {
+        for (int q = 0; q < 4; ++q) v[q] = sum[x][q] * o.factor;
+        if constexpr (KIND == Product::kPolynomial) {
+            const int64_t at = b * o.a.batch + (int64_t)row * o.a.ld + j;
+            const half4 h = *reinterpret_cast<const half4*>(o.a.hi + at);
+            const half4 w = *reinterpret_cast<const half4*>(o.a.lo + at);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (i < out.m && j + q < out.n)
-                out.x[b * out.batch + i * out.si + (j + q) * out.sj] = (T)(v[q] * (out.scale / kScale));
-    } else {
-        half4 h, w;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            f16 hi, lo;
-            split(v[q], hi, lo);
-            h[q] = hi;
-            w[q] = lo;
+            for (int q = 0; q < 4; ++q)
+                v[q] = k.b * ((float)h[q] + (float)w[q]) + k.c * v[q] + (row == j + q ? k.a * kScale : 0.0f);
         }
-        const int64_t at = b * o.c.batch + (int64_t)i * o.c.ld + j;
-        *reinterpret_cast<half4*>(o.c.hi + at) = h;
-        *reinterpret_cast<half4*>(o.c.lo + at) = w;
-        if (mirrored) {
+        if constexpr (KIND == Product::kLast) {
+            T* to = out.x + b * out.batch + row * out.si + j * out.sj;
+            if (out.sj == 1 && row < out.m && j + 4 <= out.n) {
+                typedef T U __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+                U u;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) u[q] = (T)v[q];
+                *reinterpret_cast<U*>(to) = u;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (row < out.m && j + q < out.n) to[q * out.sj] = (T)v[q];
+            }
+        } else {
+            half4 h, w;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t att = b * o.ct.batch + (int64_t)(j + q) * o.ct.ld + i;
-                o.ct.hi[att] = h[q];
-                o.ct.lo[att] = w[q];
+                f16 hi, lo;
+                split(v[q], hi, lo);
+                h[q] = hi;
+                w[q] = lo;
             }
+            const int64_t at = b * o.c.batch + (int64_t)row * o.c.ld + j;
+            *reinterpret_cast<half4*>(o.c.hi + at) = h;
+            *reinterpret_cast<half4*>(o.c.lo + at) = w;
+            if (mirrored) {
+                f16* to = turn + (lane / 16 * 4) * kTurnRow<MI> + x * 16 + lane % 16;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    to[q * kTurnRow<MI>] = h[q];
+                    to[(16 + q) * kTurnRow<MI>] = w[q];
+                }
+            }
+        }
+    }
+    if constexpr (KIND != Product::kLast) {
+        if (mirrored) {
+            wave_order();
+            const int i0 = i - lane % 16, j0 = j - lane / 16 * 4;
+            constexpr int kRowPieces = MI * 2;
+#pragma unroll
+            for (int q = 0; q < kRowPieces * 16; q += 64) {
+                const int row = (q + lane) / kRowPieces, p = (q + lane) % kRowPieces * 8;
+                const int64_t att = b * o.ct.batch + (int64_t)(j0 + row) * o.ct.ld + i0 + p;
+                if (q + lane < kRowPieces * 16) {
+                    *reinterpret_cast<half8*>(o.ct.hi + att) =
+                        *reinterpret_cast<const half8*>(turn + row * kTurnRow<MI> + p);
+                    *reinterpret_cast<half8*>(o.ct.lo + att) =
+                        *reinterpret_cast<const half8*>(turn + (16 + row) * kTurnRow<MI> + p);
+                }
+            }
+            wave_order();
         }
     }
 }
@@ -343,7 +394,7 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
 template <Product KIND, int TILE, int LP, int RP, typename T>
 __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
-    constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
+    constexpr bool kSymmetric = is_symmetric(KIND);
     constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16;
     extern __shared__ half8 stages[];
     // one XCD's workgroups take neighbouring tiles: all rows of some columns
@@ -360,11 +411,18 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void product_kernel(Operands o
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int i = ti * TILE + wave / S::kCols * (MI * 16) + lane % 16;
     const int j = tj * TILE + wave % S::kCols * (NI * 16) + lane / 16 * 4;
+    static_assert(KIND == Product::kLast ||
+                      S::kRows * S::kCols * kTurn<MI> <= S::kStages * (LP + RP) * TILE * S::kDepth,
+                  "the waves' turns fit into the stages");
+    if constexpr (KIND != Product::kLast) __syncthreads();  // every wave has read the last stage
+    f16* turn = reinterpret_cast<f16*>(stages) + wave * kTurn<MI>;
 #pragma unroll
-    for (int x = 0; x < MI; ++x)
+    for (int y = 0; y < NI; ++y) {
+        float4v column[MI];
 #pragma unroll
-        for (int y = 0; y < NI; ++y)
-            finish<KIND, T>(o, out, b, k, i + x * 16, j + y * 16, !kSymmetric || ti != tj, acc[x][y]);
+        for (int x = 0; x < MI; ++x) column[x] = acc[x][y];
+        finish<KIND, MI, T>(o, out, b, k, i, j + y * 16, !kSymmetric || ti != tj, column, turn);
+    }
 }
 
 // A symmetric product whose tiles fill the GPU badly: kWorkers workgroups share all stages of all
@@ -400,23 +458,21 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Ope
         for (int x = 0; x < MI; ++x)
 #pragma unroll
             for (int y = 0; y < NI; ++y)
-                *reinterpret_cast<float4v*>(part + (x * NI + y) * (kThreads * 4)) = acc[x][y];
+                *reinterpret_cast<float4v*>(part + (y * MI + x) * (kThreads * 4)) = acc[x][y];
         at = stop;
         __syncthreads();  // every wave has read the last stage
     }
 }
 
-// The parts of a tile, added in the workers' order; a workgroup takes kJoin of its 16 x 16 pieces a wave.
-constexpr int kJoin = 2;
-
+// The parts of a tile, added in the workers' order: a workgroup takes 16 columns of each wave's part of C.
 template <Product KIND, int TILE>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands o, Shares s) {
     using S = Shape<TILE>;
     constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
-    constexpr int kGroups = MI * NI / kJoin;
+    __shared__ half8 turns[kThreads / 64 * kTurn<MI> / 8];
     const int tiles = o.rows * (o.rows + 1) / 2;
-    const int64_t t = blockIdx.x / kGroups;
-    const int piece = blockIdx.x % kGroups * kJoin;
+    const int64_t t = blockIdx.x / NI;
+    const int y = blockIdx.x % NI;
     const int64_t b = t / tiles;
     int ti, tj;
     triangle((int)(t % tiles), ti, tj);
@@ -425,23 +481,20 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
     int64_t w0 = first * kWorkers / s.stages, w1 = last * kWorkers / s.stages;
     while (s.begin(w0 + 1) <= first) ++w0;
     while (s.begin(w1 + 1) <= last) ++w1;
-    float4v sum[kJoin] = {};
+    float4v sum[MI] = {};
     for (int64_t w = w0; w <= w1; ++w) {
         if (s.begin(w) == s.begin(w + 1)) continue;  // a worker without a stage
         const float* part = s.parts + (t + w) * (TILE * TILE) + threadIdx.x * 4;
 #pragma unroll
-        for (int q = 0; q < kJoin; ++q)
-            sum[q] += *reinterpret_cast<const float4v*>(part + (piece + q) * (kThreads * 4));
+        for (int x = 0; x < MI; ++x)
+            sum[x] += *reinterpret_cast<const float4v*>(part + (y * MI + x) * (kThreads * 4));
     }
     Coefficients k = o.k;
     if (KIND == Product::kPolynomial && o.first) k = o.first[b];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int i = ti * TILE + wave / S::kCols * (MI * 16) + lane % 16;
-    const int j = tj * TILE + wave % S::kCols * (NI * 16) + lane / 16 * 4;
-#pragma unroll
-    for (int q = 0; q < kJoin; ++q)
-        finish<KIND>(o, Output<f16>{}, b, k, i + (piece + q) / NI * 16, j + (piece + q) % NI * 16, ti != tj,
-                     sum[q]);
+    finish<KIND, MI>(o, Output<f16>{}, b, k, ti * TILE + wave / S::kCols * (MI * 16) + lane % 16,
+                     tj * TILE + wave % S::kCols * (NI * 16) + y * 16 + lane / 16 * 4, ti != tj, sum,
+                     reinterpret_cast<f16*>(turns) + wave * kTurn<MI>);
 }
 
 // Whole matrices of up to 64 x 256 in one workgroup each, with everything in local memory: X both ways
@@ -530,7 +583,7 @@ constexpr int kSmallA = kSmallSide * kSmallSide / 8;
 // n: X's columns padded to whole panels.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Output<T> out, int n, SmallSteps s,
-                                                              float eps) {
+                                                              float scale, float eps) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     constexpr int kWaves = kSmallThreads / 64, kTiles = kSmallSide / 16;
@@ -623,7 +676,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
                 for (int c = 0; c < 4; ++c)
                     if (i < out.m && j + c < out.n)
                         out.x[blockIdx.x * out.batch + i * out.si + (j + c) * out.sj] =
-                            (T)(w[c] * (out.scale / kScale));
+                            (T)(w[c] * (scale / kScale));
             }
         }
         __syncthreads();
@@ -648,26 +701,31 @@ bool shared(int tile, int64_t tiles, int64_t depth) {
     return idle * depth >= 512.0;
 }
 
+// How many products of each sort a call takes.
+struct Counts {
+    int grams, squares, updates;
+};
+
 // The pair that takes the least time by the measured rates, counting whole rounds of the 256 CUs and the
 // padding.
-Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
+Tiles tiles_of(int64_t batch, int64_t m, int64_t n, Counts count) {
     const auto cost = [&](int tile, int64_t tiles, int64_t depth, bool symmetric) {
         const double rate = tile == 256 ? 1.0 : tile == 128 ? 0.76 : 0.5;
-        const double rounds = symmetric && shared(tile, batch * tiles, depth)
-                                  ? batch * tiles / 256.0
-                                  : (double)((batch * tiles + 255) / 256);
+        const bool share = symmetric && shared(tile, batch * tiles, depth);
+        const double rounds = share ? batch * tiles / 256.0 : (double)((batch * tiles + 255) / 256);
         // in units of 1/720000 us; the second launch of shared products takes 10 us
-        return rounds * tile * tile * depth / rate + (symmetric && shared(tile, batch * tiles, depth) ? 7.2e6 : 0.0);
+        return rounds * tile * tile * depth / rate + (share ? 7.2e6 : 0.0);
     };
     Tiles best{64, 64};
     double least = INFINITY;
     for (const int s : {64, 128})
         for (const int u : {64, 128, 256}) {
+            if (u == 256 && m <= 128) continue;  // the workspace has no such padding
             const Tiles t{s, u};
             const int64_t pm = padded(m, t.pad()), pn = padded(n, t.pad());
-            const int64_t ms = pm / s;
-            const double c = cost(s, ms * (ms + 1) / 2, pn, true) + cost(s, ms * (ms + 1) / 2, pm, true) +
-                             cost(u, pm / u * (pn / u), pm, false);
+            const int64_t ms = pm / s, half = ms * (ms + 1) / 2;
+            const double c = count.grams * cost(s, half, pn, true) + count.squares * cost(s, half, pm, true) +
+                             count.updates * cost(u, pm / u * (pn / u), pm, false);
             if (c < least) {
                 least = c;
                 best = t;
@@ -676,11 +734,49 @@ Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
     return best;
 }
 
-// The workspace: norm parts and first coefficients, then the planes of X and X' twice, A and P.
+// Steps of which X is formed only once. Within a group A itself is carried on, A <- A P P, and the polynomials
+// multiply up, Q <- P Q: products of the smaller side instead of the larger. They keep what A
+// holds of a weak direction, its singular value squared, which is lost in the rounding of A sooner than
+// the value itself in that of X: the error of a weak direction grows by |b / a| times the squares of
+// the growth so far. Up to 256 it stays at that of fp32 steps for every spectrum measured, two or three steps
+// of the usual coefficients, but several times it for some; so fp32 matrices take single steps, and
+// 16-bit ones, whose own rounding is far larger, groups. These pay where the larger side is twice the
+// smaller or more and products are not too small to fill the GPU.
+constexpr int kMaxGroup = 3;
+
+int group_of(const float* k, int step, int steps, int dtype, int64_t m, int64_t n) {
+    if (dtype == TRIVANCE_F32 || n < 2 * m || m < 512) return 1;
+    double growth = 1.0, lost = 0.0;
+    int g = 0;
+    for (; g < kMaxGroup && step + g < steps; ++g) {
+        const double a = k[3 * (step + g)], b = k[3 * (step + g) + 1];
+        lost += std::fabs(b / a) * growth;
+        if (g > 0 && !(lost <= 256.0)) break;
+        growth *= a * a;
+    }
+    return g;
+}
+
+Counts counts_of(const float* k, int steps, int dtype, int64_t m, int64_t n) {
+    Counts c{0, 0, 0};
+    for (int s = 0; s < steps;) {
+        const int g = group_of(k, s, steps, dtype, m, n);
+        ++c.grams;
+        c.squares += 4 * g - 3;
+        ++c.updates;
+        s += g;
+    }
+    return c;
+}
+
+// The workspace: norm parts and first coefficients, then the planes of X and X' twice, of A and Q (twice
+// each), P and P P, and the parts of shared products. It has to serve every call of these sizes, so it is laid out
+// for the largest padding and for groups.
+constexpr int kSquares = 6, kMostPad = 256;
+
 struct Layout {
-    int64_t parts, first, x[2], xt[2], a, p, shares, bytes;  // byte offsets
-    Tiles tiles;
-    int m, n;
+    int64_t parts, first, x[2], xt[2], square[kSquares], shares, bytes;  // byte offsets
+    int64_t m, n;
     bool small;  // nothing else then
 };
 
@@ -688,34 +784,28 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     Layout w;
     const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
     w.small = m <= kSmallSide && n <= kSmallLong;
-    if (w.small) {
-        w.m = kSmallSide;
-        w.n = (int)padded(n, 64);
-        w.bytes = 0;
-        return w;
-    }
-    w.tiles = tiles_of(batch, m, n);
-    w.m = (int)padded(m, w.tiles.pad());
-    w.n = (int)padded(n, w.tiles.pad());
+    w.m = m;
+    w.n = n;
+    w.bytes = 0;
+    if (w.small) return w;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    const int64_t xs = batch * w.m * w.n * 2 * (int64_t)sizeof(f16);
-    const int64_t as = batch * w.m * w.m * 2 * (int64_t)sizeof(f16);
+    // tiles of 256 are taken where a side has that many
+    const int64_t pm = padded(m, m > 128 ? kMostPad : 128), pn = padded(n, n > 128 ? kMostPad : 128);
+    const int64_t xs = batch * pm * pn * 2 * (int64_t)sizeof(f16), as = batch * pm * pm * 2 * (int64_t)sizeof(f16);
     w.parts = take(batch * kNormParts * (int64_t)sizeof(double));
     w.first = take(batch * (int64_t)sizeof(Coefficients));
     for (int i = 0; i < 2; ++i) {
         w.x[i] = take(xs);
         w.xt[i] = take(xs);
     }
-    w.a = take(as);
-    w.p = take(as);
-    const int64_t ms = w.m / w.tiles.symmetric, tiles = batch * ms * (ms + 1) / 2;
-    const bool any = shared(w.tiles.symmetric, tiles, w.n) || shared(w.tiles.symmetric, tiles, w.m);
-    w.shares = take(any ? (tiles + kWorkers) * w.tiles.symmetric * w.tiles.symmetric * (int64_t)sizeof(float) : 0);
+    for (int64_t& q : w.square) q = take(as);
+    const int64_t ms = padded(m, kMostPad) / 128;
+    w.shares = take((batch * ms * (ms + 1) / 2 + kWorkers) * 128 * 128 * (int64_t)sizeof(float));
     w.bytes = at + 256;
     return w;
 }
@@ -730,7 +820,7 @@ bool allow_local(K kernel, size_t local) {
 template <Product KIND, int TILE, int LP, int RP, typename T>
 int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float* parts, hipStream_t stream) {
     using S = Shape<TILE>;
-    constexpr bool kSymmetric = KIND == Product::kGram || KIND == Product::kPolynomial;
+    constexpr bool kSymmetric = is_symmetric(KIND);
     constexpr size_t local = (size_t)S::kStages * (LP + RP) * TILE * S::kDepth * sizeof(f16);
     const int64_t tiles = batch * (kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols);
     if constexpr (kSymmetric && TILE == 128) {
@@ -739,8 +829,7 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
             const Shares s{parts, tiles * (o.depth / S::kDepth), o.depth / S::kDepth};
             kernel<<<kWorkers, kThreadsOf<TILE>, local, stream>>>(o, s);
-            constexpr int kGroups = TILE / S::kRows / 16 * (TILE / S::kCols / 16) / kJoin;
-            join_product_kernel<KIND, TILE><<<(unsigned)(tiles * kGroups), kThreadsOf<TILE>, 0, stream>>>(o, s);
+            join_product_kernel<KIND, TILE><<<(unsigned)(tiles * (TILE / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
             return launch_status();
         }
     }
@@ -750,76 +839,125 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
     return launch_status();
 }
 
-// A product by the call's tiles. `exact`: X0 has one plane.
+// Which planes a product takes. kBoth: hi hi + hi lo + lo hi. kExact: X0 from 16 bits, whose lower plane is zero. kUpper:
+// hi hi, for the last product of a call that ends in bf16: an error of 2^-12 below one of 2^-9.
+enum class Depth { kBoth, kExact, kUpper };
+
+// A product by the call's tiles.
 template <Product KIND, typename T>
-int product(Operands o, const Output<T>& out, int64_t batch, int tile, bool exact, float* parts,
+int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth depth, float* parts,
             hipStream_t stream) {
     o.rows = o.rows / tile;
     o.cols = o.cols / tile;
-    // in a first step from 16 bits the lower plane of X is zero: both operands of the Gram matrix, the
-    // right one of the update
-    constexpr int LP = KIND == Product::kGram ? 1 : 2;
-#define LAUNCH(TILE)                                                                                 \
-    if (tile == TILE) {                                                                              \
-        if constexpr (KIND != Product::kPolynomial)                                                  \
-            if (exact) return launch_product<KIND, TILE, LP, 1>(o, out, batch, parts, stream);       \
-        return launch_product<KIND, TILE, 2, 2>(o, out, batch, parts, stream);                       \
+#define LAUNCH(TILE, LP, RP) \
+    if (tile == TILE) return launch_product<KIND, TILE, LP, RP>(o, out, batch, parts, stream)
+    if constexpr (KIND == Product::kLast && sizeof(T) == 2) {
+        if (depth == Depth::kUpper) {
+            LAUNCH(256, 1, 1);
+            LAUNCH(128, 1, 1);
+            LAUNCH(64, 1, 1);
+        }
     }
-    if constexpr (KIND == Product::kUpdate || KIND == Product::kLast) LAUNCH(256)
-    LAUNCH(128)
-    LAUNCH(64)
+    if constexpr (KIND == Product::kGram) {
+        if (depth == Depth::kExact) {
+            LAUNCH(128, 1, 1);
+            LAUNCH(64, 1, 1);
+        }
+    }
+    if constexpr (KIND == Product::kUpdate || KIND == Product::kLast) {
+        if (depth == Depth::kExact) {
+            LAUNCH(256, 2, 1);
+            LAUNCH(128, 2, 1);
+            LAUNCH(64, 2, 1);
+        }
+        LAUNCH(256, 2, 2);
+    }
+    LAUNCH(128, 2, 2);
+    LAUNCH(64, 2, 2);
 #undef LAUNCH
     return TRIVANCE_EINVAL;
 }
 
 template <typename T>
-int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, float eps, const Layout& w,
-        void* workspace, hipStream_t stream) {
+int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, float scale, float eps,
+        const Layout& w, int dtype, void* workspace, hipStream_t stream) {
     if (w.small) {
         SmallSteps s;
         s.steps = steps;
         for (int i = 0; i < steps; ++i) s.k[i] = {k[3 * i], k[3 * i + 1], k[3 * i + 2]};
-        const size_t local = sizeof(half8) * (4 * small_x(w.n) + 4 * kSmallA);
+        const int n = (int)padded(w.n, 64);
+        const size_t local = sizeof(half8) * (4 * small_x(n) + 4 * kSmallA);
         if (!allow_local(&small_kernel<T>, local)) return TRIVANCE_EHIP;
-        small_kernel<T><<<(unsigned)batch, kSmallThreads, local, stream>>>(in, out, w.n, s, eps);
+        small_kernel<T><<<(unsigned)batch, kSmallThreads, local, stream>>>(in, out, n, s, scale, eps);
         return launch_status();
     }
+    const Tiles tiles = tiles_of(batch, w.m, w.n, counts_of(k, steps, dtype, w.m, w.n));
+    const int m = (int)padded(w.m, tiles.pad()), n = (int)padded(w.n, tiles.pad());
     char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
-    const auto planes = [&](int64_t offset, int rows, int ld) {
+    const auto planes = [&](int64_t offset, int64_t rows, int ld) {
         f16* hi = reinterpret_cast<f16*>(base + offset);
-        return Planes{hi, hi + batch * rows * ld, (int64_t)rows * ld, ld};
+        return Planes{hi, hi + batch * rows * ld, rows * ld, ld};
     };
     double* parts = reinterpret_cast<double*>(base + w.parts);
     Coefficients* first = reinterpret_cast<Coefficients*>(base + w.first);
     float* shares = reinterpret_cast<float*>(base + w.shares);
-    Planes x[2], xt[2];
+    Planes x[2], xt[2], a[2], q[2];
     for (int i = 0; i < 2; ++i) {
-        x[i] = planes(w.x[i], w.m, w.n);
-        xt[i] = planes(w.xt[i], w.n, w.m);
+        x[i] = planes(w.x[i], m, n);
+        xt[i] = planes(w.xt[i], n, m);
+        a[i] = planes(w.square[i], m, m);
+        q[i] = planes(w.square[2 + i], m, m);
     }
-    const Planes a = planes(w.a, w.m, w.m), p = planes(w.p, w.m, w.m);
+    const Planes next = planes(w.square[4], m, m), pp = planes(w.square[5], m, m);
     const int rows = in.sj != 1 ? in.n : in.m;
     const int64_t pieces = (int64_t)rows * (((rows == in.n ? in.m : in.n) + 256 * kVec<T> - 1) / (256 * kVec<T>));
     const int nparts = (int)(pieces < kNormParts ? pieces : kNormParts);
     const unsigned nb = (unsigned)batch;
     norm_parts_kernel<T><<<dim3(nparts, nb), 256, 0, stream>>>(in, parts);
-    split_kernel<T><<<dim3(w.n / 64, w.m / 64, nb), 256, 0, stream>>>(
+    split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(
         in, parts, nparts, x[0], xt[0], Coefficients{k[0], k[1], k[2]}, eps, first);
     int rc = launch_status();
-    for (int s = 0; s < steps && !rc; ++s) {
-        const Coefficients c{k[3 * s], k[3 * s + 1], k[3 * s + 2]};
-        const int q = s % 2;
-        const bool exact = s == 0 && sizeof(T) == 2;
-        const Output<f16> none{};
-        rc = product<Product::kGram>({x[q], x[q], w.n, w.m, w.m, a, a, a, c, nullptr}, none, batch,
-                                     w.tiles.symmetric, exact, shares, stream);
+    const Output<f16> none{};
+    const auto square = [&](const Planes& l, const Planes& r, const Planes& c, float factor) {
+        return product<Product::kSquare>({l, r, m, m, m, c, c, factor, a[0], {}, nullptr}, none, batch,
+                                         tiles.symmetric, Depth::kBoth, shares, stream);
+    };
+    int turn = 0;  // of X
+    for (int s = 0; s < steps && !rc;) {
+        const int group = group_of(k, s, steps, dtype, w.m, w.n);
+        const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : Depth::kBoth;
+        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a[0], a[0], 1.0f / kScale, a[0], {}, nullptr},
+                                     none, batch, tiles.symmetric, depth, shares, stream);
+        int at = 0, qt = 0;
+        float qs = kScale;  // Q's scale: factors of up to 15 a step leave it less
+        for (int g = 0; g < group && !rc; ++g) {
+            const Coefficients c{k[3 * (s + g)], k[3 * (s + g) + 1], k[3 * (s + g) + 2]};
+            const Planes p = g == 0 ? q[0] : next;
+            rc = product<Product::kPolynomial>(
+                {a[at], a[at], m, m, m, p, p, 1.0f / kScale, a[at], c, s + g == 0 ? first : nullptr}, none, batch,
+                tiles.symmetric, Depth::kBoth, shares, stream);
+            if (g > 0 && !rc) {
+                rc = square(p, q[qt], q[1 - qt], 1.0f / (16.0f * kScale));
+                qt = 1 - qt;
+                qs /= 16.0f;
+            }
+            if (g + 1 < group && !rc) {  // A <- A (P P), with P P at a sixteenth of the scale
+                rc = square(p, p, pp, 1.0f / (16.0f * kScale));
+                if (!rc) rc = square(a[at], pp, a[1 - at], 16.0f / kScale);
+                at = 1 - at;
+            }
+        }
+        s += group;
         if (rc) break;
-        rc = product<Product::kPolynomial>({a, a, w.m, w.m, w.m, p, p, a, c, s == 0 ? first : nullptr}, none,
-                                           batch, w.tiles.symmetric, false, shares, stream);
-        if (rc) break;
-        const Operands update{p, xt[q], w.m, w.m, w.n, x[1 - q], xt[1 - q], a, c, nullptr};
-        rc = s + 1 < steps ? product<Product::kUpdate>(update, none, batch, w.tiles.update, exact, shares, stream)
-                           : product<Product::kLast>(update, out, batch, w.tiles.update, exact, shares, stream);
+        Operands update{q[qt], xt[turn], m, m, n, x[1 - turn], xt[1 - turn], 1.0f / qs, a[0], {}, nullptr};
+        if (s < steps) {
+            rc = product<Product::kUpdate>(update, none, batch, tiles.update, depth, shares, stream);
+            turn = 1 - turn;
+        } else {
+            update.factor *= scale / kScale;
+            rc = product<Product::kLast>(update, out, batch, tiles.update,
+                                         dtype == TRIVANCE_BF16 ? Depth::kUpper : depth, shares, stream);
+        }
     }
     return rc;
 }
@@ -882,8 +1020,8 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
         return run<T>({static_cast<const T*>(x), x_batch_stride, tall ? 1 : x_row_stride,
                        tall ? x_row_stride : 1, m, n},
                       {static_cast<T*>(out), out_batch_stride, tall ? 1 : out_row_stride,
-                       tall ? out_row_stride : 1, m, n, (float)scale},
-                      batch, steps, coefficients, (float)eps, w, workspace, s);
+                       tall ? out_row_stride : 1, m, n},
+                      batch, steps, coefficients, (float)scale, (float)eps, w, dtype, workspace, s);
     };
     return dtype == TRIVANCE_F32 ? go(float{}) : dtype == TRIVANCE_BF16 ? go(bf16{}) : go(f16{});
 }
