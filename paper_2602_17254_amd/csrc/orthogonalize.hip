@@ -102,12 +102,13 @@ __device__ __forceinline__ void scale_of(double squares, Coefficients c, float e
 }
 
 // X both ways round, scaled by 2^12 over the power of two below the norm and padded with zeros, and the
-// first step's coefficients, which hold what is left of the norm.
+// first step's coefficients. A workgroup takes 64 x 64 values, read as they lie in memory.
 template <typename T>
 __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* parts, int nparts,
                                                     Planes x, Planes xt, Coefficients c, float eps,
                                                     Coefficients* first) {
-    __shared__ float tile[64][65];
+    constexpr int V = kVec<T>, kRow = 64 + 8;
+    __shared__ half8 tiles[2][64 * kRow / 8];
     const int64_t b = blockIdx.z;
     double sum = 0.0;
     for (int i = threadIdx.x % 64; i < nparts; i += 64) sum += parts[b * kNormParts + i];
@@ -118,24 +119,42 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
     scale_of(sum, c, eps, e, mine);
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
     if (i0 == 0 && j0 == 0 && threadIdx.x == 0) first[b] = mine;
-    const T* g = in.x + b * in.batch;
+    // rows and columns as in memory: X's, or those of its transpose
     const bool tall = in.sj != 1;
-    const int lane = threadIdx.x % 64;
-    for (int q = threadIdx.x / 64; q < 64; q += 4) {
-        const int i = tall ? i0 + lane : i0 + q, j = tall ? j0 + q : j0 + lane;
-        const float v = i < in.m && j < in.n ? (float)g[i * in.si + j * in.sj] : 0.0f;
-        if (tall) tile[lane][q] = ldexpf(v, kScaleExp - e);
-        else tile[q][lane] = ldexpf(v, kScaleExp - e);
+    const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0, rows = tall ? in.n : in.m, cols = tall ? in.m : in.n;
+    const T* g = in.x + b * in.batch;
+    const int64_t stride = tall ? in.sj : in.si;
+    f16* hi = reinterpret_cast<f16*>(tiles[0]);
+    f16* lo = reinterpret_cast<f16*>(tiles[1]);
+#pragma unroll
+    for (int q = threadIdx.x; q < 64 * 64 / V; q += 256) {
+        const int r = q / (64 / V), k0 = q % (64 / V) * V;
+        float v[V] = {};
+        if (r0 + r < rows) load_row<T>(g + (r0 + r) * stride, c0 + k0, cols, 0.0f, v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) split(ldexpf(v[k], kScaleExp - e), hi[r * kRow + k0 + k], lo[r * kRow + k0 + k]);
     }
     __syncthreads();
-    for (int q = threadIdx.x / 64; q < 64; q += 4) {
-        const int64_t at = b * x.batch + (int64_t)(i0 + q) * x.ld + j0 + lane;
-        const int64_t att = b * xt.batch + (int64_t)(j0 + q) * xt.ld + i0 + lane;
-        f16 lo;
-        split(tile[q][lane], x.hi[at], lo);
-        if (sizeof(T) > 2) x.lo[at] = lo;  // zero otherwise, and not read in the first step
-        split(tile[lane][q], xt.hi[att], lo);
-        if (sizeof(T) > 2) xt.lo[att] = lo;
+    const Planes straight = tall ? xt : x, turned = tall ? x : xt;
+    // the lower plane of 16-bit values is zero, and not read in the first step
+    constexpr int kPlanes = sizeof(T) > 2 ? 2 : 1;
+#pragma unroll
+    for (int q = threadIdx.x; q < 64 * 8; q += 256) {
+        const int r = q / 8, p = q % 8 * 8;
+        const int64_t at = b * straight.batch + (int64_t)(r0 + r) * straight.ld + c0 + p;
+        // neighbouring lanes take neighbouring rows of the turned tile, whose columns then share banks less
+        const int tr = q % 64, tp = q / 64 * 8;
+        const int64_t att = b * turned.batch + (int64_t)(c0 + tr) * turned.ld + r0 + tp;
+#pragma unroll
+        for (int plane = 0; plane < kPlanes; ++plane) {
+            const f16* tile = plane ? lo : hi;
+            *reinterpret_cast<half8*>((plane ? straight.lo : straight.hi) + at) =
+                *reinterpret_cast<const half8*>(tile + r * kRow + p);
+            half8 t;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = tile[(tp + k) * kRow + tr];
+            *reinterpret_cast<half8*>((plane ? turned.lo : turned.hi) + att) = t;
+        }
     }
 }
 
@@ -312,6 +331,15 @@ template <Product KIND, int MI, typename T>
 __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, int64_t b, Coefficients k,
                                        int i, int j, bool mirrored, const float4v (&sum)[MI], f16* turn) {
     const int lane = threadIdx.x % 64;
+    half4 ah[MI], aw[MI];  // all on their way before the first store
+    if constexpr (KIND == Product::kPolynomial) {
+#pragma unroll
+        for (int x = 0; x < MI; ++x) {
+            const int64_t at = b * o.a.batch + (int64_t)(i + x * 16) * o.a.ld + j;
+            ah[x] = *reinterpret_cast<const half4*>(o.a.hi + at);
+            aw[x] = *reinterpret_cast<const half4*>(o.a.lo + at);
+        }
+    }
 #pragma unroll
     for (int x = 0; x < MI; ++x) {
         const int row = i + x * 16;
@@ -319,12 +347,10 @@ __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, 
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = sum[x][q] * o.factor;
         if constexpr (KIND == Product::kPolynomial) {
-            const int64_t at = b * o.a.batch + (int64_t)row * o.a.ld + j;
-            const half4 h = *reinterpret_cast<const half4*>(o.a.hi + at);
-            const half4 w = *reinterpret_cast<const half4*>(o.a.lo + at);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                v[q] = k.b * ((float)h[q] + (float)w[q]) + k.c * v[q] + (row == j + q ? k.a * kScale : 0.0f);
+                v[q] = k.b * ((float)ah[x][q] + (float)aw[x][q]) + k.c * v[q] +
+                       (row == j + q ? k.a * kScale : 0.0f);
         }
         if constexpr (KIND == Product::kLast) {
             T* to = out.x + b * out.batch + row * out.si + j * out.sj;
@@ -432,9 +458,16 @@ constexpr int kWorkers = 256;
 
 struct Shares {
     float* parts;
-    int64_t stages;  // of all tiles
-    int depth;       // stages of a tile
-    __device__ __forceinline__ int64_t begin(int64_t w) const { return w * stages / kWorkers; }
+    int stages;  // of all tiles
+    int depth;   // stages of a tile
+    __device__ __forceinline__ int begin(int w) const { return (int)((uint64_t)(uint32_t)w * (uint32_t)stages / kWorkers); }
+    // The worker that holds a stage.
+    __device__ __forceinline__ int holder(int stage) const {
+        int w = (int)((float)stage * ((float)kWorkers / (float)stages));
+        while (w > 0 && begin(w) > stage) --w;
+        while (begin(w + 1) <= stage) ++w;
+        return w;
+    }
 };
 
 template <int TILE, int LP, int RP>
@@ -443,17 +476,17 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Ope
     constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
     extern __shared__ half8 stages[];
     const int tiles = o.rows * (o.rows + 1) / 2;
-    const int64_t w = xcd_contiguous(blockIdx.x, kWorkers);
-    const int64_t end = s.begin(w + 1);
-    for (int64_t at = s.begin(w); at < end;) {
-        const int64_t t = at / s.depth;
-        const int64_t stop = (t + 1) * s.depth < end ? (t + 1) * s.depth : end;
+    const int w = xcd_contiguous(blockIdx.x, kWorkers);
+    const int end = s.begin(w + 1);
+    for (int at = s.begin(w); at < end;) {
+        const int t = at / s.depth;
+        const int stop = (t + 1) * s.depth < end ? (t + 1) * s.depth : end;
         int ti, tj;
-        triangle((int)(t % tiles), ti, tj);
+        triangle(t % tiles, ti, tj);
         float4v acc[MI][NI] = {};
-        multiply<TILE, LP, RP>(o, t / tiles, ti * TILE, tj * TILE, (int)(at - t * s.depth) * S::kDepth,
-                               (int)(stop - t * s.depth) * S::kDepth, stages, acc);
-        float* part = s.parts + (t + w) * (TILE * TILE) + threadIdx.x * 4;
+        multiply<TILE, LP, RP>(o, t / tiles, ti * TILE, tj * TILE, (at - t * s.depth) * S::kDepth,
+                               (stop - t * s.depth) * S::kDepth, stages, acc);
+        float* part = s.parts + (int64_t)(t + w) * (TILE * TILE) + threadIdx.x * 4;
 #pragma unroll
         for (int x = 0; x < MI; ++x)
 #pragma unroll
@@ -471,23 +504,29 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
     constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
     __shared__ half8 turns[kThreads / 64 * kTurn<MI> / 8];
     const int tiles = o.rows * (o.rows + 1) / 2;
-    const int64_t t = blockIdx.x / NI;
-    const int y = blockIdx.x % NI;
+    const int t = blockIdx.x / NI, y = blockIdx.x % NI;
     const int64_t b = t / tiles;
     int ti, tj;
-    triangle((int)(t % tiles), ti, tj);
-    // the workers that hold the tile's first and last stage
-    const int64_t first = t * s.depth, last = first + s.depth - 1;
-    int64_t w0 = first * kWorkers / s.stages, w1 = last * kWorkers / s.stages;
-    while (s.begin(w0 + 1) <= first) ++w0;
-    while (s.begin(w1 + 1) <= last) ++w1;
+    triangle(t % tiles, ti, tj);
+    const int w0 = s.holder(t * s.depth), w1 = s.holder((t + 1) * s.depth - 1);
+    const float* part = s.parts + (int64_t)t * (TILE * TILE) + y * (MI * kThreads * 4) + threadIdx.x * 4;
     float4v sum[MI] = {};
-    for (int64_t w = w0; w <= w1; ++w) {
-        if (s.begin(w) == s.begin(w + 1)) continue;  // a worker without a stage
-        const float* part = s.parts + (t + w) * (TILE * TILE) + threadIdx.x * 4;
+    constexpr int kAtOnce = 3;  // workers whose parts are on their way together
+    for (int w = w0; w <= w1; w += kAtOnce) {
+        float4v v[kAtOnce][MI];
 #pragma unroll
-        for (int x = 0; x < MI; ++x)
-            sum[x] += *reinterpret_cast<const float4v*>(part + (y * MI + x) * (kThreads * 4));
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int from = w + q <= w1 ? w + q : w1;
+#pragma unroll
+            for (int x = 0; x < MI; ++x)
+                v[q][x] = *reinterpret_cast<const float4v*>(part + (int64_t)from * (TILE * TILE) + x * (kThreads * 4));
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q)
+            if (w + q <= w1) {
+#pragma unroll
+                for (int x = 0; x < MI; ++x) sum[x] += v[q][x];
+            }
     }
     Coefficients k = o.k;
     if (KIND == Product::kPolynomial && o.first) k = o.first[b];
@@ -695,8 +734,9 @@ int64_t padded(int64_t side, int tile) { return (side + tile - 1) / tile * tile;
 // costs a launch and the parts' way through memory, about 10 us: a round of tiles of 128 takes 30 us for
 // 1000 values of the summed index. 136 tiles from 2048 measured 60 us as they are and 43 shared out,
 // from 8192 200 and 117.
+// Every worker has a stage then.
 bool shared(int tile, int64_t tiles, int64_t depth) {
-    if (tile != 128) return false;
+    if (tile != 128 || tiles * (depth / 64) < kWorkers || tiles * (depth / 64) > INT32_MAX / 2) return false;
     const double rounds = tiles / 256.0, idle = std::ceil(rounds) - rounds;
     return idle * depth >= 512.0;
 }
@@ -827,7 +867,7 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
         if (shared(TILE, tiles, o.depth)) {
             const auto kernel = shared_product_kernel<TILE, LP, RP>;
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
-            const Shares s{parts, tiles * (o.depth / S::kDepth), o.depth / S::kDepth};
+            const Shares s{parts, (int)tiles * (o.depth / S::kDepth), o.depth / S::kDepth};
             kernel<<<kWorkers, kThreadsOf<TILE>, local, stream>>>(o, s);
             join_product_kernel<KIND, TILE><<<(unsigned)(tiles * (TILE / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
             return launch_status();
