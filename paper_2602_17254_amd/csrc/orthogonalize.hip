@@ -451,19 +451,22 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void product_kernel(Operands o
     }
 }
 
-// A symmetric product whose tiles fill the GPU badly: kWorkers workgroups share all stages of all
-// tiles evenly, in order, and leave each part of a tile's sum in memory, in the order of the registers; the
-// part of worker w in tile t is part t + w.
-constexpr int kWorkers = 256;
+// A symmetric product whose tiles fill the GPU badly: workgroups share all stages of all tiles evenly, in
+// order, and leave each part of a tile's sum in memory, in the order of the registers; the part of
+// worker w in tile t is part t + w.
+constexpr int kMostWorkers = 256;
 
 struct Shares {
     float* parts;
-    int stages;  // of all tiles
-    int depth;   // stages of a tile
-    __device__ __forceinline__ int begin(int w) const { return (int)((uint64_t)(uint32_t)w * (uint32_t)stages / kWorkers); }
+    int stages;   // of all tiles
+    int depth;    // stages of a tile
+    int workers;  // as many as there are stages, or fewer
+    __device__ __forceinline__ int begin(int w) const {
+        return (int)((uint64_t)(uint32_t)w * (uint32_t)stages / (uint32_t)workers);
+    }
     // The worker that holds a stage.
     __device__ __forceinline__ int holder(int stage) const {
-        int w = (int)((float)stage * ((float)kWorkers / (float)stages));
+        int w = (int)((float)stage * ((float)workers / (float)stages));
         while (w > 0 && begin(w) > stage) --w;
         while (begin(w + 1) <= stage) ++w;
         return w;
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Ope
     constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
     extern __shared__ half8 stages[];
     const int tiles = o.rows * (o.rows + 1) / 2;
-    const int w = xcd_contiguous(blockIdx.x, kWorkers);
+    const int w = xcd_contiguous(blockIdx.x, s.workers);
     const int end = s.begin(w + 1);
     for (int at = s.begin(w); at < end;) {
         const int t = at / s.depth;
@@ -619,6 +622,106 @@ __device__ __forceinline__ void local_store(LocalPlanes m, const LocalPlanes* t,
 __host__ __device__ constexpr int small_x(int n) { return kSmallSide * n / 8; }
 constexpr int kSmallA = kSmallSide * kSmallSide / 8;
 
+// A workgroup's matrices in local memory, for n columns of X (whole panels).
+struct SmallLocal {
+    LocalPlanes x, xt, a, p;
+    __device__ __forceinline__ SmallLocal(half8* local, int n)
+        : x{local, local + small_x(n), kSmallA},
+          xt{local + 2 * small_x(n), local + 3 * small_x(n), 0},
+          a{local + 4 * small_x(n), local + 4 * small_x(n) + kSmallA, 0},
+          p{local + 4 * small_x(n) + 2 * kSmallA, local + 4 * small_x(n) + 3 * kSmallA, 0} {}
+};
+
+// Its columns of G, from j0 on, in registers; G's contiguous index runs over the lanes.
+constexpr int kSmallMine = kSmallSide * kSmallLong / kSmallThreads;
+
+__device__ __forceinline__ void small_place(bool tall, int q, int& i, int& j) {
+    i = tall ? threadIdx.x % kSmallSide : q * (kSmallThreads / kSmallLong) + threadIdx.x / kSmallLong;
+    j = tall ? q * (kSmallThreads / kSmallSide) + threadIdx.x / kSmallSide : threadIdx.x % kSmallLong;
+}
+
+template <typename T>
+__device__ __forceinline__ void small_fetch(const Input<T>& in, int64_t b, int j0, float (&v)[kSmallMine]) {
+    const T* g = in.x + b * in.batch;
+#pragma unroll
+    for (int q = 0; q < kSmallMine; ++q) {
+        int i, j;
+        small_place(in.sj != 1, q, i, j);
+        v[q] = i < in.m && j0 + j < in.n ? (float)g[i * in.si + (j0 + j) * in.sj] : 0.0f;
+    }
+}
+
+__device__ __forceinline__ void small_split(const SmallLocal& m, bool tall, int n, int exponent,
+                                            const float (&v)[kSmallMine]) {
+#pragma unroll
+    for (int q = 0; q < kSmallMine; ++q) {
+        int i, j;
+        small_place(tall, q, i, j);
+        if (j >= n) continue;
+        f16 hi, lo;
+        split(ldexpf(v[q], exponent), hi, lo);
+        const int to = (j / 64 * kSmallA + i * 8 + permuted(i, j % 64 / 8)) * 8 + j % 8;
+        const int too = (j * 8 + permuted(j, i / 8)) * 8 + i % 8;
+        reinterpret_cast<f16*>(m.x.hi)[to] = hi;
+        reinterpret_cast<f16*>(m.x.lo)[to] = lo;
+        reinterpret_cast<f16*>(m.xt.hi)[too] = hi;
+        reinterpret_cast<f16*>(m.xt.lo)[too] = lo;
+    }
+}
+
+// The wave's tile of A over the workgroup's columns, as sums of stored values.
+__device__ __forceinline__ float4v small_gram(const SmallLocal& m, int n, int ti, int tj, const LaneOffsets& at) {
+    float4v acc[1] = {};
+    for (int q = 0; q < n / 64; ++q) local_product<1>(m.x, ti, m.x, tj, q, at, acc);
+    return acc[0];
+}
+
+// From the wave's tile of A to its tile of P in local memory, for everyone.
+__device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a, Coefficients k, int ti, int tj,
+                                                 const LaneOffsets& at) {
+    float gram[4], poly[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) gram[c] = a[c] * (1.0f / kScale);
+    local_store(m.a, nullptr, ti, tj, at, gram);
+    __syncthreads();
+    float4v acc[1] = {};
+    local_product<1>(m.a, ti, m.a, tj, 0, at, acc);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        poly[c] = k.b * gram[c] + k.c * (acc[0][c] * (1.0f / kScale)) +
+                  (ti + at.row == tj + at.column + c ? k.a * kScale : 0.0f);
+    local_store(m.p, nullptr, ti, tj, at, poly);
+    __syncthreads();
+}
+
+// X <- P X in local memory, or with `last` to the caller, whose columns begin at j0.
+template <typename T>
+__device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col, const LaneOffsets& at, bool last,
+                                             const Output<T>& out, int64_t b, int j0, float scale) {
+    constexpr int kTiles = kSmallSide / 16;
+    float4v next[kTiles] = {};
+    if (col < n) local_product<kTiles>(m.p, 0, m.xt, col, 0, at, next);
+    __syncthreads();
+    if (col < n) {
+#pragma unroll
+        for (int y = 0; y < kTiles; ++y) {
+            float w[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w[c] = next[y][c] * (1.0f / kScale);
+            if (!last) {
+                local_store(m.x, &m.xt, y * 16, col, at, w);
+                continue;
+            }
+            const int i = y * 16 + at.row, j = j0 + col + at.column;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (i < out.m && j + c < out.n)
+                    out.x[b * out.batch + i * out.si + (j + c) * out.sj] = (T)(w[c] * (scale / kScale));
+        }
+    }
+    __syncthreads();
+}
+
 // n: X's columns padded to whole panels.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Output<T> out, int n, SmallSteps s,
@@ -627,32 +730,16 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     constexpr int kWaves = kSmallThreads / 64, kTiles = kSmallSide / 16;
     static_assert(kTiles * kTiles == kWaves && kSmallLong / 16 == kWaves, "a tile of A, a column of X a wave");
-    const int xs = small_x(n);
-    const LocalPlanes x{local, local + xs, kSmallA}, xt{local + 2 * xs, local + 3 * xs, 0};
-    const LocalPlanes a{local + 4 * xs, local + 4 * xs + kSmallA, 0};
-    const LocalPlanes p{local + 4 * xs + 2 * kSmallA, local + 4 * xs + 3 * kSmallA, 0};
+    const SmallLocal m(local, n);
     const LaneOffsets at(lane);
-
-    // G once, in registers; its contiguous index over the lanes
-    constexpr int kMine = kSmallSide * kSmallLong / kSmallThreads;
-    const T* g = in.x + blockIdx.x * in.batch;
-    const bool tall = in.sj != 1;
-    float v[kMine];
+    float v[kSmallMine];
+    small_fetch(in, blockIdx.x, 0, v);
     double sum = 0.0;
-    const auto place = [&](int q, int& i, int& j) {
-        i = tall ? threadIdx.x % kSmallSide : q * (kSmallThreads / kSmallLong) + threadIdx.x / kSmallLong;
-        j = tall ? q * (kSmallThreads / kSmallSide) + threadIdx.x / kSmallSide : threadIdx.x % kSmallLong;
-    };
 #pragma unroll
-    for (int q = 0; q < kMine; ++q) {
-        int i, j;
-        place(q, i, j);
-        v[q] = i < in.m && j < in.n ? (float)g[i * in.si + j * in.sj] : 0.0f;
-        sum += (double)v[q] * (double)v[q];
-    }
+    for (int q = 0; q < kSmallMine; ++q) sum += (double)v[q] * (double)v[q];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    double* sums = reinterpret_cast<double*>(p.hi);
+    double* sums = reinterpret_cast<double*>(m.p.hi);
     if (lane == 0) sums[wave] = sum;
     __syncthreads();
     sum = 0.0;
@@ -661,65 +748,85 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
     int e;
     Coefficients first;
     scale_of(sum, s.k[0], eps, e, first);
-#pragma unroll
-    for (int q = 0; q < kMine; ++q) {
-        int i, j;
-        place(q, i, j);
-        if (j >= n) continue;
-        f16 hi, lo;
-        split(ldexpf(v[q], kScaleExp - e), hi, lo);
-        const int to = (j / 64 * kSmallA + i * 8 + permuted(i, j % 64 / 8)) * 8 + j % 8;
-        const int too = (j * 8 + permuted(j, i / 8)) * 8 + i % 8;
-        reinterpret_cast<f16*>(x.hi)[to] = hi;
-        reinterpret_cast<f16*>(x.lo)[to] = lo;
-        reinterpret_cast<f16*>(xt.hi)[too] = hi;
-        reinterpret_cast<f16*>(xt.lo)[too] = lo;
-    }
+    small_split(m, in.sj != 1, n, kScaleExp - e, v);
     __syncthreads();
-
     const int ti = wave / kTiles * 16, tj = wave % kTiles * 16;  // the wave's tile of A and P
-    const int col = wave * 16;                                   // and its columns of X
     for (int step = 0; step < s.steps; ++step) {
-        const Coefficients k = step == 0 ? first : s.k[step];
-        float4v acc[1] = {};
-        for (int q = 0; q < n / 64; ++q) local_product<1>(x, ti, x, tj, q, at, acc);
-        float gram[4], poly[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) gram[c] = acc[0][c] * (1.0f / kScale);
-        local_store(a, nullptr, ti, tj, at, gram);
-        __syncthreads();
-        acc[0] = float4v{};
-        local_product<1>(a, ti, a, tj, 0, at, acc);
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            poly[c] = k.b * gram[c] + k.c * (acc[0][c] * (1.0f / kScale)) +
-                      (ti + at.row == tj + at.column + c ? k.a * kScale : 0.0f);
-        local_store(p, nullptr, ti, tj, at, poly);
-        __syncthreads();
-        float4v next[kTiles] = {};
-        if (col < n) local_product<kTiles>(p, 0, xt, col, 0, at, next);
-        const bool last = step + 1 == s.steps;
-        __syncthreads();
-        if (col < n) {
-#pragma unroll
-            for (int y = 0; y < kTiles; ++y) {
-                float w[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = next[y][c] * (1.0f / kScale);
-                if (!last) {
-                    local_store(x, &xt, y * 16, col, at, w);
-                    continue;
-                }
-                const int i = y * 16 + at.row, j = col + at.column;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (i < out.m && j + c < out.n)
-                        out.x[blockIdx.x * out.batch + i * out.si + (j + c) * out.sj] =
-                            (T)(w[c] * (scale / kScale));
-            }
-        }
-        __syncthreads();
+        small_polynomial(m, small_gram(m, n, ti, tj, at), step == 0 ? first : s.k[step], ti, tj, at);
+        small_update(m, n, wave * 16, at, step + 1 == s.steps, out, blockIdx.x, 0, scale);
     }
+}
+
+// Matrices of up to 64 rows and some thousand columns: strips of 256 columns, each with a workgroup that keeps
+// it as the one above does, and one launch a step. What a step needs of the other strips is their part of
+// A, which they left in memory in the launch before; every workgroup adds all parts in order and
+// forms P for itself. 64 x 2048 takes 67 us, and 149 with the product kernels, whose only tile of A runs
+// through 2048 columns on one CU.
+constexpr int kMostStrips = 32;
+
+struct Strips {
+    float* parts;  // [batch][strips][64 x 64], in the order of the registers: read; `made`: written
+    float* made;
+    half8* planes;  // [batch][strips]: X of a strip as in local memory
+    int strips;
+};
+
+constexpr int kStripPlanes = 4 * small_x(kSmallLong);  // pieces
+
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in, const double* norm, int nparts,
+                                                                    Coefficients k, float eps, Strips s,
+                                                                    Coefficients* first) {
+    extern __shared__ half8 local[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t b = blockIdx.y, strip = b * s.strips + blockIdx.x;
+    const SmallLocal m(local, kSmallLong);
+    const LaneOffsets at(lane);
+    float v[kSmallMine];
+    small_fetch(in, b, blockIdx.x * kSmallLong, v);
+    double sum = 0.0;
+    for (int i = lane; i < nparts; i += 64) sum += norm[b * kNormParts + i];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    int e;
+    Coefficients mine;
+    scale_of(sum, k, eps, e, mine);
+    if (blockIdx.x == 0 && threadIdx.x == 0) first[b] = mine;
+    small_split(m, in.sj != 1, kSmallLong, kScaleExp - e, v);
+    __syncthreads();
+    const float4v a = small_gram(m, kSmallLong, wave / 4 * 16, wave % 4 * 16, at);
+    reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
+#pragma unroll
+    for (int q = 0; q < kStripPlanes; q += kSmallThreads)
+        s.planes[strip * kStripPlanes + q + threadIdx.x] = local[q + threadIdx.x];
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out, Strips s, Coefficients k,
+                                                                   const Coefficients* first, bool last,
+                                                                   float scale) {
+    extern __shared__ half8 local[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t b = blockIdx.y, strip = b * s.strips + blockIdx.x;
+    const SmallLocal m(local, kSmallLong);
+    const LaneOffsets at(lane);
+#pragma unroll
+    for (int q = 0; q < kStripPlanes; q += kSmallThreads)
+        local[q + threadIdx.x] = s.planes[strip * kStripPlanes + q + threadIdx.x];
+    const float4v* parts = reinterpret_cast<const float4v*>(s.parts) + b * s.strips * kSmallThreads + threadIdx.x;
+    float4v a = {};
+#pragma unroll 8
+    for (int q = 0; q < s.strips; ++q) a += parts[q * kSmallThreads];
+    if (first) k = first[b];
+    const int ti = wave / 4 * 16, tj = wave % 4 * 16;
+    small_polynomial(m, a, k, ti, tj, at);
+    small_update(m, kSmallLong, wave * 16, at, last, out, b, blockIdx.x * kSmallLong, scale);
+    if (last) return;
+    a = small_gram(m, kSmallLong, ti, tj, at);
+    reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
+#pragma unroll
+    for (int q = 0; q < kStripPlanes; q += kSmallThreads)
+        s.planes[strip * kStripPlanes + q + threadIdx.x] = local[q + threadIdx.x];
 }
 
 // The tiles of a call: of the symmetric products and of the others. Sides are padded to the larger.
@@ -730,15 +837,19 @@ struct Tiles {
 
 int64_t padded(int64_t side, int tile) { return (side + tile - 1) / tile * tile; }
 
-// Whether a symmetric product's stages are shared out evenly. It leaves no CU idle in the last round, and
-// costs a launch and the parts' way through memory, about 10 us: a round of tiles of 128 takes 30 us for
-// 1000 values of the summed index. 136 tiles from 2048 measured 60 us as they are and 43 shared out,
-// from 8192 200 and 117.
-// Every worker has a stage then.
-bool shared(int tile, int64_t tiles, int64_t depth) {
-    if (tile != 128 || tiles * (depth / 64) < kWorkers || tiles * (depth / 64) > INT32_MAX / 2) return false;
-    const double rounds = tiles / 256.0, idle = std::ceil(rounds) - rounds;
-    return idle * depth >= 512.0;
+// Over how many workgroups a symmetric product's stages are shared out; 0: a workgroup takes a tile. It leaves
+// no CU idle, and costs a launch and the parts' way through memory, 6 to 14 us. With tiles of 128 the
+// idle CUs of the last round decide: a round takes 30 us for 1000 values of the summed index. 136 tiles from
+// 2048 measured 60 us as they are and 53 shared out, from 8192 200 and 130. Tiles of 64 take 0.56 us a stage
+// of 64; a worker has two stages or more.
+int workers_of(int tile, int64_t tiles, int64_t depth) {
+    const int64_t all = tiles * (depth / 64);
+    if (all > INT32_MAX / 2) return 0;
+    const double rounds = tiles / 256.0;
+    if (tile == 128) return all >= kMostWorkers && (std::ceil(rounds) - rounds) * depth >= 512.0 ? kMostWorkers : 0;
+    if (tile != 64 || all < 4) return 0;
+    const int64_t w = all / 2 < kMostWorkers ? all / 2 : kMostWorkers;
+    return 0.56 * all / w + 6.0 < 0.56 * std::ceil(rounds) * (depth / 64) ? (int)w : 0;
 }
 
 // How many products of each sort a call takes.
@@ -751,7 +862,7 @@ struct Counts {
 Tiles tiles_of(int64_t batch, int64_t m, int64_t n, Counts count) {
     const auto cost = [&](int tile, int64_t tiles, int64_t depth, bool symmetric) {
         const double rate = tile == 256 ? 1.0 : tile == 128 ? 0.76 : 0.5;
-        const bool share = symmetric && shared(tile, batch * tiles, depth);
+        const bool share = symmetric && workers_of(tile, batch * tiles, depth);
         const double rounds = share ? batch * tiles / 256.0 : (double)((batch * tiles + 255) / 256);
         // in units of 1/720000 us; the second launch of shared products takes 10 us
         return rounds * tile * tile * depth / rate + (share ? 7.2e6 : 0.0);
@@ -816,8 +927,10 @@ constexpr int kSquares = 6, kMostPad = 256;
 
 struct Layout {
     int64_t parts, first, x[2], xt[2], square[kSquares], shares, bytes;  // byte offsets
+    int64_t strip_parts[2], strip_planes;
     int64_t m, n;
-    bool small;  // nothing else then
+    bool small;   // nothing else then
+    int strips;   // 0: the product kernels; otherwise norm, first and strips only
 };
 
 Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
@@ -827,7 +940,9 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     w.m = m;
     w.n = n;
     w.bytes = 0;
+    w.strips = 0;
     if (w.small) return w;
+    if (m <= kSmallSide && n <= kSmallLong * kMostStrips) w.strips = (int)padded(n, kSmallLong) / kSmallLong;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -839,13 +954,24 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     const int64_t xs = batch * pm * pn * 2 * (int64_t)sizeof(f16), as = batch * pm * pm * 2 * (int64_t)sizeof(f16);
     w.parts = take(batch * kNormParts * (int64_t)sizeof(double));
     w.first = take(batch * (int64_t)sizeof(Coefficients));
+    if (w.strips) {
+        for (int64_t& p : w.strip_parts) p = take(batch * w.strips * kSmallSide * kSmallSide * (int64_t)sizeof(float));
+        w.strip_planes = take(batch * w.strips * kStripPlanes * (int64_t)sizeof(half8));
+        w.bytes = at + 256;
+        return w;
+    }
     for (int i = 0; i < 2; ++i) {
         w.x[i] = take(xs);
         w.xt[i] = take(xs);
     }
     for (int64_t& q : w.square) q = take(as);
-    const int64_t ms = padded(m, kMostPad) / 128;
-    w.shares = take((batch * ms * (ms + 1) / 2 + kWorkers) * 128 * 128 * (int64_t)sizeof(float));
+    int64_t most = 0;
+    for (const int64_t tile : {64, 128}) {
+        const int64_t ms = pm / tile;
+        const int64_t bytes = (batch * ms * (ms + 1) / 2 + kMostWorkers) * tile * tile * (int64_t)sizeof(float);
+        most = bytes > most ? bytes : most;
+    }
+    w.shares = take(most);
     w.bytes = at + 256;
     return w;
 }
@@ -863,12 +989,12 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
     constexpr bool kSymmetric = is_symmetric(KIND);
     constexpr size_t local = (size_t)S::kStages * (LP + RP) * TILE * S::kDepth * sizeof(f16);
     const int64_t tiles = batch * (kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols);
-    if constexpr (kSymmetric && TILE == 128) {
-        if (shared(TILE, tiles, o.depth)) {
+    if constexpr (kSymmetric) {
+        if (const int workers = workers_of(TILE, tiles, o.depth)) {
             const auto kernel = shared_product_kernel<TILE, LP, RP>;
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
-            const Shares s{parts, (int)tiles * (o.depth / S::kDepth), o.depth / S::kDepth};
-            kernel<<<kWorkers, kThreadsOf<TILE>, local, stream>>>(o, s);
+            const Shares s{parts, (int)tiles * (o.depth / S::kDepth), o.depth / S::kDepth, workers};
+            kernel<<<workers, kThreadsOf<TILE>, local, stream>>>(o, s);
             join_product_kernel<KIND, TILE><<<(unsigned)(tiles * (TILE / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
             return launch_status();
         }
@@ -931,15 +1057,39 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
         small_kernel<T><<<(unsigned)batch, kSmallThreads, local, stream>>>(in, out, n, s, scale, eps);
         return launch_status();
     }
+    char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
+    double* parts = reinterpret_cast<double*>(base + w.parts);
+    Coefficients* first = reinterpret_cast<Coefficients*>(base + w.first);
+    const unsigned nb = (unsigned)batch;
+    const int rows = in.sj != 1 ? in.n : in.m;
+    const int64_t pieces = (int64_t)rows * (((rows == in.n ? in.m : in.n) + 256 * kVec<T> - 1) / (256 * kVec<T>));
+    const int nparts = (int)(pieces < kNormParts ? pieces : kNormParts);
+    const Coefficients k0{k[0], k[1], k[2]};
+    norm_parts_kernel<T><<<dim3(nparts, nb), 256, 0, stream>>>(in, parts);
+    if (w.strips) {
+        const size_t local = sizeof(half8) * (kStripPlanes + 4 * kSmallA);
+        if (!allow_local(&strip_start_kernel<T>, local) || !allow_local(&strip_step_kernel<T>, local))
+            return TRIVANCE_EHIP;
+        Strips s{reinterpret_cast<float*>(base + w.strip_parts[0]), reinterpret_cast<float*>(base + w.strip_parts[1]),
+                 reinterpret_cast<half8*>(base + w.strip_planes), w.strips};
+        const dim3 grid(w.strips, nb);
+        strip_start_kernel<T><<<grid, kSmallThreads, local, stream>>>(in, parts, nparts, k0, eps, s, first);
+        for (int i = 0; i < steps; ++i) {
+            float* read = s.made;
+            s.made = s.parts;
+            s.parts = read;
+            strip_step_kernel<T><<<grid, kSmallThreads, local, stream>>>(
+                out, s, Coefficients{k[3 * i], k[3 * i + 1], k[3 * i + 2]}, i == 0 ? first : nullptr,
+                i + 1 == steps, scale);
+        }
+        return launch_status();
+    }
     const Tiles tiles = tiles_of(batch, w.m, w.n, counts_of(k, steps, dtype, w.m, w.n));
     const int m = (int)padded(w.m, tiles.pad()), n = (int)padded(w.n, tiles.pad());
-    char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
     const auto planes = [&](int64_t offset, int64_t rows, int ld) {
         f16* hi = reinterpret_cast<f16*>(base + offset);
         return Planes{hi, hi + batch * rows * ld, rows * ld, ld};
     };
-    double* parts = reinterpret_cast<double*>(base + w.parts);
-    Coefficients* first = reinterpret_cast<Coefficients*>(base + w.first);
     float* shares = reinterpret_cast<float*>(base + w.shares);
     Planes x[2], xt[2], a[2], q[2];
     for (int i = 0; i < 2; ++i) {
@@ -949,13 +1099,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
         q[i] = planes(w.square[2 + i], m, m);
     }
     const Planes next = planes(w.square[4], m, m), pp = planes(w.square[5], m, m);
-    const int rows = in.sj != 1 ? in.n : in.m;
-    const int64_t pieces = (int64_t)rows * (((rows == in.n ? in.m : in.n) + 256 * kVec<T> - 1) / (256 * kVec<T>));
-    const int nparts = (int)(pieces < kNormParts ? pieces : kNormParts);
-    const unsigned nb = (unsigned)batch;
-    norm_parts_kernel<T><<<dim3(nparts, nb), 256, 0, stream>>>(in, parts);
-    split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(
-        in, parts, nparts, x[0], xt[0], Coefficients{k[0], k[1], k[2]}, eps, first);
+    split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(in, parts, nparts, x[0], xt[0], k0, eps, first);
     int rc = launch_status();
     const Output<f16> none{};
     const auto square = [&](const Planes& l, const Planes& r, const Planes& c, float factor) {

@@ -379,7 +379,9 @@ def test_balance_gradient_of_the_sum_over_ranks_against_differences(experts):
 
 
 ORTHO_SIZES = [(1, 1, 1), (1, 1, 40), (2, 7, 3), (1, 16, 16), (3, 33, 65), (1, 64, 256), (2, 100, 64),
-               (1, 257, 130), (1, 128, 515), (2, 300, 300), (1, 20, 2000), (1, 640, 200), (1, 515, 1030)]
+               (1, 257, 130), (1, 128, 515), (2, 300, 300), (1, 20, 2000), (1, 640, 200), (1, 515, 1030),
+              (2, 64, 515), (3, 700, 33), (1, 64, 8192), (1, 50, 9000), (2, 1100, 520), (1, 520, 2600),
+              (1, 1280, 1280), (1, 600, 5000)]
 QUINTIC = [(3.4445, -4.7750, 2.0315)] * 5
 
 
