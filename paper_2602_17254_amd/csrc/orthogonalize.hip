@@ -173,29 +173,36 @@ struct Output {
     int m, n;
 };
 
-// How a square tile of a product is computed: the rows and columns of waves that share it, the values
-// of the summed index in one stage of local memory, and the stages. Rates measured
-// with both operands in two planes, on 2048 x 8192 from 2048 and on 2048 x 2048 from 2048: tiles of 256
-// 1125 and 370 TFLOP/s (64 tiles for 256 CUs), of 128 860 and 860, of 64 530 and 574 with two stages.
-// Larger tiles read less of the operands again; a stage of 64 halves the barriers, and tiles of 256
-// have no room for it. Tiles of 64 serve products too small to fill the GPU; there stages of 32 or 128
-// values, three or four stages, and 8 or 16 waves all measured within 15% of this one (135 tiles from
-// 768, 351 from 576).
-template <int TILE>
+// How a square tile of a product is computed: its side, the rows and columns of waves that share it, and the
+// values of the summed index in one stage of local memory, of which two lie there. Rates measured with both
+// operands in two planes, on 2048 x 8192 from 2048 and on 2048 x 2048 from 2048: tiles of 256 1125 and
+// 370 TFLOP/s (64 tiles for 256 CUs), of 128 860 and 860, of 64 530 and 574. Larger tiles read less of the
+// operands again; a longer stage saves barriers. Tiles of 64 serve products too small to fill the GPU:
+// with at most one for each CU (k64Few) 16 waves and stages of 128 measured 10.4 us on 135 tiles from 768, 4
+// waves and stages of 64 12.6; with more the latter, of which a CU holds two, 185 us against 223 for
+// eight matrices of 512 x 512. Three or four stages were no faster than two, and operands straight to
+// registers, each wave on every fourth part of the summed index, half as slow again.
+enum class Tile { k256, k128, k64, k64Few };
+
+template <Tile TILE>
 struct Shape;
 template <>
-struct Shape<256> {
-    static constexpr int kRows = 2, kCols = 4, kDepth = 32, kStages = 2;
+struct Shape<Tile::k256> {
+    static constexpr int kSide = 256, kRows = 2, kCols = 4, kDepth = 32;
 };
 template <>
-struct Shape<128> {
-    static constexpr int kRows = 2, kCols = 2, kDepth = 64, kStages = 2;
+struct Shape<Tile::k128> {
+    static constexpr int kSide = 128, kRows = 2, kCols = 2, kDepth = 64;
 };
 template <>
-struct Shape<64> {
-    static constexpr int kRows = 2, kCols = 2, kDepth = 64, kStages = 2;
+struct Shape<Tile::k64> {
+    static constexpr int kSide = 64, kRows = 2, kCols = 2, kDepth = 64;
 };
-template <int TILE>
+template <>
+struct Shape<Tile::k64Few> {
+    static constexpr int kSide = 64, kRows = 4, kCols = 4, kDepth = 128;
+};
+template <Tile TILE>
 constexpr int kThreadsOf = Shape<TILE>::kRows * Shape<TILE>::kCols * 64;
 
 // Where a stage holds 16-byte piece p of a row of DEPTH values: pieces are permuted within their row so
@@ -203,6 +210,7 @@ constexpr int kThreadsOf = Shape<TILE>::kRows * Shape<TILE>::kCols * 64;
 template <int DEPTH>
 __device__ __forceinline__ int piece_of(int row, int p) {
     if constexpr (DEPTH == 32) return p ^ ((row >> 1 & 3) ^ (row >> 3 & 1));
+    if constexpr (DEPTH == 128) return p ^ (row & 15);
     return p ^ ((row & 7) ^ (row >> 3 & 1));
 }
 
@@ -224,24 +232,16 @@ struct Operands {
     const Coefficients* first;  // in place of k, for each matrix
 };
 
-// Waits until at most `n` of the wave's loads are on their way and its reads of local memory have arrived.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    static_assert(N < 64, "vmcnt has six bits");
-    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
-}
-
-// A workgroup's tile: the sums over values d0 .. d1 (whole stages) of the summed index of rows i0 of L and
-// j0 of R. LP and RP: the planes that are not zero. While the waves multiply one stage of the
-// operands the next ones are on their way into the other parts of local memory, so a stage has one
-// barrier.
-template <int TILE, int LP, int RP, int MI, int NI>
+// A workgroup's tile: the sums over values d0 .. d1 of the summed index of rows i0 of L and j0 of R; d1 - d0 is a
+// multiple of 64, and a last stage of 128 may be half one. LP and RP: the planes that are not zero. While the
+// waves multiply one stage of the operands the next one is on its way into the other half of local
+// memory, so a stage has one barrier.
+template <Tile TILE, int LP, int RP, int MI, int NI>
 __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
                                          half8* stages, float4v (&acc)[MI][NI]) {
     using S = Shape<TILE>;
     constexpr int kThreads = kThreadsOf<TILE>, kDepth = S::kDepth, kPieces = kDepth / 8;
-    constexpr int kPlane = TILE * kPieces, kStage = (LP + RP) * kPlane;
-    constexpr int kLoads = kStage / kThreads;  // of a thread for a stage
+    constexpr int kPlane = S::kSide * kPieces, kStage = (LP + RP) * kPlane;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wi = wave / S::kCols * (MI * 16), wj = wave % S::kCols * (NI * 16);
     const f16* lsrc[2] = {o.l.hi + b * o.l.batch + (int64_t)i0 * o.l.ld,
@@ -257,30 +257,26 @@ __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, i
             const int64_t ld = left ? o.l.ld : o.r.ld;
 #pragma unroll
             for (int q0 = 0; q0 < kPlane; q0 += kThreads) {
-                const int q = q0 + threadIdx.x, row = q / kPieces;
-                copy_to_local(src + row * ld + d + piece_of<kDepth>(row, q % kPieces) * 8,
-                              stage + p * kPlane + q0 + wave * 64);
+                const int q = q0 + threadIdx.x, row = q / kPieces, at = piece_of<kDepth>(row, q % kPieces) * 8;
+                if (kDepth <= 64 || d + at < d1)
+                    copy_to_local(src + row * ld + d + at, stage + p * kPlane + q0 + wave * 64);
             }
         }
     };
-#pragma unroll
-    for (int s = 0; s + 1 < S::kStages; ++s)
-        if (d0 + s * kDepth < d1) load(d0 + s * kDepth, s);
-    for (int d = d0, part = 0; d < d1; d += kDepth) {
-        // this stage has arrived, and every wave has read the one before, whose place is taken next
+    load(d0, 0);
+    for (int d = d0, part = 0; d < d1; d += kDepth, part ^= 1) {
+        // this stage has arrived, and every wave has read the other half
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
-        if (d + (S::kStages - 2) * kDepth < d1) wait_loads<kLoads * (S::kStages - 2)>();
-        else wait_loads<0>();
+        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        const int ahead = part == 0 ? S::kStages - 1 : part - 1;
-        if (d + (S::kStages - 1) * kDepth < d1) load(d + (S::kStages - 1) * kDepth, ahead);
+        if (d + kDepth < d1) load(d + kDepth, part ^ 1);
         const half8* stage = stages + part * kStage;
-        part = part + 1 == S::kStages ? 0 : part + 1;
 #pragma unroll
         for (int kk = 0; kk < kPieces / 4; ++kk) {
+            if (kDepth > 64 && d + kk * 32 >= d1) break;
             half8 l[LP][MI], r[RP][NI];
 #pragma unroll
             for (int p = 0; p < LP; ++p)
@@ -417,11 +413,11 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
 }
 
 // C = L R', a workgroup a tile.
-template <Product KIND, int TILE, int LP, int RP, typename T>
-__global__ __launch_bounds__(kThreadsOf<TILE>, 1) void product_kernel(Operands o, Output<T> out) {
+template <Product KIND, Tile TILE, int LP, int RP, typename T>
+__global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
     constexpr bool kSymmetric = is_symmetric(KIND);
-    constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16;
+    constexpr int MI = S::kSide / S::kRows / 16, NI = S::kSide / S::kCols / 16;
     extern __shared__ half8 stages[];
     // one XCD's workgroups take neighbouring tiles: all rows of some columns
     const int tiles = kSymmetric ? o.rows * (o.rows + 1) / 2 : o.rows * o.cols;
@@ -431,14 +427,14 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void product_kernel(Operands o
     int ti = tile % o.rows, tj = tile / o.rows;
     if constexpr (kSymmetric) triangle(tile, ti, tj);
     float4v acc[MI][NI] = {};
-    multiply<TILE, LP, RP>(o, b, ti * TILE, tj * TILE, 0, o.depth, stages, acc);
+    multiply<TILE, LP, RP>(o, b, ti * S::kSide, tj * S::kSide, 0, o.depth, stages, acc);
     Coefficients k = o.k;
     if (KIND == Product::kPolynomial && o.first) k = o.first[b];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int i = ti * TILE + wave / S::kCols * (MI * 16) + lane % 16;
-    const int j = tj * TILE + wave % S::kCols * (NI * 16) + lane / 16 * 4;
+    const int i = ti * S::kSide + wave / S::kCols * (MI * 16) + lane % 16;
+    const int j = tj * S::kSide + wave % S::kCols * (NI * 16) + lane / 16 * 4;
     static_assert(KIND == Product::kLast ||
-                      S::kRows * S::kCols * kTurn<MI> <= S::kStages * (LP + RP) * TILE * S::kDepth,
+                      S::kRows * S::kCols * kTurn<MI> <= 2 * (LP + RP) * S::kSide * S::kDepth,
                   "the waves' turns fit into the stages");
     if constexpr (KIND != Product::kLast) __syncthreads();  // every wave has read the last stage
     f16* turn = reinterpret_cast<f16*>(stages) + wave * kTurn<MI>;
@@ -458,8 +454,8 @@ constexpr int kMostWorkers = 256;
 
 struct Shares {
     float* parts;
-    int stages;   // of all tiles
-    int depth;    // stages of a tile
+    int stages;   // of 64 values of the summed index, of all tiles
+    int depth;    // those of a tile
     int workers;  // as many as there are stages, or fewer
     __device__ __forceinline__ int begin(int w) const {
         return (int)((uint64_t)(uint32_t)w * (uint32_t)stages / (uint32_t)workers);
@@ -473,10 +469,10 @@ struct Shares {
     }
 };
 
-template <int TILE, int LP, int RP>
-__global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Operands o, Shares s) {
+template <Tile TILE, int LP, int RP>
+__global__ __launch_bounds__(kThreadsOf<TILE>) void shared_product_kernel(Operands o, Shares s) {
     using S = Shape<TILE>;
-    constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
+    constexpr int MI = S::kSide / S::kRows / 16, NI = S::kSide / S::kCols / 16, kThreads = kThreadsOf<TILE>;
     extern __shared__ half8 stages[];
     const int tiles = o.rows * (o.rows + 1) / 2;
     const int w = xcd_contiguous(blockIdx.x, s.workers);
@@ -487,9 +483,9 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Ope
         int ti, tj;
         triangle(t % tiles, ti, tj);
         float4v acc[MI][NI] = {};
-        multiply<TILE, LP, RP>(o, t / tiles, ti * TILE, tj * TILE, (at - t * s.depth) * S::kDepth,
-                               (stop - t * s.depth) * S::kDepth, stages, acc);
-        float* part = s.parts + (int64_t)(t + w) * (TILE * TILE) + threadIdx.x * 4;
+        multiply<TILE, LP, RP>(o, t / tiles, ti * S::kSide, tj * S::kSide, (at - t * s.depth) * 64,
+                               (stop - t * s.depth) * 64, stages, acc);
+        float* part = s.parts + (int64_t)(t + w) * (S::kSide * S::kSide) + threadIdx.x * 4;
 #pragma unroll
         for (int x = 0; x < MI; ++x)
 #pragma unroll
@@ -501,10 +497,10 @@ __global__ __launch_bounds__(kThreadsOf<TILE>, 1) void shared_product_kernel(Ope
 }
 
 // The parts of a tile, added in the workers' order: a workgroup takes 16 columns of each wave's part of C.
-template <Product KIND, int TILE>
+template <Product KIND, Tile TILE>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands o, Shares s) {
     using S = Shape<TILE>;
-    constexpr int MI = TILE / S::kRows / 16, NI = TILE / S::kCols / 16, kThreads = kThreadsOf<TILE>;
+    constexpr int MI = S::kSide / S::kRows / 16, NI = S::kSide / S::kCols / 16, kThreads = kThreadsOf<TILE>;
     __shared__ half8 turns[kThreads / 64 * kTurn<MI> / 8];
     const int tiles = o.rows * (o.rows + 1) / 2;
     const int t = blockIdx.x / NI, y = blockIdx.x % NI;
@@ -512,7 +508,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
     int ti, tj;
     triangle(t % tiles, ti, tj);
     const int w0 = s.holder(t * s.depth), w1 = s.holder((t + 1) * s.depth - 1);
-    const float* part = s.parts + (int64_t)t * (TILE * TILE) + y * (MI * kThreads * 4) + threadIdx.x * 4;
+    const float* part = s.parts + (int64_t)t * (S::kSide * S::kSide) + y * (MI * kThreads * 4) + threadIdx.x * 4;
     float4v sum[MI] = {};
     constexpr int kAtOnce = 3;  // workers whose parts are on their way together
     for (int w = w0; w <= w1; w += kAtOnce) {
@@ -522,7 +518,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
             const int from = w + q <= w1 ? w + q : w1;
 #pragma unroll
             for (int x = 0; x < MI; ++x)
-                v[q][x] = *reinterpret_cast<const float4v*>(part + (int64_t)from * (TILE * TILE) + x * (kThreads * 4));
+                v[q][x] = *reinterpret_cast<const float4v*>(part + (int64_t)from * (S::kSide * S::kSide) + x * (kThreads * 4));
         }
 #pragma unroll
         for (int q = 0; q < kAtOnce; ++q)
@@ -534,8 +530,8 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
     Coefficients k = o.k;
     if (KIND == Product::kPolynomial && o.first) k = o.first[b];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    finish<KIND, MI>(o, Output<f16>{}, b, k, ti * TILE + wave / S::kCols * (MI * 16) + lane % 16,
-                     tj * TILE + wave % S::kCols * (NI * 16) + y * 16 + lane / 16 * 4, ti != tj, sum,
+    finish<KIND, MI>(o, Output<f16>{}, b, k, ti * S::kSide + wave / S::kCols * (MI * 16) + lane % 16,
+                     tj * S::kSide + wave % S::kCols * (NI * 16) + y * 16 + lane / 16 * 4, ti != tj, sum,
                      reinterpret_cast<f16*>(turns) + wave * kTurn<MI>);
 }
 
@@ -840,8 +836,8 @@ int64_t padded(int64_t side, int tile) { return (side + tile - 1) / tile * tile;
 // Over how many workgroups a symmetric product's stages are shared out; 0: a workgroup takes a tile. It leaves
 // no CU idle, and costs a launch and the parts' way through memory, 6 to 14 us. With tiles of 128 the
 // idle CUs of the last round decide: a round takes 30 us for 1000 values of the summed index. 136 tiles from
-// 2048 measured 60 us as they are and 53 shared out, from 8192 200 and 130. Tiles of 64 take 0.56 us a stage
-// of 64; a worker has two stages or more.
+// 2048 measured 60 us as they are and 53 shared out, from 8192 200 and 130. Tiles of 64 take 0.4 us for 64
+// values; a worker has 128 or more.
 int workers_of(int tile, int64_t tiles, int64_t depth) {
     const int64_t all = tiles * (depth / 64);
     if (all > INT32_MAX / 2) return 0;
@@ -849,7 +845,7 @@ int workers_of(int tile, int64_t tiles, int64_t depth) {
     if (tile == 128) return all >= kMostWorkers && (std::ceil(rounds) - rounds) * depth >= 512.0 ? kMostWorkers : 0;
     if (tile != 64 || all < 4) return 0;
     const int64_t w = all / 2 < kMostWorkers ? all / 2 : kMostWorkers;
-    return 0.56 * all / w + 6.0 < 0.56 * std::ceil(rounds) * (depth / 64) ? (int)w : 0;
+    return 0.4 * all / w + 6.0 < 0.4 * std::ceil(rounds) * (depth / 64) ? (int)w : 0;
 }
 
 // How many products of each sort a call takes.
@@ -983,19 +979,19 @@ bool allow_local(K kernel, size_t local) {
                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)local) == hipSuccess;
 }
 
-template <Product KIND, int TILE, int LP, int RP, typename T>
+template <Product KIND, Tile TILE, int LP, int RP, typename T>
 int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float* parts, hipStream_t stream) {
     using S = Shape<TILE>;
     constexpr bool kSymmetric = is_symmetric(KIND);
-    constexpr size_t local = (size_t)S::kStages * (LP + RP) * TILE * S::kDepth * sizeof(f16);
+    constexpr size_t local = (size_t)2 * (LP + RP) * S::kSide * S::kDepth * sizeof(f16);
     const int64_t tiles = batch * (kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols);
     if constexpr (kSymmetric) {
-        if (const int workers = workers_of(TILE, tiles, o.depth)) {
+        if (const int workers = workers_of(S::kSide, tiles, o.depth)) {
             const auto kernel = shared_product_kernel<TILE, LP, RP>;
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
-            const Shares s{parts, (int)tiles * (o.depth / S::kDepth), o.depth / S::kDepth, workers};
+            const Shares s{parts, (int)tiles * (o.depth / 64), o.depth / 64, workers};
             kernel<<<workers, kThreadsOf<TILE>, local, stream>>>(o, s);
-            join_product_kernel<KIND, TILE><<<(unsigned)(tiles * (TILE / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
+            join_product_kernel<KIND, TILE><<<(unsigned)(tiles * (S::kSide / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
             return launch_status();
         }
     }
@@ -1015,33 +1011,33 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
             hipStream_t stream) {
     o.rows = o.rows / tile;
     o.cols = o.cols / tile;
-#define LAUNCH(TILE, LP, RP) \
-    if (tile == TILE) return launch_product<KIND, TILE, LP, RP>(o, out, batch, parts, stream)
+    const bool few = batch * (is_symmetric(KIND) ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols) <= 256;
+#define LAUNCH(TILE, LP, RP) return launch_product<KIND, Tile::TILE, LP, RP>(o, out, batch, parts, stream)
+#define LAUNCH_SMALLER(LP, RP)              \
+    if (tile == 128) LAUNCH(k128, LP, RP);  \
+    if (few) LAUNCH(k64Few, LP, RP);        \
+    LAUNCH(k64, LP, RP)
     if constexpr (KIND == Product::kLast && sizeof(T) == 2) {
         if (depth == Depth::kUpper) {
-            LAUNCH(256, 1, 1);
-            LAUNCH(128, 1, 1);
-            LAUNCH(64, 1, 1);
+            if (tile == 256) LAUNCH(k256, 1, 1);
+            LAUNCH_SMALLER(1, 1);
         }
     }
     if constexpr (KIND == Product::kGram) {
         if (depth == Depth::kExact) {
-            LAUNCH(128, 1, 1);
-            LAUNCH(64, 1, 1);
+            LAUNCH_SMALLER(1, 1);
         }
     }
     if constexpr (KIND == Product::kUpdate || KIND == Product::kLast) {
         if (depth == Depth::kExact) {
-            LAUNCH(256, 2, 1);
-            LAUNCH(128, 2, 1);
-            LAUNCH(64, 2, 1);
+            if (tile == 256) LAUNCH(k256, 2, 1);
+            LAUNCH_SMALLER(2, 1);
         }
-        LAUNCH(256, 2, 2);
+        if (tile == 256) LAUNCH(k256, 2, 2);
     }
-    LAUNCH(128, 2, 2);
-    LAUNCH(64, 2, 2);
+    LAUNCH_SMALLER(2, 2);
+#undef LAUNCH_SMALLER
 #undef LAUNCH
-    return TRIVANCE_EINVAL;
 }
 
 template <typename T>
