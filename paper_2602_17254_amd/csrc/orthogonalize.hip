@@ -628,40 +628,55 @@ struct SmallLocal {
           p{local + 4 * small_x(n) + 2 * kSmallA, local + 4 * small_x(n) + 3 * kSmallA, 0} {}
 };
 
-// Its columns of G, from j0 on, in registers; G's contiguous index runs over the lanes.
+// Its columns of G, from j0 on, in registers: vectors as they lie in memory, with X's rows or columns.
 constexpr int kSmallMine = kSmallSide * kSmallLong / kSmallThreads;
 
-__device__ __forceinline__ void small_place(bool tall, int q, int& i, int& j) {
-    i = tall ? threadIdx.x % kSmallSide : q * (kSmallThreads / kSmallLong) + threadIdx.x / kSmallLong;
-    j = tall ? q * (kSmallThreads / kSmallSide) + threadIdx.x / kSmallSide : threadIdx.x % kSmallLong;
-}
-
 template <typename T>
-__device__ __forceinline__ void small_fetch(const Input<T>& in, int64_t b, int j0, float (&v)[kSmallMine]) {
+__device__ __forceinline__ void small_fetch(const Input<T>& in, int64_t b, int j0, float (&v)[kSmallMine / kVec<T>][kVec<T>]) {
+    constexpr int V = kVec<T>;
+    const bool tall = in.sj != 1;
     const T* g = in.x + b * in.batch;
 #pragma unroll
-    for (int q = 0; q < kSmallMine; ++q) {
-        int i, j;
-        small_place(in.sj != 1, q, i, j);
-        v[q] = i < in.m && j0 + j < in.n ? (float)g[i * in.si + (j0 + j) * in.sj] : 0.0f;
+    for (int q = 0; q < kSmallMine / V; ++q) {
+        const int e = q * kSmallThreads + threadIdx.x;
+        const int r = tall ? e / (kSmallSide / V) : e / (kSmallLong / V);
+        const int c = tall ? e % (kSmallSide / V) * V : e % (kSmallLong / V) * V;
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[q][k] = 0.0f;
+        if (tall && j0 + r < in.n) load_row<T>(g + (int64_t)(j0 + r) * in.sj, c, in.m, 0.0f, v[q]);
+        if (!tall && r < in.m) load_row<T>(g + (int64_t)r * in.si, j0 + c, in.n, 0.0f, v[q]);
     }
 }
 
+// Scaled and split into X, both ways round.
+template <int V>
 __device__ __forceinline__ void small_split(const SmallLocal& m, bool tall, int n, int exponent,
-                                            const float (&v)[kSmallMine]) {
+                                            const float (&v)[kSmallMine / V][V]) {
+    typedef f16 halfv __attribute__((ext_vector_type(V)));
+    const LocalPlanes straight = tall ? m.xt : m.x, turned = tall ? m.x : m.xt;
 #pragma unroll
-    for (int q = 0; q < kSmallMine; ++q) {
-        int i, j;
-        small_place(tall, q, i, j);
-        if (j >= n) continue;
-        f16 hi, lo;
-        split(ldexpf(v[q], exponent), hi, lo);
-        const int to = (j / 64 * kSmallA + i * 8 + permuted(i, j % 64 / 8)) * 8 + j % 8;
-        const int too = (j * 8 + permuted(j, i / 8)) * 8 + i % 8;
-        reinterpret_cast<f16*>(m.x.hi)[to] = hi;
-        reinterpret_cast<f16*>(m.x.lo)[to] = lo;
-        reinterpret_cast<f16*>(m.xt.hi)[too] = hi;
-        reinterpret_cast<f16*>(m.xt.lo)[too] = lo;
+    for (int q = 0; q < kSmallMine / V; ++q) {
+        const int e = q * kSmallThreads + threadIdx.x;
+        const int r = tall ? e / (kSmallSide / V) : e / (kSmallLong / V);
+        const int c = tall ? e % (kSmallSide / V) * V : e % (kSmallLong / V) * V;
+        if ((tall ? r : c) >= n) continue;
+        halfv h, w;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            f16 hi, lo;
+            split(ldexpf(v[q][k], exponent), hi, lo);
+            h[k] = hi;
+            w[k] = lo;
+        }
+        const int to = (c / 64 * straight.panel + r * 8 + permuted(r, c % 64 / 8)) * 8 + c % 8;
+        *reinterpret_cast<halfv*>(reinterpret_cast<f16*>(straight.hi) + to) = h;
+        *reinterpret_cast<halfv*>(reinterpret_cast<f16*>(straight.lo) + to) = w;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int too = (r / 64 * turned.panel + (c + k) * 8 + permuted(c + k, r % 64 / 8)) * 8 + r % 8;
+            reinterpret_cast<f16*>(turned.hi)[too] = h[k];
+            reinterpret_cast<f16*>(turned.lo)[too] = w[k];
+        }
     }
 }
 
@@ -709,10 +724,18 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
                 continue;
             }
             const int i = y * 16 + at.row, j = j0 + col + at.column;
+            if (i < out.m) {
+                T* to = out.x + b * out.batch + i * out.si + j * out.sj;
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (i < out.m && j + c < out.n)
-                    out.x[b * out.batch + i * out.si + (j + c) * out.sj] = (T)(w[c] * (scale / kScale));
+                for (int c = 0; c < 4; ++c) w[c] *= scale / kScale;
+                if (out.sj == 1) {
+                    store_row<T, 4>(to, 0, out.n - j, w);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (j + c < out.n) to[c * out.sj] = (T)w[c];
+                }
+            }
         }
     }
     __syncthreads();
@@ -728,11 +751,13 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
     static_assert(kTiles * kTiles == kWaves && kSmallLong / 16 == kWaves, "a tile of A, a column of X a wave");
     const SmallLocal m(local, n);
     const LaneOffsets at(lane);
-    float v[kSmallMine];
+    float v[kSmallMine / kVec<T>][kVec<T>];
     small_fetch(in, blockIdx.x, 0, v);
     double sum = 0.0;
 #pragma unroll
-    for (int q = 0; q < kSmallMine; ++q) sum += (double)v[q] * (double)v[q];
+    for (int q = 0; q < kSmallMine / kVec<T>; ++q)
+#pragma unroll
+        for (int c = 0; c < kVec<T>; ++c) sum += (double)v[q][c] * (double)v[q][c];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     double* sums = reinterpret_cast<double*>(m.p.hi);
@@ -744,7 +769,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
     int e;
     Coefficients first;
     scale_of(sum, s.k[0], eps, e, first);
-    small_split(m, in.sj != 1, n, kScaleExp - e, v);
+    small_split<kVec<T>>(m, in.sj != 1, n, kScaleExp - e, v);
     __syncthreads();
     const int ti = wave / kTiles * 16, tj = wave % kTiles * 16;  // the wave's tile of A and P
     for (int step = 0; step < s.steps; ++step) {
@@ -778,7 +803,7 @@ __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in,
     const int64_t b = blockIdx.y, strip = b * s.strips + blockIdx.x;
     const SmallLocal m(local, kSmallLong);
     const LaneOffsets at(lane);
-    float v[kSmallMine];
+    float v[kSmallMine / kVec<T>][kVec<T>];
     small_fetch(in, b, blockIdx.x * kSmallLong, v);
     double sum = 0.0;
     for (int i = lane; i < nparts; i += 64) sum += norm[b * kNormParts + i];
@@ -788,7 +813,7 @@ __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in,
     Coefficients mine;
     scale_of(sum, k, eps, e, mine);
     if (blockIdx.x == 0 && threadIdx.x == 0) first[b] = mine;
-    small_split(m, in.sj != 1, kSmallLong, kScaleExp - e, v);
+    small_split<kVec<T>>(m, in.sj != 1, kSmallLong, kScaleExp - e, v);
     __syncthreads();
     const float4v a = small_gram(m, kSmallLong, wave / 4 * 16, wave % 4 * 16, at);
     reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
