@@ -9,10 +9,11 @@
 // a = 3.4445), and so does any rounding noise that falls into it: with bf16 operands five steps end 1
 // to 30% off, with fp16 0.1 to 3%, by the spectrum. Every matrix is kept as two fp16 numbers hi + lo of
 // 22 bits together, and a product is three MFMA products hi hi + hi lo + lo hi in fp32 sums: fp32
-// accuracy for every spectrum at a third of the fp16 rate, five times the rate of fp32 MFMA. Values are
-// held times 2^12: all entries are at most 15 (checked for the coefficients) and the spacing of lo
-// is 2^-36. G enters scaled by a power of two, exactly where it has 16 bits; the rest of the norm goes into
-// the first step's coefficients.
+// accuracy for every spectrum at a third of the fp16 rate, five times the rate of fp32 MFMA. Small
+// entries, which lo holds with a fixed spacing, decide how near that comes: X, A and P are each held times
+// the largest power of two that their range allows, 2^15, 2^15 and 2^13 for the usual coefficients (with
+// 2^12 for all, 2176 x 1600 fp32 was 5.0e-6 off where fp32 products are 3.2e-6). G enters scaled by a power
+// of two, exactly where it has 16 bits; the rest of the norm goes into the first step's coefficients.
 //
 // What bounds it: the MFMA rate, for matrices of some hundred rows and more.
 // Layout. X is kept both ways round, so that both operands of every product have their summed index
@@ -29,8 +30,6 @@
 namespace trivance {
 namespace {
 
-constexpr float kScale = 4096.0f;  // 2^12, of every stored matrix
-constexpr int kScaleExp = 12;
 constexpr int kMaxSteps = 64;
 constexpr int64_t kMaxSide = 1 << 16;
 constexpr int kNormParts = 1024;  // most partial sums of a matrix's norm
@@ -46,6 +45,8 @@ struct Planes {
     int ld;
 };
 
+// Of a step, times the scales of what they multiply and make: P as stored is
+// a + b (A as stored) + c (the sums of products of A as stored).
 struct Coefficients {
     float a, b, c;
 };
@@ -89,11 +90,11 @@ __global__ __launch_bounds__(256) void norm_parts_kernel(Input<T> in, double* pa
         parts[blockIdx.y * kNormParts + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// The power of two 2^e below the norm, and the first step's coefficients, which hold what is left of it:
+// The power of two 2^e above the norm, and the first step's coefficients, which hold what is left of it:
 // zeros for a zero matrix, not a number where the norm is none.
 __device__ __forceinline__ void scale_of(double squares, Coefficients c, float eps, int& e, Coefficients& first) {
     const double norm = sqrt(squares);
-    e = norm > 0.0 && norm < __builtin_inf() ? ilogb(norm) : 0;
+    e = norm > 0.0 && norm < __builtin_inf() ? ilogb(norm) + 1 : 0;
     const double alpha = norm == 0.0 ? 0.0
                          : norm < __builtin_inf() ? ldexp(1.0, e) / (norm + eps)
                                                   : __builtin_nan("");
@@ -101,11 +102,11 @@ __device__ __forceinline__ void scale_of(double squares, Coefficients c, float e
     first = {(float)(c.a * alpha), (float)(c.b * cube), (float)(c.c * (cube * alpha * alpha))};
 }
 
-// X both ways round, scaled by 2^12 over the power of two below the norm and padded with zeros, and the
+// X both ways round, scaled by 2^scale over the power of two above the norm and padded with zeros, and the
 // first step's coefficients. A workgroup takes 64 x 64 values, read as they lie in memory.
 template <typename T>
 __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* parts, int nparts,
-                                                    Planes x, Planes xt, Coefficients c, float eps,
+                                                    Planes x, Planes xt, int scale, Coefficients c, float eps,
                                                     Coefficients* first) {
     constexpr int V = kVec<T>, kRow = 64 + 8;
     __shared__ half8 tiles[2][64 * kRow / 8];
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
         float v[V] = {};
         if (r0 + r < rows) load_row<T>(g + (r0 + r) * stride, c0 + k0, cols, 0.0f, v);
 #pragma unroll
-        for (int k = 0; k < V; ++k) split(ldexpf(v[k], kScaleExp - e), hi[r * kRow + k0 + k], lo[r * kRow + k0 + k]);
+        for (int k = 0; k < V; ++k) split(ldexpf(v[k], scale - e), hi[r * kRow + k0 + k], lo[r * kRow + k0 + k]);
     }
     __syncthreads();
     const Planes straight = tall ? xt : x, turned = tall ? x : xt;
@@ -226,7 +227,7 @@ struct Operands {
     int depth;       // the summed index, a multiple of 64
     int rows, cols;  // tiles of C
     Planes c, ct;    // C and its transpose
-    float factor;    // of the sums, which carry the scales of both operands
+    float factor;    // of the sums, from the scales of both operands to that of C
     Planes a;        // of the polynomial
     Coefficients k;
     const Coefficients* first;  // in place of k, for each matrix
@@ -341,12 +342,11 @@ __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, 
         const int row = i + x * 16;
         float v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = sum[x][q] * o.factor;
-        if constexpr (KIND == Product::kPolynomial) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                v[q] = k.b * ((float)ah[x][q] + (float)aw[x][q]) + k.c * v[q] +
-                       (row == j + q ? k.a * kScale : 0.0f);
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (KIND == Product::kPolynomial)
+                v[q] = k.b * ((float)ah[x][q] + (float)aw[x][q]) + k.c * sum[x][q] + (row == j + q ? k.a : 0.0f);
+            else
+                v[q] = sum[x][q] * o.factor;
         }
         if constexpr (KIND == Product::kLast) {
             T* to = out.x + b * out.batch + row * out.si + j * out.sj;
@@ -546,6 +546,12 @@ struct SmallSteps {
     Coefficients k[kMaxSteps];
 };
 
+// From sums of products to what is stored, and to the caller's values.
+struct SmallFactors {
+    int x;  // the exponent of X's scale
+    float gram, update, last;
+};
+
 // Matrices in local memory lie in panels of 64 columns: 8 pieces a row, permuted as a stage's.
 struct LocalPlanes {
     half8 *hi, *lo;
@@ -688,19 +694,18 @@ __device__ __forceinline__ float4v small_gram(const SmallLocal& m, int n, int ti
 }
 
 // From the wave's tile of A to its tile of P in local memory, for everyone.
-__device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a, Coefficients k, int ti, int tj,
-                                                 const LaneOffsets& at) {
+__device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a, Coefficients k, float factor, int ti,
+                                                 int tj, const LaneOffsets& at) {
     float gram[4], poly[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) gram[c] = a[c] * (1.0f / kScale);
+    for (int c = 0; c < 4; ++c) gram[c] = a[c] * factor;
     local_store(m.a, nullptr, ti, tj, at, gram);
     __syncthreads();
     float4v acc[1] = {};
     local_product<1>(m.a, ti, m.a, tj, 0, at, acc);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        poly[c] = k.b * gram[c] + k.c * (acc[0][c] * (1.0f / kScale)) +
-                  (ti + at.row == tj + at.column + c ? k.a * kScale : 0.0f);
+        poly[c] = k.b * gram[c] + k.c * acc[0][c] + (ti + at.row == tj + at.column + c ? k.a : 0.0f);
     local_store(m.p, nullptr, ti, tj, at, poly);
     __syncthreads();
 }
@@ -708,7 +713,7 @@ __device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a,
 // X <- P X in local memory, or with `last` to the caller, whose columns begin at j0.
 template <typename T>
 __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col, const LaneOffsets& at, bool last,
-                                             const Output<T>& out, int64_t b, int j0, float scale) {
+                                             const Output<T>& out, int64_t b, int j0, SmallFactors f) {
     constexpr int kTiles = kSmallSide / 16;
     float4v next[kTiles] = {};
     if (col < n) local_product<kTiles>(m.p, 0, m.xt, col, 0, at, next);
@@ -718,7 +723,7 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
         for (int y = 0; y < kTiles; ++y) {
             float w[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) w[c] = next[y][c] * (1.0f / kScale);
+            for (int c = 0; c < 4; ++c) w[c] = next[y][c] * (last ? f.last : f.update);
             if (!last) {
                 local_store(m.x, &m.xt, y * 16, col, at, w);
                 continue;
@@ -726,8 +731,6 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
             const int i = y * 16 + at.row, j = j0 + col + at.column;
             if (i < out.m) {
                 T* to = out.x + b * out.batch + i * out.si + j * out.sj;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] *= scale / kScale;
                 if (out.sj == 1) {
                     store_row<T, 4>(to, 0, out.n - j, w);
                 } else {
@@ -744,7 +747,7 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
 // n: X's columns padded to whole panels.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Output<T> out, int n, SmallSteps s,
-                                                              float scale, float eps) {
+                                                              SmallFactors f, float eps) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     constexpr int kWaves = kSmallThreads / 64, kTiles = kSmallSide / 16;
@@ -769,12 +772,12 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
     int e;
     Coefficients first;
     scale_of(sum, s.k[0], eps, e, first);
-    small_split<kVec<T>>(m, in.sj != 1, n, kScaleExp - e, v);
+    small_split<kVec<T>>(m, in.sj != 1, n, f.x - e, v);
     __syncthreads();
     const int ti = wave / kTiles * 16, tj = wave % kTiles * 16;  // the wave's tile of A and P
     for (int step = 0; step < s.steps; ++step) {
-        small_polynomial(m, small_gram(m, n, ti, tj, at), step == 0 ? first : s.k[step], ti, tj, at);
-        small_update(m, n, wave * 16, at, step + 1 == s.steps, out, blockIdx.x, 0, scale);
+        small_polynomial(m, small_gram(m, n, ti, tj, at), step == 0 ? first : s.k[step], f.gram, ti, tj, at);
+        small_update(m, n, wave * 16, at, step + 1 == s.steps, out, blockIdx.x, 0, f);
     }
 }
 
@@ -796,7 +799,7 @@ constexpr int kStripPlanes = 4 * small_x(kSmallLong);  // pieces
 
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in, const double* norm, int nparts,
-                                                                    Coefficients k, float eps, Strips s,
+                                                                    int scale, Coefficients k, float eps, Strips s,
                                                                     Coefficients* first) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -813,7 +816,7 @@ __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in,
     Coefficients mine;
     scale_of(sum, k, eps, e, mine);
     if (blockIdx.x == 0 && threadIdx.x == 0) first[b] = mine;
-    small_split<kVec<T>>(m, in.sj != 1, kSmallLong, kScaleExp - e, v);
+    small_split<kVec<T>>(m, in.sj != 1, kSmallLong, scale - e, v);
     __syncthreads();
     const float4v a = small_gram(m, kSmallLong, wave / 4 * 16, wave % 4 * 16, at);
     reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
@@ -825,7 +828,7 @@ __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in,
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out, Strips s, Coefficients k,
                                                                    const Coefficients* first, bool last,
-                                                                   float scale) {
+                                                                   SmallFactors f) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t b = blockIdx.y, strip = b * s.strips + blockIdx.x;
@@ -840,8 +843,8 @@ __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out
     for (int q = 0; q < s.strips; ++q) a += parts[q * kSmallThreads];
     if (first) k = first[b];
     const int ti = wave / 4 * 16, tj = wave % 4 * 16;
-    small_polynomial(m, a, k, ti, tj, at);
-    small_update(m, kSmallLong, wave * 16, at, last, out, b, blockIdx.x * kSmallLong, scale);
+    small_polynomial(m, a, k, f.gram, ti, tj, at);
+    small_update(m, kSmallLong, wave * 16, at, last, out, b, blockIdx.x * kSmallLong, f);
     if (last) return;
     a = small_gram(m, kSmallLong, ti, tj, at);
     reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
@@ -1065,17 +1068,56 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
 #undef LAUNCH
 }
 
+// The ranges that the coefficients give: the largest singular value of X in any step, from values in [0, 1] on,
+// and the largest factor of one, and the powers of two by which X, A, P, and products of two and three factors can
+// be held in fp16. The first step's factors may be doubled (what is left of the norm).
+struct Ranges {
+    bool ok;
+    int x, a, p[3];  // exponents
+};
+
+Ranges ranges_of(const float* k, int steps) {
+    constexpr double kMargin = 1.01;  // between the samples, and the rounding of the products
+    double most = 1.0, all = 1.0, factor = 0.0;
+    for (int s = 0; s < steps; ++s) {
+        const double a = k[3 * s], b = k[3 * s + 1], c = k[3 * s + 2];
+        double next = 0.0;
+        constexpr int kSamples = 256;
+        for (int i = 0; i <= kSamples; ++i) {
+            const double v = most * i / kSamples, p = std::fabs(a + v * v * (b + v * v * c));
+            if (!(p <= 15.0)) return {false, 0, 0, {}};
+            factor = std::fmax(factor, s == 0 ? 2.0 * p : p);
+            next = std::fmax(next, p * v);
+        }
+        most = next * kMargin;
+        if (!(most <= 3.9)) return {false, 0, 0, {}};
+        all = std::fmax(all, most);
+    }
+    factor = std::fmax(factor, 1.0) * kMargin;
+    const auto exponent = [](double bound) { return std::ilogb(60000.0 / bound); };
+    return {true, exponent(all), exponent(all * all),
+            {exponent(factor), exponent(factor * factor), exponent(factor * factor * factor)}};
+}
+
+float power(int exponent) { return std::ldexp(1.0f, exponent); }
+
 template <typename T>
-int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, float scale, float eps,
-        const Layout& w, int dtype, void* workspace, hipStream_t stream) {
+int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, const Ranges& range, float scale,
+        float eps, const Layout& w, int dtype, void* workspace, hipStream_t stream) {
+    const auto coefficients = [&](int s) {
+        return Coefficients{k[3 * s] * power(range.p[0]), k[3 * s + 1] * power(range.p[0] - range.a),
+                            k[3 * s + 2] * power(range.p[0] - 2 * range.a)};
+    };
+    const float gram = power(range.a - 2 * range.x);
+    const SmallFactors factors{range.x, gram, power(-range.p[0]), scale * power(-range.p[0] - range.x)};
     if (w.small) {
         SmallSteps s;
         s.steps = steps;
-        for (int i = 0; i < steps; ++i) s.k[i] = {k[3 * i], k[3 * i + 1], k[3 * i + 2]};
+        for (int i = 0; i < steps; ++i) s.k[i] = coefficients(i);
         const int n = (int)padded(w.n, 64);
         const size_t local = sizeof(half8) * (4 * small_x(n) + 4 * kSmallA);
         if (!allow_local(&small_kernel<T>, local)) return TRIVANCE_EHIP;
-        small_kernel<T><<<(unsigned)batch, kSmallThreads, local, stream>>>(in, out, n, s, scale, eps);
+        small_kernel<T><<<(unsigned)batch, kSmallThreads, local, stream>>>(in, out, n, s, factors, eps);
         return launch_status();
     }
     char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
@@ -1085,7 +1127,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
     const int rows = in.sj != 1 ? in.n : in.m;
     const int64_t pieces = (int64_t)rows * (((rows == in.n ? in.m : in.n) + 256 * kVec<T> - 1) / (256 * kVec<T>));
     const int nparts = (int)(pieces < kNormParts ? pieces : kNormParts);
-    const Coefficients k0{k[0], k[1], k[2]};
+    const Coefficients k0 = coefficients(0);
     norm_parts_kernel<T><<<dim3(nparts, nb), 256, 0, stream>>>(in, parts);
     if (w.strips) {
         const size_t local = sizeof(half8) * (kStripPlanes + 4 * kSmallA);
@@ -1094,14 +1136,13 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
         Strips s{reinterpret_cast<float*>(base + w.strip_parts[0]), reinterpret_cast<float*>(base + w.strip_parts[1]),
                  reinterpret_cast<half8*>(base + w.strip_planes), w.strips};
         const dim3 grid(w.strips, nb);
-        strip_start_kernel<T><<<grid, kSmallThreads, local, stream>>>(in, parts, nparts, k0, eps, s, first);
+        strip_start_kernel<T><<<grid, kSmallThreads, local, stream>>>(in, parts, nparts, range.x, k0, eps, s, first);
         for (int i = 0; i < steps; ++i) {
             float* read = s.made;
             s.made = s.parts;
             s.parts = read;
             strip_step_kernel<T><<<grid, kSmallThreads, local, stream>>>(
-                out, s, Coefficients{k[3 * i], k[3 * i + 1], k[3 * i + 2]}, i == 0 ? first : nullptr,
-                i + 1 == steps, scale);
+                out, s, coefficients(i), i == 0 ? first : nullptr, i + 1 == steps, factors);
         }
         return launch_status();
     }
@@ -1120,7 +1161,8 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
         q[i] = planes(w.square[2 + i], m, m);
     }
     const Planes next = planes(w.square[4], m, m), pp = planes(w.square[5], m, m);
-    split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(in, parts, nparts, x[0], xt[0], k0, eps, first);
+    split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(in, parts, nparts, x[0], xt[0], range.x, k0, eps,
+                                                                    first);
     int rc = launch_status();
     const Output<f16> none{};
     const auto square = [&](const Planes& l, const Planes& r, const Planes& c, float factor) {
@@ -1131,59 +1173,38 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, fl
     for (int s = 0; s < steps && !rc;) {
         const int group = group_of(k, s, steps, dtype, w.m, w.n);
         const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : Depth::kBoth;
-        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a[0], a[0], 1.0f / kScale, a[0], {}, nullptr},
+        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a[0], a[0], gram, a[0], {}, nullptr},
                                      none, batch, tiles.symmetric, depth, shares, stream);
         int at = 0, qt = 0;
-        float qs = kScale;  // Q's scale: factors of up to 15 a step leave it less
         for (int g = 0; g < group && !rc; ++g) {
-            const Coefficients c{k[3 * (s + g)], k[3 * (s + g) + 1], k[3 * (s + g) + 2]};
             const Planes p = g == 0 ? q[0] : next;
             rc = product<Product::kPolynomial>(
-                {a[at], a[at], m, m, m, p, p, 1.0f / kScale, a[at], c, s + g == 0 ? first : nullptr}, none, batch,
-                tiles.symmetric, Depth::kBoth, shares, stream);
-            if (g > 0 && !rc) {
-                rc = square(p, q[qt], q[1 - qt], 1.0f / (16.0f * kScale));
+                {a[at], a[at], m, m, m, p, p, 1.0f, a[at], coefficients(s + g), s + g == 0 ? first : nullptr}, none,
+                batch, tiles.symmetric, Depth::kBoth, shares, stream);
+            if (g > 0 && !rc) {  // Q's scale is that of g + 1 factors
+                rc = square(p, q[qt], q[1 - qt], power(range.p[g] - range.p[0] - range.p[g - 1]));
                 qt = 1 - qt;
-                qs /= 16.0f;
             }
-            if (g + 1 < group && !rc) {  // A <- A (P P), with P P at a sixteenth of the scale
-                rc = square(p, p, pp, 1.0f / (16.0f * kScale));
-                if (!rc) rc = square(a[at], pp, a[1 - at], 16.0f / kScale);
+            if (g + 1 < group && !rc) {  // A <- A (P P)
+                rc = square(p, p, pp, power(range.p[1] - 2 * range.p[0]));
+                if (!rc) rc = square(a[at], pp, a[1 - at], power(-range.p[1]));
                 at = 1 - at;
             }
         }
         s += group;
         if (rc) break;
-        Operands update{q[qt], xt[turn], m, m, n, x[1 - turn], xt[1 - turn], 1.0f / qs, a[0], {}, nullptr};
+        Operands update{q[qt], xt[turn], m, m, n, x[1 - turn], xt[1 - turn],
+                        power(-range.p[group - 1]), a[0], {}, nullptr};
         if (s < steps) {
             rc = product<Product::kUpdate>(update, none, batch, tiles.update, depth, shares, stream);
             turn = 1 - turn;
         } else {
-            update.factor *= scale / kScale;
+            update.factor *= scale * power(-range.x);
             rc = product<Product::kLast>(update, out, batch, tiles.update,
                                          dtype == TRIVANCE_BF16 ? Depth::kUpper : depth, shares, stream);
         }
     }
     return rc;
-}
-
-// Whether the stored numbers stay in fp16's range for every singular value in [0, 1]: step by step, the
-// largest singular value stays below 3.9 and P's within 15.
-bool coefficients_ok(const float* k, int steps) {
-    double most = 1.0;  // the largest singular value so far
-    for (int s = 0; s < steps; ++s) {
-        const double a = k[3 * s], b = k[3 * s + 1], c = k[3 * s + 2];
-        double next = 0.0;
-        constexpr int kSamples = 4096;
-        for (int i = 0; i <= kSamples; ++i) {
-            const double v = most * i / kSamples, p = a + v * v * (b + v * v * c);
-            if (!(std::fabs(p) <= 15.0)) return false;
-            if (std::fabs(p * v) > next) next = std::fabs(p * v);
-        }
-        most = next * 1.001;  // between the samples, and the rounding of the products
-        if (!(most <= 3.9)) return false;
-    }
-    return true;
 }
 
 }  // namespace
@@ -1209,7 +1230,9 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
         return TRIVANCE_EINVAL;
     const int64_t need = trivance_orthogonalize_workspace_bytes(batch, rows, cols);
     if (need < 0) return (int)need;
-    if (steps > kMaxSteps || !coefficients_ok(coefficients, steps)) return TRIVANCE_EUNSUPPORTED;
+    if (steps > kMaxSteps) return TRIVANCE_EUNSUPPORTED;
+    const Ranges range = ranges_of(coefficients, steps);
+    if (!range.ok) return TRIVANCE_EUNSUPPORTED;
     if (batch == 0 || rows == 0 || cols == 0) return TRIVANCE_OK;
     if (!x || !out || !rows_fit(batch, rows, cols, x_batch_stride, x_row_stride) ||
         !rows_fit(batch, rows, cols, out_batch_stride, out_row_stride) ||
@@ -1226,7 +1249,7 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
                        tall ? x_row_stride : 1, m, n},
                       {static_cast<T*>(out), out_batch_stride, tall ? 1 : out_row_stride,
                        tall ? out_row_stride : 1, m, n},
-                      batch, steps, coefficients, (float)scale, (float)eps, w, dtype, workspace, s);
+                      batch, steps, coefficients, range, (float)scale, (float)eps, w, dtype, workspace, s);
     };
     return dtype == TRIVANCE_F32 ? go(float{}) : dtype == TRIVANCE_BF16 ? go(bf16{}) : go(f16{});
 }
