@@ -236,10 +236,10 @@ struct Operands {
 // A workgroup's tile: the sums over values d0 .. d1 of the summed index of rows i0 of L and j0 of R; d1 - d0 is a
 // multiple of 64, and a last stage of 128 may be half one. LP and RP: the planes that are not zero. While the
 // waves multiply one stage of the operands the next one is on its way into the other half of local
-// memory, so a stage has one barrier.
-template <Tile TILE, int LP, int RP, int MI, int NI>
+// memory, so a stage has one barrier. The products with a lower plane go into `cross`, which may be `acc`.
+template <Tile TILE, int LP, int RP, bool UPPER, int MI, int NI>
 __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
-                                         half8* stages, float4v (&acc)[MI][NI]) {
+                                         half8* stages, float4v (&acc)[MI][NI], float4v (&cross)[MI][NI]) {
     using S = Shape<TILE>;
     constexpr int kThreads = kThreadsOf<TILE>, kDepth = S::kDepth, kPieces = kDepth / 8;
     constexpr int kPlane = S::kSide * kPieces, kStage = (LP + RP) * kPlane;
@@ -302,10 +302,36 @@ __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, i
 #pragma unroll
                     for (int x = 0; x < MI; ++x)
 #pragma unroll
-                        for (int y = 0; y < NI; ++y)
-                            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[pr][y], l[pl][x],
-                                                                               acc[x][y], 0, 0, 0);
+                        for (int y = 0; y < NI; ++y) {
+                            if (!UPPER && pl + pr == 0) continue;
+                            float4v& sum = pl + pr ? cross[x][y] : acc[x][y];
+                            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[pr][y], l[pl][x], sum, 0, 0, 0);
+                        }
         }
+    }
+}
+
+// The sums of a tile. Each matrix instruction rounds its sum, and there are three for each 32 values of the summed
+// index where one has the large terms. PRECISE, for fp32 results, spares the large sum the roundings of
+// the small terms: they have sums of their own, or where there are no registers for those (tiles of
+// 256), all the small terms come first and the operands' upper planes are read twice. Without it five
+// steps of 2176 x 1600 were 5.0e-6 off in place of 3.3e-6; for results in 16 bits that is nothing.
+template <Tile TILE, int LP, int RP, bool PRECISE, int MI, int NI>
+__device__ __forceinline__ void multiply_tile(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
+                                              half8* stages, float4v (&acc)[MI][NI]) {
+    if constexpr (!PRECISE) {
+        multiply<TILE, LP, RP, true>(o, b, i0, j0, d0, d1, stages, acc, acc);
+    } else if constexpr (TILE == Tile::k256) {
+        multiply<TILE, LP, RP, false>(o, b, i0, j0, d0, d1, stages, acc, acc);
+        __syncthreads();  // every wave has read the last stage
+        multiply<TILE, 1, 1, true>(o, b, i0, j0, d0, d1, stages, acc, acc);
+    } else {
+        float4v cross[MI][NI] = {};
+        multiply<TILE, LP, RP, true>(o, b, i0, j0, d0, d1, stages, acc, cross);
+#pragma unroll
+        for (int x = 0; x < MI; ++x)
+#pragma unroll
+            for (int y = 0; y < NI; ++y) acc[x][y] += cross[x][y];
     }
 }
 
@@ -413,7 +439,7 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
 }
 
 // C = L R', a workgroup a tile.
-template <Product KIND, Tile TILE, int LP, int RP, typename T>
+template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
     constexpr bool kSymmetric = is_symmetric(KIND);
@@ -427,7 +453,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, O
     int ti = tile % o.rows, tj = tile / o.rows;
     if constexpr (kSymmetric) triangle(tile, ti, tj);
     float4v acc[MI][NI] = {};
-    multiply<TILE, LP, RP>(o, b, ti * S::kSide, tj * S::kSide, 0, o.depth, stages, acc);
+    multiply_tile<TILE, LP, RP, PRECISE>(o, b, ti * S::kSide, tj * S::kSide, 0, o.depth, stages, acc);
     Coefficients k = o.k;
     if (KIND == Product::kPolynomial && o.first) k = o.first[b];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -469,7 +495,7 @@ struct Shares {
     }
 };
 
-template <Tile TILE, int LP, int RP>
+template <Tile TILE, int LP, int RP, bool PRECISE>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void shared_product_kernel(Operands o, Shares s) {
     using S = Shape<TILE>;
     constexpr int MI = S::kSide / S::kRows / 16, NI = S::kSide / S::kCols / 16, kThreads = kThreadsOf<TILE>;
@@ -483,8 +509,8 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void shared_product_kernel(Operan
         int ti, tj;
         triangle(t % tiles, ti, tj);
         float4v acc[MI][NI] = {};
-        multiply<TILE, LP, RP>(o, t / tiles, ti * S::kSide, tj * S::kSide, (at - t * s.depth) * 64,
-                               (stop - t * s.depth) * 64, stages, acc);
+        multiply_tile<TILE, LP, RP, PRECISE>(o, t / tiles, ti * S::kSide, tj * S::kSide, (at - t * s.depth) * 64,
+                                             (stop - t * s.depth) * 64, stages, acc);
         float* part = s.parts + (int64_t)(t + w) * (S::kSide * S::kSide) + threadIdx.x * 4;
 #pragma unroll
         for (int x = 0; x < MI; ++x)
@@ -576,10 +602,10 @@ struct LaneOffsets {
 };
 
 // acc += the 16 x 16 tiles of L R' for NL tiles of rows from L's row i on (every 16) and R's 16 rows from j on,
-// over one panel.
+// over one panel; the small terms go into `cross`, which may be `acc` where registers are short.
 template <int NL>
 __device__ __forceinline__ void local_product(LocalPlanes l, int i, LocalPlanes r, int j, int panel,
-                                              const LaneOffsets& at, float4v (&acc)[NL]) {
+                                              const LaneOffsets& at, float4v (&acc)[NL], float4v (&cross)[NL]) {
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
         const int rr = panel * r.panel + j * 8 + at.half[kk];
@@ -589,8 +615,8 @@ __device__ __forceinline__ void local_product(LocalPlanes l, int i, LocalPlanes 
             const int ll = panel * l.panel + (i + x * 16) * 8 + at.half[kk];
             const half8 lh = l.hi[ll], lw = l.lo[ll];
             acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rh, lh, acc[x], 0, 0, 0);
-            acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rl, lh, acc[x], 0, 0, 0);
-            acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rh, lw, acc[x], 0, 0, 0);
+            cross[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rl, lh, cross[x], 0, 0, 0);
+            cross[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rh, lw, cross[x], 0, 0, 0);
         }
     }
 }
@@ -688,9 +714,9 @@ __device__ __forceinline__ void small_split(const SmallLocal& m, bool tall, int 
 
 // The wave's tile of A over the workgroup's columns, as sums of stored values.
 __device__ __forceinline__ float4v small_gram(const SmallLocal& m, int n, int ti, int tj, const LaneOffsets& at) {
-    float4v acc[1] = {};
-    for (int q = 0; q < n / 64; ++q) local_product<1>(m.x, ti, m.x, tj, q, at, acc);
-    return acc[0];
+    float4v acc[1] = {}, cross[1] = {};
+    for (int q = 0; q < n / 64; ++q) local_product<1>(m.x, ti, m.x, tj, q, at, acc, cross);
+    return acc[0] + cross[0];
 }
 
 // From the wave's tile of A to its tile of P in local memory, for everyone.
@@ -701,8 +727,9 @@ __device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a,
     for (int c = 0; c < 4; ++c) gram[c] = a[c] * factor;
     local_store(m.a, nullptr, ti, tj, at, gram);
     __syncthreads();
-    float4v acc[1] = {};
-    local_product<1>(m.a, ti, m.a, tj, 0, at, acc);
+    float4v acc[1] = {}, cross[1] = {};
+    local_product<1>(m.a, ti, m.a, tj, 0, at, acc, cross);
+    acc[0] += cross[0];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
         poly[c] = k.b * gram[c] + k.c * acc[0][c] + (ti + at.row == tj + at.column + c ? k.a : 0.0f);
@@ -716,7 +743,7 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
                                              const Output<T>& out, int64_t b, int j0, SmallFactors f) {
     constexpr int kTiles = kSmallSide / 16;
     float4v next[kTiles] = {};
-    if (col < n) local_product<kTiles>(m.p, 0, m.xt, col, 0, at, next);
+    if (col < n) local_product<kTiles>(m.p, 0, m.xt, col, 0, at, next, next);
     __syncthreads();
     if (col < n) {
 #pragma unroll
@@ -1007,7 +1034,7 @@ bool allow_local(K kernel, size_t local) {
                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)local) == hipSuccess;
 }
 
-template <Product KIND, Tile TILE, int LP, int RP, typename T>
+template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
 int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float* parts, hipStream_t stream) {
     using S = Shape<TILE>;
     constexpr bool kSymmetric = is_symmetric(KIND);
@@ -1015,7 +1042,7 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
     const int64_t tiles = batch * (kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols);
     if constexpr (kSymmetric) {
         if (const int workers = workers_of(S::kSide, tiles, o.depth)) {
-            const auto kernel = shared_product_kernel<TILE, LP, RP>;
+            const auto kernel = shared_product_kernel<TILE, LP, RP, PRECISE>;
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
             const Shares s{parts, (int)tiles * (o.depth / 64), o.depth / 64, workers};
             kernel<<<workers, kThreadsOf<TILE>, local, stream>>>(o, s);
@@ -1023,15 +1050,15 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
             return launch_status();
         }
     }
-    const auto kernel = product_kernel<KIND, TILE, LP, RP, T>;
+    const auto kernel = product_kernel<KIND, TILE, LP, RP, PRECISE, T>;
     if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
     kernel<<<(unsigned)tiles, kThreadsOf<TILE>, local, stream>>>(o, out);
     return launch_status();
 }
 
-// Which planes a product takes. kBoth: hi hi + hi lo + lo hi. kExact: X0 from 16 bits, whose lower plane is zero. kUpper:
+// Which planes a product takes. kBoth: hi hi + hi lo + lo hi; kPrecise: with sums apart. kExact: X0 from 16 bits, whose lower plane is zero. kUpper:
 // hi hi, for the last product of a call that ends in bf16: an error of 2^-12 below one of 2^-9.
-enum class Depth { kBoth, kExact, kUpper };
+enum class Depth { kBoth, kPrecise, kExact, kUpper };
 
 // A product by the call's tiles.
 template <Product KIND, typename T>
@@ -1040,32 +1067,46 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
     o.rows = o.rows / tile;
     o.cols = o.cols / tile;
     const bool few = batch * (is_symmetric(KIND) ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols) <= 256;
-#define LAUNCH(TILE, LP, RP) return launch_product<KIND, Tile::TILE, LP, RP>(o, out, batch, parts, stream)
-#define LAUNCH_SMALLER(LP, RP)              \
-    if (tile == 128) LAUNCH(k128, LP, RP);  \
-    if (few) LAUNCH(k64Few, LP, RP);        \
-    LAUNCH(k64, LP, RP)
+#define LAUNCH(TILE, LP, RP, P) return launch_product<KIND, Tile::TILE, LP, RP, P>(o, out, batch, parts, stream)
+#define LAUNCH_SMALLER(LP, RP, P)              \
+    if (tile == 128) LAUNCH(k128, LP, RP, P);  \
+    if (few) LAUNCH(k64Few, LP, RP, P);        \
+    LAUNCH(k64, LP, RP, P)
+    constexpr bool kPlain = KIND == Product::kUpdate || KIND == Product::kLast;
     if constexpr (KIND == Product::kLast && sizeof(T) == 2) {
         if (depth == Depth::kUpper) {
-            if (tile == 256) LAUNCH(k256, 1, 1);
-            LAUNCH_SMALLER(1, 1);
+            if (tile == 256) LAUNCH(k256, 1, 1, false);
+            LAUNCH_SMALLER(1, 1, false);
         }
     }
     if constexpr (KIND == Product::kGram) {
         if (depth == Depth::kExact) {
-            LAUNCH_SMALLER(1, 1);
+            LAUNCH_SMALLER(1, 1, false);
         }
     }
-    if constexpr (KIND == Product::kUpdate || KIND == Product::kLast) {
+    if constexpr (kPlain && (KIND == Product::kUpdate || sizeof(T) == 2)) {
         if (depth == Depth::kExact) {
-            if (tile == 256) LAUNCH(k256, 2, 1);
-            LAUNCH_SMALLER(2, 1);
+            if (tile == 256) LAUNCH(k256, 2, 1, false);
+            LAUNCH_SMALLER(2, 1, false);
         }
-        if (tile == 256) LAUNCH(k256, 2, 2);
     }
-    LAUNCH_SMALLER(2, 2);
+    if constexpr (KIND != Product::kSquare && (KIND != Product::kLast || sizeof(T) == 4)) {
+        if (depth == Depth::kPrecise) {
+            if constexpr (kPlain) {
+                if (tile == 256) LAUNCH(k256, 2, 2, true);
+            }
+            LAUNCH_SMALLER(2, 2, true);
+        }
+    }
+    if constexpr (KIND != Product::kLast || sizeof(T) == 2) {
+        if constexpr (kPlain) {
+            if (tile == 256) LAUNCH(k256, 2, 2, false);
+        }
+        LAUNCH_SMALLER(2, 2, false);
+    }
 #undef LAUNCH_SMALLER
 #undef LAUNCH
+    return TRIVANCE_EINVAL;
 }
 
 // The ranges that the coefficients give: the largest singular value of X in any step, from values in [0, 1] on,
@@ -1172,7 +1213,8 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
     int turn = 0;  // of X
     for (int s = 0; s < steps && !rc;) {
         const int group = group_of(k, s, steps, dtype, w.m, w.n);
-        const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : Depth::kBoth;
+        const Depth both = sizeof(T) == 4 ? Depth::kPrecise : Depth::kBoth;
+        const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : both;
         rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a[0], a[0], gram, a[0], {}, nullptr},
                                      none, batch, tiles.symmetric, depth, shares, stream);
         int at = 0, qt = 0;
@@ -1180,7 +1222,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
             const Planes p = g == 0 ? q[0] : next;
             rc = product<Product::kPolynomial>(
                 {a[at], a[at], m, m, m, p, p, 1.0f, a[at], coefficients(s + g), s + g == 0 ? first : nullptr}, none,
-                batch, tiles.symmetric, Depth::kBoth, shares, stream);
+                batch, tiles.symmetric, both, shares, stream);
             if (g > 0 && !rc) {  // Q's scale is that of g + 1 factors
                 rc = square(p, q[qt], q[1 - qt], power(range.p[g] - range.p[0] - range.p[g - 1]));
                 qt = 1 - qt;
