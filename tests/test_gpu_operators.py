@@ -523,3 +523,47 @@ def test_operators_repeat_on_streams_and_in_graphs():
             assert torch.equal(want[name], replayed[name]), (name, turn)
         # the program's own work between replays
         float((x.float() ** 2).sum())
+
+
+def test_offsets_beyond_32_bits():
+    """Rows, ranks and matrices further than 2^31 elements apart."""
+    import paper_2602_17254_amd as T
+
+    far = 2 ** 31 + 72
+    base = torch.zeros(far + 70000, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(base)
+    dev = _gen(2)
+    for shape, strides in (((1, 2, 300), (0, far, 1)), ((2, 1, 300), (far, 300, 1)), ((2, 3, 77), (far, 80, 1))):
+        x, y = base.as_strided(shape, strides), out.as_strided(shape, strides)
+        x.copy_(torch.randn(shape, **dev))
+        near = x.contiguous()
+        want, mean, rstd = torch.empty_like(near), torch.empty(shape[:2], device="cuda"), torch.empty(shape[:2], device="cuda")
+        T.trivance_layernorm_forward(near, None, None, want, mean, rstd)
+        T.trivance_layernorm_forward(x, None, None, y)
+        assert torch.equal(y, want)
+        width = shape[2]
+        ws = torch.empty(T.trivance_layernorm_workspace_bytes(*shape), dtype=torch.uint8, device="cuda")
+        dg = [torch.empty((shape[0], width), device="cuda") for _ in range(4)]
+        T.trivance_layernorm_backward(near, near, None, mean, rstd, want, dg[0], dg[1], ws)
+        T.trivance_layernorm_backward(x, x, None, mean, rstd, y, dg[2], dg[3], ws)
+        assert torch.equal(y, want) and torch.equal(dg[0], dg[2]) and torch.equal(dg[1], dg[3])
+
+        chosen = torch.zeros((shape[0], shape[1], 1), dtype=torch.int32, device="cuda")
+        ws = torch.empty(T.trivance_balance_workspace_bytes(*shape), dtype=torch.uint8, device="cuda")
+        got = []
+        for logits, d in ((near, want), (x, y)):
+            counts = torch.empty((shape[0], width + 1), dtype=torch.int32, device="cuda")
+            probs = torch.empty((shape[0], width), device="cuda")
+            T.trivance_balance_counts(logits, chosen, counts, probs, ws)
+            T.trivance_balance_backward(logits, counts, 1, d)
+            got.append((counts, probs))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and torch.equal(y, want)
+    for shape, strides in (((2, 70, 90), (far, 96, 1)), ((2, 300, 130), (far, 130, 1)), ((2, 40, 600), (far, 600, 1))):
+        x, y = base.as_strided(shape, strides), out.as_strided(shape, strides)
+        x.copy_(torch.randn(shape, **dev))
+        near = x.contiguous()
+        want = torch.empty_like(near)
+        ws = torch.empty(T.trivance_orthogonalize_workspace_bytes(*shape), dtype=torch.uint8, device="cuda")
+        T.trivance_orthogonalize(near, want, ws)
+        T.trivance_orthogonalize(x, y, ws)
+        assert torch.equal(y, want)
