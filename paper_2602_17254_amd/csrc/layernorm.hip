@@ -10,8 +10,8 @@
 // the forward pass takes the mean and then the squares about it, the backward pass both row sums, from
 // there. A lane holds the same columns of every row, so the weight gradients of a workgroup's
 // rows add up in registers too; a workgroup's sums go to the workspace and a second kernel joins them
-// in a fixed order, in 64 bits, into the rank's row. All sums are in fp32 or more; y and dx are
-// rounded once.
+// in a fixed order, in 64 bits, into the rank's row. All sums are in fp32 or more, that of the mean in 64
+// bits, as a row's values may nearly cancel; y and dx are rounded once.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -34,14 +34,14 @@ constexpr int kBlock = LANES < kThreads ? kThreads : LANES;
 // Sum over the LANES lanes that hold a row. Rows wider than a wave meet in local memory, in `slot`,
 // which alternates between two from one sum to the next: the barrier of the second sum stands between
 // the reads of the first and the writes of the third.
-template <int LANES>
-__device__ __forceinline__ float row_sum(float x, float* slot) {
+template <int LANES, typename F>
+__device__ __forceinline__ F row_sum(F x, F* slot) {
     if constexpr (LANES <= 64) return lanes_sum<LANES>(x);
     constexpr int kWaves = LANES / 64;
     x = lanes_sum<64>(x);
     if (threadIdx.x % 64 == 0) slot[threadIdx.x / 64] = x;
     __syncthreads();
-    float s = 0.0f;
+    F s = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s += slot[w];
     return s;
@@ -81,13 +81,13 @@ struct Columns {
             skip[j] = i < width ? i - first[j] : V;
         }
     }
-    // The sum of f(j, k) over the values that count.
+    // The sum of f(j, k), of its type, over the values that count.
     template <typename F>
-    __device__ __forceinline__ float sum(F f) const {
-        float s = 0.0f;
+    __device__ __forceinline__ auto sum(F f) const {
+        decltype(f(0, 0)) s = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            float part = 0.0f;
+            decltype(f(0, 0)) part = 0;
             if (skip[j] == 0) {
 #pragma unroll
                 for (int k = 0; k < V; ++k) part += f(j, k);
@@ -133,7 +133,8 @@ __device__ __forceinline__ int group_of_lane() {
 template <typename T, int V, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> a) {
     constexpr int G = kBlock<LANES> / LANES;
-    __shared__ float slots[2][kWide / 64];
+    __shared__ double sums[kWide / 64];
+    __shared__ float squares[kWide / 64];
     const int lane = threadIdx.x % LANES, group = group_of_lane<LANES>();
     const Columns<V, LANES, NV> own(lane, (int)a.width);
     const float inv = 1.0f / (float)a.width;
@@ -162,13 +163,14 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> 
 #pragma unroll
                 for (int k = 0; k < V; ++k) v[j][k] = (float)next[j][k];
             if (t + step < a.tokens) fetch(r, t + step, next);  // on its way during this row's sums
-            const float mean = row_sum<LANES>(own.sum([&](int j, int k) { return v[j][k]; }), slots[0]) * inv;
+            const float mean =
+                (float)(row_sum<LANES>(own.sum([&](int j, int k) { return (double)v[j][k]; }), sums) / (double)a.width);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int k = 0; k < V; ++k) v[j][k] -= mean;
             const float square =
-                row_sum<LANES>(own.sum([&](int j, int k) { return v[j][k] * v[j][k]; }), slots[1]);
+                row_sum<LANES>(own.sum([&](int j, int k) { return v[j][k] * v[j][k]; }), squares);
             const float rstd = 1.0f / sqrtf(square * inv + a.eps);
             T* y = a.y + r * a.y_rank + t * a.y_token;
 #pragma unroll
@@ -190,26 +192,28 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> 
 template <typename T>
 __global__ __launch_bounds__(kWide) void norm_forward_long_kernel(Forward<T> a) {
     constexpr int V = kVec<T>;
-    __shared__ float slots[2][kWide / 64];
+    __shared__ double sums[kWide / 64];
+    __shared__ float squares[kWide / 64];
     const float inv = 1.0f / (float)a.width;
     const int64_t i0 = (int64_t)threadIdx.x * V;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
             const T* x = a.x + r * a.x_rank + t * a.x_token;
             T* y = a.y + r * a.y_rank + t * a.y_token;
-            float v[V], s = 0.0f, q = 0.0f;
+            float v[V], q = 0.0f;
+            double s = 0.0;
             for (int64_t i = i0; i < a.width; i += kWide * V) {
                 load_row<T>(x, i, a.width, 0.0f, v);
 #pragma unroll
                 for (int k = 0; k < V; ++k) s += v[k];
             }
-            const float mean = row_sum<kWide>(s, slots[0]) * inv;
+            const float mean = (float)(row_sum<kWide>(s, sums) / (double)a.width);
             for (int64_t i = i0; i < a.width; i += kWide * V) {
                 load_row<T>(x, i, a.width, mean, v);
 #pragma unroll
                 for (int k = 0; k < V; ++k) q += (v[k] - mean) * (v[k] - mean);
             }
-            const float rstd = 1.0f / sqrtf(row_sum<kWide>(q, slots[1]) * inv + a.eps);
+            const float rstd = 1.0f / sqrtf(row_sum<kWide>(q, squares) * inv + a.eps);
             for (int64_t i = i0; i < a.width; i += kWide * V) {
                 float gamma[V], beta[V];
                 load_row<T>(x, i, a.width, 0.0f, v);

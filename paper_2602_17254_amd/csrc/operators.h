@@ -119,35 +119,63 @@ __device__ __forceinline__ void store_row(T* row, int64_t i, int64_t width, cons
 // 2; then mirroring 8 and 16 lanes and exchanging halves of 32 and 64 bring together what
 // the steps before have made equal. One instruction a step, and none of local memory's latency.
 template <int CONTROL>
-__device__ __forceinline__ float from_lane(float x) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+__device__ __forceinline__ int word_from_lane(int x) {
+    return __builtin_amdgcn_mov_dpp(x, CONTROL, 0xf, 0xf, true);
 }
 
-template <int L, typename OP>
-__device__ __forceinline__ float over_lanes(float x, OP op) {
+template <int CONTROL>
+__device__ __forceinline__ float from_lane(float x) {
+    return __builtin_bit_cast(float, word_from_lane<CONTROL>(__builtin_bit_cast(int, x)));
+}
+
+struct Words {
+    int lo, hi;
+};
+
+template <int CONTROL>
+__device__ __forceinline__ double from_lane(double x) {
+    const Words w = __builtin_bit_cast(Words, x);
+    return __builtin_bit_cast(double, Words{word_from_lane<CONTROL>(w.lo), word_from_lane<CONTROL>(w.hi)});
+}
+
+// v_permlaneN_swap exchanges the odd rows of N lanes of its first register with the even rows of its
+// second: of two copies, each lane then holds the pair's values. (The builtins of this compiler
+// return the first register for both; two wait states stand between the copies and the exchange.)
+template <int N>
+__device__ __forceinline__ void exchange(int& x, int& y) {
+    if constexpr (N == 16) asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    else asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+}
+
+template <int N, typename OP>
+__device__ __forceinline__ float with_pair(float x, OP op) {
+    int a = __builtin_bit_cast(int, x), b = a;
+    exchange<N>(a, b);
+    return op(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+template <int N, typename OP>
+__device__ __forceinline__ double with_pair(double x, OP op) {
+    Words a = __builtin_bit_cast(Words, x), b = a;
+    exchange<N>(a.lo, b.lo);
+    exchange<N>(a.hi, b.hi);
+    return op(__builtin_bit_cast(double, a), __builtin_bit_cast(double, b));
+}
+
+template <int L, typename F, typename OP>
+__device__ __forceinline__ F over_lanes(F x, OP op) {
     if constexpr (L >= 2) x = op(x, from_lane<0xB1>(x));    // quads 1 0 3 2
     if constexpr (L >= 4) x = op(x, from_lane<0x4E>(x));    // quads 2 3 0 1
     if constexpr (L >= 8) x = op(x, from_lane<0x141>(x));   // halves of 16 mirrored
     if constexpr (L >= 16) x = op(x, from_lane<0x140>(x));  // 16 mirrored
-    // v_permlaneN_swap exchanges the odd rows of N lanes of its first register with the even rows of its
-    // second: of two copies, each lane then holds the pair's values. (The builtins of this compiler
-    // return the first register for both; two wait states stand between the copies and the exchange.)
-    if constexpr (L >= 32) {
-        float y = x;
-        asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(x), "+v"(y));
-        x = op(x, y);
-    }
-    if constexpr (L >= 64) {
-        float y = x;
-        asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
-        x = op(x, y);
-    }
+    if constexpr (L >= 32) x = with_pair<16>(x, op);
+    if constexpr (L >= 64) x = with_pair<32>(x, op);
     return x;
 }
 
-template <int L>
-__device__ __forceinline__ float lanes_sum(float x) {
-    return over_lanes<L>(x, [](float a, float b) { return a + b; });
+template <int L, typename F>
+__device__ __forceinline__ F lanes_sum(F x) {
+    return over_lanes<L>(x, [](F a, F b) { return a + b; });
 }
 
 template <int L>

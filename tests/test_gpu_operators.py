@@ -157,13 +157,28 @@ def test_layernorm_rows_that_are_no_numbers_stay_apart():
         x[0, 2, width // 2] = math.nan
         x[0, 5, 0] = math.inf
         x[0, 6] = 4.0  # no spread: h is zero
-        y = torch.empty_like(x)
-        T.trivance_layernorm_forward(x, None, torch.full((width,), 0.5, device="cuda"), y)
+        y, mean, rstd = torch.empty_like(x), torch.empty((1, 8), device="cuda"), torch.empty((1, 8), device="cuda")
+        T.trivance_layernorm_forward(x, None, torch.full((width,), 0.5, device="cuda"), y, mean, rstd)
         torch.cuda.synchronize()
         for t in range(8):
+            assert bool(torch.isnan(rstd[0, t])) == (t in (2, 5))
             assert bool(torch.isnan(y[0, t]).all()) == (t in (2, 5))
             assert bool(torch.isfinite(y[0, t]).all()) == (t not in (2, 5))
         assert bool((y[0, 6] == 0.5).all())
+
+
+def test_layernorm_mean_of_rows_that_nearly_cancel():
+    """The sum of a row's values is exact but for 2^-53 a step: the mean is within its rounding to fp32, and
+    2^-40 of the values' mean size."""
+    import paper_2602_17254_amd as T
+
+    for width in (5, 60, 1024, 4096, 12000, 20000):
+        x = torch.randn((1, 5, width), **_gen(width))
+        x -= x.mean(2, keepdim=True) * (1 - 1e-3)
+        y, mean, rstd = torch.empty_like(x), torch.empty((1, 5), device="cuda"), torch.empty((1, 5), device="cuda")
+        T.trivance_layernorm_forward(x, None, None, y, mean, rstd)
+        want = x.double().mean(2)
+        ref.assert_within(mean, want, ref.U * want.abs() * 1.01 + 2.0 ** -40 * x.double().abs().mean(2), "mean")
 
 
 def test_layernorm_statistics_of_rows_far_from_zero():
