@@ -209,19 +209,25 @@ __device__ __forceinline__ double count_weight(int tokens, int experts, int64_t 
     return tokens > 0 ? scale * experts / ((double)top_k * n * n) : 0.0;
 }
 
-__global__ __launch_bounds__(64) void balance_loss_kernel(const int* counts, const float* probs,
-                                                          float* loss, int64_t ranks, int experts,
-                                                          int64_t top_k, int64_t counts_rank,
-                                                          int64_t probs_rank, double scale) {
+__global__ __launch_bounds__(kThreads) void balance_loss_kernel(const int* counts, const float* probs,
+                                                                float* loss, int64_t ranks, int experts,
+                                                                int64_t top_k, int64_t counts_rank,
+                                                                int64_t probs_rank, double scale) {
+    __shared__ double sums[kThreads / 64];
     for (int64_t r = blockIdx.x; r < ranks; r += gridDim.x) {
         const int* c = counts + r * counts_rank;
         const float* p = probs + r * probs_rank;
+        const int tokens = c[experts];
         double s = 0.0;
-        for (int e = threadIdx.x; e < experts; e += 64) s += (double)c[e] * p[e];
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
-        if (threadIdx.x == 0)
-            loss[r] = c[experts] > 0 ? (float)(s * count_weight(c[experts], experts, top_k, scale)) : 0.0f;
+        for (int e = threadIdx.x; e < experts; e += kThreads) s += (double)c[e] * p[e];
+        s = lanes_sum<64>(s);
+        if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            loss[r] = tokens > 0 ? (float)(s * count_weight(tokens, experts, top_k, scale)) : 0.0f;
+        }
+        __syncthreads();
     }
 }
 
@@ -440,7 +446,7 @@ int trivance_balance_loss(const int32_t* counts, const float* probs, float* loss
     if (!counts || !probs || !loss || !rows_fit(ranks, 1, experts + 1, counts_rank_stride, 0) ||
         !rows_fit(ranks, 1, experts, probs_rank_stride, 0))
         return TRIVANCE_EINVAL;
-    balance_loss_kernel<<<(unsigned)imin(ranks, kMaxGridX), 64, 0, reinterpret_cast<hipStream_t>(stream)>>>(
+    balance_loss_kernel<<<(unsigned)imin(ranks, kMaxGridX), kThreads, 0, reinterpret_cast<hipStream_t>(stream)>>>(
         counts, probs, loss, ranks, (int)experts, top_k, counts_rank_stride, probs_rank_stride, scale);
     return launch_status();
 }
