@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> 
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (own.skip[j] < V)
-                to[j] = load_vector<STREAM>(reinterpret_cast<const Some<T, V>*>(x + own.first[j]));
+                to[j] = load_vector<STREAM, V>(x + own.first[j]);
     };
     const int64_t step = (int64_t)gridDim.x * G;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void norm_forward_kernel(Forward<T> 
                 Some<T, V> o;
 #pragma unroll
                 for (int k = 0; k < V; ++k) o[k] = (T)(v[j][k] * rstd * gamma[j][k] + beta[j][k]);
-                if (own.skip[j] < V) store_vector<STREAM>(reinterpret_cast<Some<T, V>*>(y + own.first[j]), o);
+                if (own.skip[j] < V) store_vector<STREAM, V>(y + own.first[j], o);
             }
             if (lane == 0) {
                 if (a.mean) a.mean[r * a.tokens + t] = mean;
@@ -294,8 +294,8 @@ __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1))
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (own.skip[j] < V) {
-                    to.x[j] = load_vector<STREAM>(reinterpret_cast<const Some<T, V>*>(x + own.first[j]));
-                    to.dy[j] = load_vector<STREAM>(reinterpret_cast<const Some<T, V>*>(dy + own.first[j]));
+                    to.x[j] = load_vector<STREAM, V>(x + own.first[j]);
+                    to.dy[j] = load_vector<STREAM, V>(dy + own.first[j]);
                 }
             to.mean = a.mean[r * a.tokens + t];
             to.rstd = a.rstd[r * a.tokens + t];
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1))
                 Some<T, V> o;
 #pragma unroll
                 for (int k = 0; k < V; ++k) o[k] = (T)(rstd * (g[j][k] - s1 - h[j][k] * s2));
-                if (own.skip[j] < V) store_vector<STREAM>(reinterpret_cast<Some<T, V>*>(dx + own.first[j]), o);
+                if (own.skip[j] < V) store_vector<STREAM, V>(dx + own.first[j], o);
             }
         };
         Ahead next;

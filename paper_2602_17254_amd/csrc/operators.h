@@ -23,13 +23,31 @@ struct Packed {
     typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
+// A vector load or store that, where STREAM, does not stay in the caches: of tensors beyond kStreamBytes,
+// the L2 caches together, which would drop it before its next reader.
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+
+template <bool STREAM, int V, typename T>
+__device__ __forceinline__ auto load_vector(const T* p) {
+    typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const U*>(p));
+    else return *reinterpret_cast<const U*>(p);
+}
+
+template <bool STREAM, int V, typename T, typename U>
+__device__ __forceinline__ void store_vector(T* p, U v) {
+    typedef T W __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<W*>(p));
+    else *reinterpret_cast<W*>(p) = v;
+}
+
 // A lane's vector of a row as it lies in memory, values i .. i + VEC; `fill` beyond the row's end.
-template <typename T>
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ typename Packed<T>::type load_packed(const T* row, int64_t i, int64_t width, T fill) {
     constexpr int V = kVec<T>;
     typename Packed<T>::type x;
     if (i + V <= width) {
-        x = *reinterpret_cast<const typename Packed<T>::type*>(row + i);
+        x = load_vector<STREAM, V>(row + i);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) x[k] = fill;
@@ -49,22 +67,6 @@ __device__ __forceinline__ void load_row(const T* row, int64_t i, int64_t width,
     const typename Packed<T>::type x = load_packed<T>(row, i, width, (T)fill);
 #pragma unroll
     for (int k = 0; k < kVec<T>; ++k) out[k] = (float)x[k];
-}
-
-// A vector load or store that, where STREAM, does not stay in the caches: of tensors beyond kStreamBytes,
-// the L2 caches together, which would drop it before its next reader.
-constexpr int64_t kStreamBytes = (int64_t)32 << 20;
-
-template <bool STREAM, typename V>
-__device__ __forceinline__ V load_vector(const V* p) {
-    if constexpr (STREAM) return __builtin_nontemporal_load(p);
-    return *p;
-}
-
-template <bool STREAM, typename V>
-__device__ __forceinline__ void store_vector(V* p, V v) {
-    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
-    else *p = v;
 }
 
 // V values of weights, whose type is known at run time (the branch is uniform and taken once a row
@@ -99,14 +101,14 @@ __device__ __forceinline__ void load_weights(const void* p, int dtype, int64_t i
     }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool STREAM = false>
 __device__ __forceinline__ void store_row(T* row, int64_t i, int64_t width, const float (&v)[V]) {
     typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     if (i + V <= width) {
         U x;
 #pragma unroll
         for (int k = 0; k < V; ++k) x[k] = (T)v[k];
-        *reinterpret_cast<U*>(row + i) = x;
+        store_vector<STREAM, V>(row + i, x);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
