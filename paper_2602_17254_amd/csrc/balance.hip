@@ -12,8 +12,8 @@
 // exchanges between lanes. A lane holds the same experts of every row: a workgroup's sums of
 // probabilities add up in registers, its counts in local memory (integers: the order of
 // additions does not matter); a second kernel joins the workgroups' sums in a fixed order, in 64 bits.
-// Measured at 8 ranks of 32768 tokens: counts of 256 bf16 experts, 143 MB, 26.8 us (5.3 TB/s, a good part of it
-// from the caches) and 4.1 us to join; gradient of 256 fp32 experts, 537 MB, 90.5 us (5.9 TB/s).
+// Measured at 8 ranks of 32768 tokens: counts of 256 bf16 experts with two tokens in five unmasked, some 60 MB, 24
+// us and 4 to join; gradient of 256 fp32 experts, 537 MB, 93 us (5.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -83,12 +83,16 @@ struct Counts {
     float* probs;  // rows `probs_rank` apart
     int* part_counts;   // [ranks][chunks][experts + 1], where a rank's tokens are in several chunks
     float* part_probs;  // [ranks][chunks][experts]
-    int64_t ranks, tokens, rank_stride, token_stride, counts_rank, probs_rank, chunks, per;
+    int64_t ranks, tokens, rank_stride, token_stride, counts_rank, probs_rank, chunks, per;  // per: most tokens of a chunk
     int experts, top_k, wide_ids;
     FastDiv32 by_top_k;
 };
 
-// Bound by the logits' bytes where there are many tokens, by latency (4.9 us at 9 x 512 x 64) where there are few.
+// A chunk's tokens are those of every `chunks`th group of rows, so that padding at the end of a rank's tokens
+// leaves all workgroups the same work (28 us in place of 31 with contiguous chunks, at the size above). There the
+// rows take half the time and what stands before and after them, with the join, the other half; more rows
+// of a lane on their way at once were slower (30 us for two, 35 for four). With few tokens latency bounds it: 4.9 us
+// at 9 ranks of 512 tokens and 64 experts.
 template <typename T, int L, int NV>
 __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
     constexpr int V = kVec<T>, G = kThreads / L;
@@ -97,8 +101,7 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
     float* join = reinterpret_cast<float*>(shared + a.experts + 1);
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
-        const int64_t c = blockIdx.x, t1 = c * a.per;
-        const int64_t t2 = t1 + a.per < a.tokens ? t1 + a.per : a.tokens;
+        const int64_t c = blockIdx.x, step = a.chunks * G;
         const uint8_t* mask = a.mask ? a.mask + r * a.tokens : nullptr;
         __syncthreads();
         for (int e = threadIdx.x; e <= a.experts; e += kThreads) hist[e] = 0;
@@ -106,12 +109,12 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
         // the logits first, so that they are on their way during the counting
         Row<T, L, NV> next;
         const T* x = a.logits + r * a.rank_stride;
-        int64_t t = t1 + group;
-        const auto counted = [&](int64_t t) { return t < t2 && (!mask || mask[t]); };
-        bool used = counted(t), after = counted(t + G);  // a token's mask is known before its row is fetched
+        int64_t t = c * G + group;
+        const auto counted = [&](int64_t t) { return t < a.tokens && (!mask || mask[t]); };
+        bool used = counted(t), after = counted(t + step);  // a token's mask is known before its row is fetched
         if (used) next.template fetch<false>(x + t * a.token_stride, lane, a.experts);
-        const int64_t first = (r * a.tokens + t1) * a.top_k;
-        const uint32_t slots = (uint32_t)(t2 - t1) * (uint32_t)a.top_k;  // below 2^31, i0 below 2^32
+        const uint32_t most = (uint32_t)(a.per < a.tokens ? a.per : a.tokens);
+        const uint32_t slots = most * (uint32_t)a.top_k;  // below 2^31, i0 below 2^32
         constexpr int kIds = 4;  // of a lane on their way at once
         for (uint32_t i0 = threadIdx.x; i0 < slots; i0 += kIds * kThreads) {
             int64_t id[kIds];
@@ -119,9 +122,12 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
             for (int q = 0; q < kIds; ++q) {
                 const uint32_t i = i0 + q * kThreads;
                 id[q] = -1;
-                if (i < slots && (!mask || mask[t1 + fdiv32(i, a.by_top_k)]))
-                    id[q] = a.wide_ids ? static_cast<const int64_t*>(a.ids)[first + i]
-                                       : static_cast<const int*>(a.ids)[first + i];
+                if (i >= slots) continue;
+                const uint32_t u = fdiv32(i, a.by_top_k);  // the slot's token among the chunk's
+                const int64_t of = c * G + u / G * step + u % G;
+                const int64_t at = (r * a.tokens + of) * a.top_k + (i - u * (uint32_t)a.top_k);
+                if (counted(of))
+                    id[q] = a.wide_ids ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int*>(a.ids)[at];
             }
 #pragma unroll
             for (int q = 0; q < kIds; ++q)
@@ -129,14 +135,14 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
         }
         float sum[NV][V] = {};
         int live = 0;
-        while (t < t2) {
+        while (t < a.tokens) {
             const bool use = used;
             float v[NV][V];
             next.values(v);
-            t += G;
+            t += step;
             used = after;
             if (used) next.template fetch<false>(x + t * a.token_stride, lane, a.experts);
-            after = counted(t + G);
+            after = counted(t + step);
             if (!use) continue;
             row_exp<T, L, NV>(v);
             float s = 0.0f;
@@ -325,7 +331,7 @@ int row_lanes(int experts, int vec) {
     return l;
 }
 
-// The tokens of a chunk: enough chunks to fill the GPU, but four rows at least for each group of lanes;
+// The most tokens of a chunk: enough chunks to fill the GPU, but four rows at least for each group of lanes;
 // so few that a chunk's slots are counted in 31 bits.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, int lanes) {
     const int64_t rows = kThreads / lanes;
