@@ -17,8 +17,8 @@
 // of two, exactly where it has 16 bits; the rest of the norm goes into the first step's coefficients.
 //
 // What bounds it: the MFMA rate, for matrices of some hundred rows and more; below that the latency of the steps'
-// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 1.17 ms, 0.47 PFLOP/s
-// of the products' own and 0.7 to 1.3 of MFMA in each kernel; 1024 x 4096 0.29 ms; 512 x 512 fp32 0.14;
+// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 1.26 ms, 0.45 PFLOP/s
+// of the products' own and 0.55 to 0.9 of MFMA in each kernel; 1024 x 4096 0.29 ms; 512 x 512 fp32 0.14;
 // 64 x 2048 0.064; 64 x 256 0.039.
 // Layout. X is kept both ways round, so that both operands of every product have their summed index
 // contiguous; sides are padded with zeros to whole tiles. A and A A are symmetric: only tiles on and
@@ -444,8 +444,8 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
 }
 
 // C = L R', a workgroup a tile. Bound by the MFMA rate and what each stage waits for: P X at 2048 x 8192 from
-// 2048 takes 155 us with three products (2.1e11 flop, 1.33 PFLOP/s), the last with one 92 (0.75: reading the operands
-// weighs more). With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
+// 2048 takes 183 us with three products (2.1e11 flop, 1.13 PFLOP/s), 155 with two (0.89) and 92 with one (0.75):
+// reading the operands weighs more. With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
 template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
@@ -1066,8 +1066,9 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
 }
 
 // Which planes a product takes. kBoth: hi hi + hi lo + lo hi; kPrecise: with sums apart. kExact: X0 from 16 bits,
-// whose lower plane is zero. kUpper: hi hi, for the last product of a call that ends in bf16: an error of 2^-12
-// below one of 2^-9.
+// whose lower plane is zero. kUpper: hi hi, for the last product of a call that ends in bf16, where it is one step: 3%
+// more error than the rounding to bf16 has by itself. Products of several polynomials have larger entries
+// for the same result, and it would be 20% at 2048 x 8192.
 enum class Depth { kBoth, kPrecise, kExact, kUpper };
 
 // A product by the call's tiles.
@@ -1253,7 +1254,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
         } else {
             update.factor *= scale * power(-range.x);
             rc = product<Product::kLast>(update, out, batch, tiles.update,
-                                         dtype == TRIVANCE_BF16 ? Depth::kUpper : depth, shares, stream);
+                                         dtype == TRIVANCE_BF16 && group == 1 ? Depth::kUpper : depth, shares, stream);
         }
     }
     return rc;

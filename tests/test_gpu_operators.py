@@ -582,3 +582,55 @@ def test_offsets_beyond_32_bits():
         T.trivance_orthogonalize(near, want, ws)
         T.trivance_orthogonalize(x, y, ws)
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tensors_beyond_the_caches(dtype):
+    """Large tensors take other loads and stores: every row has the bits that it has in a call of its rank alone,
+    which is small."""
+    import paper_2602_17254_amd as T
+
+    dt, dev = ref.DTYPES[dtype], _gen(8)
+    size = torch.finfo(dt).bits // 8
+    tokens, width = 701, 12007 // size
+    x, _ = _place(torch.randn((6, tokens, width), **dev), "padded", dt)
+    dy, _ = _place(torch.randn((6, tokens, width), **dev), "padded", dt)
+    assert x.numel() * size > 2 ** 25 > x[:1].numel() * size
+    gamma = 1 + 0.3 * torch.randn(width, **dev)
+
+    def norm(x, dy):
+        y, y_base = _place(torch.zeros_like(x), "padded", dt)
+        dx, dx_base = _place(torch.zeros_like(x), "padded", dt)
+        mean, rstd = (torch.full(x.shape[:2], math.nan, device="cuda") for _ in range(2))
+        sums = torch.full((2, x.shape[0], width), math.nan, device="cuda")
+        ws = torch.full((T.trivance_layernorm_workspace_bytes(*x.shape) // 4,), math.nan, device="cuda")
+        T.trivance_layernorm_forward(x, gamma, None, y, mean, rstd)
+        T.trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, sums[0], sums[1], ws)
+        out = y.clone(), mean, rstd, dx.clone(), sums
+        _gaps_kept(y, y_base)
+        _gaps_kept(dx, dx_base)
+        return out
+
+    y, mean, rstd, dx, sums = norm(x, dy)
+    for r in range(6):
+        one = norm(x[r:r + 1], dy[r:r + 1])
+        for got, want in zip((y, mean, rstd, dx), one):
+            assert torch.equal(got[r:r + 1], want)
+        _, (dgamma, bg), (dbeta, bb) = ref.layernorm_backward(
+            dy[r:r + 1].double(), x[r:r + 1].double(), gamma.double(), mean[r:r + 1].double(), rstd[r:r + 1].double())
+        ref.assert_within(sums[0][r:r + 1], dgamma, bg, "dgamma")
+        ref.assert_within(sums[1][r:r + 1], dbeta, bb, "dbeta")
+
+    experts = 251
+    logits, _ = _place(2 * torch.randn((5, 40000 // size, experts), **dev), "padded", dt)
+    assert logits.numel() * size > 2 ** 25 > logits[:1].numel() * size
+    mask = torch.rand(logits.shape[:2], **dev) < 0.7
+    counts = torch.randint(0, 300, (5, experts + 1), **dev).to(torch.int32)
+    d, d_base = _place(torch.zeros_like(logits), "padded", dt)
+    T.trivance_balance_backward(logits, counts, 2, d, mask)
+    got = d.clone()
+    _gaps_kept(d, d_base)
+    for r in range(5):
+        want, _ = _place(torch.zeros_like(logits[r:r + 1]), "padded", dt)
+        T.trivance_balance_backward(logits[r:r + 1], counts[r:r + 1], 2, want, mask[r:r + 1])
+        assert torch.equal(got[r:r + 1], want)
