@@ -258,13 +258,14 @@ __device__ __forceinline__ float* sums_of(const Backward<T>& a, int64_t r, int64
     return d ? d + r * a.grad_rank : nullptr;
 }
 
-// Whether gamma stays in local memory, so that the registers suffice for two workgroups on a CU: one goes on
-// while the other waits for its row's sums.
+// Whether gamma stays in local memory, so that the registers suffice for two workgroups of 512 lanes on a CU, or four of
+// 256: some go on while others wait for their row's sums. With 256 lanes 2 x 8192 x 2200 bf16 takes 57 us in place of
+// 66, 8 x 4096 x 4096 161 in place of 166, 4 x 500 x 4000 18.6 in place of 18.0.
 template <int V, int LANES, int NV>
-constexpr bool kLocalGamma = LANES == 512 && V == 8 && NV == 2;
+constexpr bool kLocalGamma = (LANES == 256 || LANES == 512) && V == 8 && NV == 2;
 
 // Bound by the bytes of x, dy and dx: 298 us at 8 x 4096 x 8192 bf16, 1.6 GB, 5.4 TB/s (and 67 MB of
-// workgroups' sums, which take another 11 us to join); 36 us and 5 at 9 x 1001 x 2051 fp16, 111 MB. With few rows the
+// workgroups' sums, which take another 11 us to join); 33 us and 6 at 9 x 1001 x 2051 fp16, 111 MB (3.3 TB/s). With few rows the
 // latency of a lane's rows one after another bounds it: 8.6 us at 81 x 16 tokens of 768 fp32.
 template <typename T, int V, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1)) void norm_backward_kernel(Backward<T> a) {
@@ -530,13 +531,13 @@ int64_t imax(int64_t a, int64_t b) { return a > b ? a : b; }
 
 // The tokens that a chunk of the backward pass takes. Two workgroups a CU (512; one where a row takes 512
 // lanes), of four rows at least for each group of lanes, so that few tokens still spread over the GPU;
-// four a CU where each then has 16 rows or more, as each chunk's sums take a way through memory. A few
-// workgroups above a multiple of the CUs cost a round: 9 x 1001 x 2051 fp16 measured 37 us with 504
-// workgroups, 42 with 531, 58 with 252.
+// four a CU where each then has 8 rows or more, as each chunk's sums take a way through memory: 9 x 1001 x 2051 fp16
+// takes 36 us with 1008 workgroups and 39 with 504, 27 x 333 x 2500 41 with 999 and 40 with 486. A few
+// workgroups above a multiple of what the CUs hold would cost a round.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
     const int64_t rows = group_rows(s), wide = block_lanes(s) / kThreads;
     const int64_t many = imax(1, 1024 / ranks), few = imax(1, 512 / wide / ranks);
-    const int64_t chunks = imax(1, many * 16 * rows <= tokens ? many : imin(few, tokens / (4 * rows)));
+    const int64_t chunks = imax(1, many * 8 * rows <= tokens ? many : imin(few, tokens / (4 * rows)));
     const int64_t per = (tokens + chunks - 1) / chunks;
     return imax(rows, (per + rows - 1) / rows * rows);
 }
