@@ -444,8 +444,8 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
 }
 
 // C = L R', a workgroup a tile. Bound by the MFMA rate and what each stage waits for: P X at 2048 x 8192 from
-// 2048 takes 183 us with three products (2.1e11 flop, 1.13 PFLOP/s), 155 with two (0.89) and 92 with one (0.75):
-// reading the operands weighs more. With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
+// 2048 takes 183 us with three products (2.1e11 flop, 1.13 PFLOP/s) and 155 with two (0.89): reading the
+// operands weighs more. With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
 template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
@@ -1066,10 +1066,8 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
 }
 
 // Which planes a product takes. kBoth: hi hi + hi lo + lo hi; kPrecise: with sums apart. kExact: X0 from 16 bits,
-// whose lower plane is zero. kUpper: hi hi, for the last product of a call that ends in bf16, where it is one step: 3%
-// more error than the rounding to bf16 has by itself. Products of several polynomials have larger entries
-// for the same result, and it would be 20% at 2048 x 8192.
-enum class Depth { kBoth, kPrecise, kExact, kUpper };
+// whose lower plane is zero.
+enum class Depth { kBoth, kPrecise, kExact };
 
 // A product by the call's tiles.
 template <Product KIND, typename T>
@@ -1084,12 +1082,6 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
     if (few) LAUNCH(k64Few, LP, RP, P);        \
     LAUNCH(k64, LP, RP, P)
     constexpr bool kPlain = KIND == Product::kUpdate || KIND == Product::kLast;
-    if constexpr (KIND == Product::kLast && sizeof(T) == 2) {
-        if (depth == Depth::kUpper) {
-            if (tile == 256) LAUNCH(k256, 1, 1, false);
-            LAUNCH_SMALLER(1, 1, false);
-        }
-    }
     if constexpr (KIND == Product::kGram) {
         if (depth == Depth::kExact) {
             LAUNCH_SMALLER(1, 1, false);
@@ -1253,8 +1245,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
             turn = 1 - turn;
         } else {
             update.factor *= scale * power(-range.x);
-            rc = product<Product::kLast>(update, out, batch, tiles.update,
-                                         dtype == TRIVANCE_BF16 && group == 1 ? Depth::kUpper : depth, shares, stream);
+            rc = product<Product::kLast>(update, out, batch, tiles.update, depth, shares, stream);
         }
     }
     return rc;

@@ -1,0 +1,47 @@
+"""GPU: how near trivance_orthogonalize comes to its definition in 64 bits, held to what plain fp32
+products of the same matrices reach. Limits: orthogonalize_util."""
+
+import pytest
+
+import orthogonalize_util as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+KINDS = ["even", "steep", "falling", "strong", "thin"]
+
+
+def _measure(size, kind, dtype, coefficients=ref.QUINTIC, factor=1.0, eps=1e-7):
+    """The excess of every matrix of a call, with `near` as its size asks."""
+    import paper_2602_17254_amd as T
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(sum(size))
+    x = (factor * ref.spectrum(kind, size, g, "cuda")).to(TYPES[dtype])
+    out = torch.empty_like(x)
+    ws = torch.full((T.trivance_orthogonalize_workspace_bytes(*size),), 255, dtype=torch.uint8, device="cuda")
+    T.trivance_orthogonalize(x, out, ws, coefficients, 1.0, eps)
+    torch.cuda.synchronize()
+    near = ref.FAR_SUMS if min(size[1:]) >= 512 else ref.NEAR
+    worst = 0.0
+    for b in range(size[0]):
+        want = ref.steps(x[b], coefficients, 1.0, eps, torch.float64)
+        plain = ref.steps(x[b], coefficients, 1.0, eps, torch.float32)
+        worst = max(worst, ref.excess(out[b], want, plain, near))
+    print("[orthogonalize]", size, kind, dtype, "excess %.2f of the limit" % worst, flush=True)
+    return worst
+
+
+# one workgroup, strips, and the product kernels with little to fill their tiles; a limit that rests on chance wants many values
+SMALL = [(2, 64, 250), (1, 48, 3001), (3, 130, 77), (1, 257, 130), (2, 515, 300)]
+# single steps whose last product stands alone
+SQUARE = [(1, 600, 640), (3, 770, 515), (1, 1030, 1500)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", SMALL + SQUARE, ids=lambda s: "x".join(map(str, s)))
+def test_as_near_as_fp32_products(size, kind, dtype):
+    assert _measure(size, kind, dtype) <= 1.0
