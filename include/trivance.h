@@ -520,10 +520,10 @@ int64_t trivance_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int6
  *   coefficients  host array [steps][3].
  *   workspace     at least trivance_orthogonalize_workspace_bytes.
  *
- * The norm is a 64-bit sum. Matrices are held in 22 bits between products, which are summed in fp32: fp32
- * results are as near as fp32 products come (up to 1.3 times their error measured), and out is rounded
- * once. 16-bit results of large wide or tall matrices may come from products of up to three steps'
- * polynomials: the errors stay well below the rounding of out. Entries below 2^-36 of the norm are lost. A zero matrix gives zeros,
+ * The norm is a 64-bit sum. Matrices are held in two fp16 numbers, 22 bits and a sign, between products, which
+ * are summed in fp32, and out is rounded once: the error before that is 0.3 to 1.3 times that of plain
+ * fp32 products (measured; up to 1.7 times for matrices of few rows), whatever the type.
+ * Entries below 2^-36 of the norm are lost. A zero matrix gives zeros,
  * one that holds a NaN or an infinity gives NaN throughout.
  * batch, rows or cols == 0 does nothing.
  * Errors: EINVAL for unknown types, negative sizes, steps < 1, NULL pointers, eps negative or NaN, scale

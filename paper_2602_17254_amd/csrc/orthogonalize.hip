@@ -11,15 +11,17 @@
 // 22 bits together, and a product is three MFMA products hi hi + hi lo + lo hi in fp32 sums: fp32
 // accuracy for every spectrum at a third of the fp16 rate, five times the rate of fp32 MFMA. Small
 // entries, which lo holds with a fixed spacing, decide how near that comes: X, A and P are each held times
-// the largest power of two that their range allows, 2^15, 2^15 and 2^13 for the usual coefficients. fp32
-// results keep the sums of the small products apart too: five steps of 2176 x 1600 are 3.3e-6 off, fp32
-// products 3.2e-6. G enters scaled by a power
+// the largest power of two that their range allows, 2^15, 2^15 and 2^13 for the usual coefficients. The sums of
+// the small products are kept apart: five steps of 2176 x 1600 are 3.3e-6 off, fp32 products 3.2e-6. X is
+// formed in every step: a form that carried A <- A P P through three steps, at two thirds of the time,
+// lost the singular values whose squares fall into A's rounding (8.0e-6 off at 2048 x 8192, where this
+// one is 3.3e-6 and fp32 products 3.7e-6). G enters scaled by a power
 // of two, exactly where it has 16 bits; the rest of the norm goes into the first step's coefficients.
 //
 // What bounds it: the MFMA rate, for matrices of some hundred rows and more; below that the latency of the steps'
-// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 1.26 ms, 0.45 PFLOP/s
-// of the products' own and 0.55 to 0.9 of MFMA in each kernel; 1024 x 4096 0.29 ms; 512 x 512 fp32 0.14;
-// 64 x 2048 0.064; 64 x 256 0.039.
+// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 2.03 ms, 0.28 PFLOP/s
+// of the products' own and three times that of MFMA; 1024 x 4096 0.46 ms; 512 x 512 fp32 0.14;
+// 64 x 2048 0.062; 64 x 256 0.039.
 // Layout. X is kept both ways round, so that both operands of every product have their summed index
 // contiguous; sides are padded with zeros to whole tiles. A and A A are symmetric: only tiles on and
 // above the diagonal are computed and each is written to both places.
@@ -164,13 +166,11 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
     }
 }
 
-// Symmetric: A = X X', the polynomial in A, products of such matrices. The others: X times one of them, and the
-// last of these, which goes to the caller.
-enum class Product { kGram, kPolynomial, kSquare, kUpdate, kLast };
+// Symmetric: A = X X', the polynomial in A. The others: X times one of these, and the last of them, which
+// goes to the caller.
+enum class Product { kGram, kPolynomial, kUpdate, kLast };
 
-constexpr bool is_symmetric(Product p) {
-    return p == Product::kGram || p == Product::kPolynomial || p == Product::kSquare;
-}
+constexpr bool is_symmetric(Product p) { return p == Product::kGram || p == Product::kPolynomial; }
 
 template <typename T>
 struct Output {
@@ -317,10 +317,11 @@ __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, i
 }
 
 // The sums of a tile. Each matrix instruction rounds its sum, and there are three for each 32 values of the summed
-// index where one has the large terms. PRECISE, for fp32 results, spares the large sum the roundings of
+// index where one has the large terms. PRECISE spares the large sum the roundings of
 // the small terms: they have sums of their own, or where there are no registers for those (tiles of
 // 256), all the small terms come first and the operands' upper planes are read twice. Without it five
-// steps of 2176 x 1600 were 5.0e-6 off in place of 3.3e-6; for results in 16 bits that is nothing.
+// steps of 2176 x 1600 were 5.0e-6 off in place of 3.3e-6. Products with X0 from 16 bits do without: with a
+// single plane on one side there are two instructions, or one.
 template <Tile TILE, int LP, int RP, bool PRECISE, int MI, int NI>
 __device__ __forceinline__ void multiply_tile(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
                                               half8* stages, float4v (&acc)[MI][NI]) {
@@ -912,14 +913,9 @@ int workers_of(int tile, int64_t tiles, int64_t depth) {
     return 0.4 * all / w + 6.0 < 0.4 * std::ceil(rounds) * (depth / 64) ? (int)w : 0;
 }
 
-// How many products of each sort a call takes.
-struct Counts {
-    int grams, squares, updates;
-};
-
 // The pair that takes the least time by the measured rates, counting whole rounds of the 256 CUs and the
 // padding.
-Tiles tiles_of(int64_t batch, int64_t m, int64_t n, Counts count) {
+Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
     const auto cost = [&](int tile, int64_t tiles, int64_t depth, bool symmetric) {
         const double rate = tile == 256 ? 1.0 : tile == 128 ? 0.76 : 0.5;
         const bool share = symmetric && workers_of(tile, batch * tiles, depth);
@@ -935,8 +931,7 @@ Tiles tiles_of(int64_t batch, int64_t m, int64_t n, Counts count) {
             const Tiles t{s, u};
             const int64_t pm = padded(m, t.pad()), pn = padded(n, t.pad());
             const int64_t ms = pm / s, half = ms * (ms + 1) / 2;
-            const double c = count.grams * cost(s, half, pn, true) + count.squares * cost(s, half, pm, true) +
-                             count.updates * cost(u, pm / u * (pn / u), pm, false);
+            const double c = cost(s, half, pn, true) + cost(s, half, pm, true) + cost(u, pm / u * (pn / u), pm, false);
             if (c < least) {
                 least = c;
                 best = t;
@@ -945,48 +940,12 @@ Tiles tiles_of(int64_t batch, int64_t m, int64_t n, Counts count) {
     return best;
 }
 
-// Steps of which X is formed only once. Within a group A itself is carried on, A <- A P P, and the polynomials
-// multiply up, Q <- P Q: products of the smaller side instead of the larger. They keep what A
-// holds of a weak direction, its singular value squared, which is lost in the rounding of A sooner than
-// the value itself in that of X: the error of a weak direction grows by |b / a| times the squares of
-// the growth so far. Up to 256 it stays at that of fp32 steps for every spectrum measured, two or three steps
-// of the usual coefficients, but several times it for some; so fp32 matrices take single steps, and
-// 16-bit ones, whose own rounding is far larger, groups. These pay where the larger side is twice the
-// smaller or more and products are not too small to fill the GPU.
-constexpr int kMaxGroup = 3;
-
-int group_of(const float* k, int step, int steps, int dtype, int64_t m, int64_t n) {
-    if (dtype == TRIVANCE_F32 || n < 2 * m || m < 512) return 1;
-    double growth = 1.0, lost = 0.0;
-    int g = 0;
-    for (; g < kMaxGroup && step + g < steps; ++g) {
-        const double a = k[3 * (step + g)], b = k[3 * (step + g) + 1];
-        lost += std::fabs(b / a) * growth;
-        if (g > 0 && !(lost <= 256.0)) break;
-        growth *= a * a;
-    }
-    return g;
-}
-
-Counts counts_of(const float* k, int steps, int dtype, int64_t m, int64_t n) {
-    Counts c{0, 0, 0};
-    for (int s = 0; s < steps;) {
-        const int g = group_of(k, s, steps, dtype, m, n);
-        ++c.grams;
-        c.squares += 4 * g - 3;
-        ++c.updates;
-        s += g;
-    }
-    return c;
-}
-
-// The workspace: norm parts and first coefficients, then the planes of X and X' twice, of A and Q (twice
-// each), P and P P, and the parts of shared products. It has to serve every call of these sizes, so it is laid out
-// for the largest padding and for groups.
-constexpr int kSquares = 6, kMostPad = 256;
+// The workspace: norm parts and first coefficients, then the planes of X and X' twice, of A and P, and the parts
+// of shared products. It is laid out for the largest padding.
+constexpr int kMostPad = 256;
 
 struct Layout {
-    int64_t parts, first, x[2], xt[2], square[kSquares], shares, bytes;  // byte offsets
+    int64_t parts, first, x[2], xt[2], a, p, shares, bytes;  // byte offsets
     int64_t strip_parts[2], strip_planes;
     int64_t m, n;
     bool small;   // nothing else then
@@ -1024,7 +983,8 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
         w.x[i] = take(xs);
         w.xt[i] = take(xs);
     }
-    for (int64_t& q : w.square) q = take(as);
+    w.a = take(as);
+    w.p = take(as);
     int64_t most = 0;
     for (const int64_t tile : {64, 128}) {
         const int64_t ms = pm / tile;
@@ -1065,9 +1025,8 @@ int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float
     return launch_status();
 }
 
-// Which planes a product takes. kBoth: hi hi + hi lo + lo hi; kPrecise: with sums apart. kExact: X0 from 16 bits,
-// whose lower plane is zero.
-enum class Depth { kBoth, kPrecise, kExact };
+// Which planes a product takes: hi hi + hi lo + lo hi, or kExact: X0 from 16 bits, whose lower plane is zero.
+enum class Depth { kBoth, kExact };
 
 // A product by the call's tiles.
 template <Product KIND, typename T>
@@ -1081,43 +1040,30 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
     if (tile == 128) LAUNCH(k128, LP, RP, P);  \
     if (few) LAUNCH(k64Few, LP, RP, P);        \
     LAUNCH(k64, LP, RP, P)
-    constexpr bool kPlain = KIND == Product::kUpdate || KIND == Product::kLast;
     if constexpr (KIND == Product::kGram) {
         if (depth == Depth::kExact) {
             LAUNCH_SMALLER(1, 1, false);
         }
     }
-    if constexpr (kPlain && (KIND == Product::kUpdate || sizeof(T) == 2)) {
+    if constexpr (KIND == Product::kUpdate || (KIND == Product::kLast && sizeof(T) == 2)) {
         if (depth == Depth::kExact) {
             if (tile == 256) LAUNCH(k256, 2, 1, false);
             LAUNCH_SMALLER(2, 1, false);
         }
     }
-    if constexpr (KIND != Product::kSquare && (KIND != Product::kLast || sizeof(T) == 4)) {
-        if (depth == Depth::kPrecise) {
-            if constexpr (kPlain) {
-                if (tile == 256) LAUNCH(k256, 2, 2, true);
-            }
-            LAUNCH_SMALLER(2, 2, true);
-        }
+    if constexpr (!is_symmetric(KIND)) {
+        if (tile == 256) LAUNCH(k256, 2, 2, true);
     }
-    if constexpr (KIND != Product::kLast || sizeof(T) == 2) {
-        if constexpr (kPlain) {
-            if (tile == 256) LAUNCH(k256, 2, 2, false);
-        }
-        LAUNCH_SMALLER(2, 2, false);
-    }
+    LAUNCH_SMALLER(2, 2, true);
 #undef LAUNCH_SMALLER
 #undef LAUNCH
-    return TRIVANCE_EINVAL;
 }
 
 // The ranges that the coefficients give: the largest singular value of X in any step, from values in [0, 1] on,
-// and the largest factor of one, and the powers of two by which X, A, P, and products of two and three factors can
-// be held in fp16. The first step's factors may be doubled (what is left of the norm).
+// and the largest factor of one, and the powers of two by which X, A and P can be held in fp16. The first step's factors may be doubled (what is left of the norm).
 struct Ranges {
     bool ok;
-    int x, a, p[3];  // exponents
+    int x, a, p;  // exponents
 };
 
 Ranges ranges_of(const float* k, int steps) {
@@ -1129,31 +1075,30 @@ Ranges ranges_of(const float* k, int steps) {
         constexpr int kSamples = 256;
         for (int i = 0; i <= kSamples; ++i) {
             const double v = most * i / kSamples, p = std::fabs(a + v * v * (b + v * v * c));
-            if (!(p <= 15.0)) return {false, 0, 0, {}};
+            if (!(p <= 15.0)) return {false, 0, 0, 0};
             factor = std::fmax(factor, s == 0 ? 2.0 * p : p);
             next = std::fmax(next, p * v);
         }
         most = next * kMargin;
-        if (!(most <= 3.9)) return {false, 0, 0, {}};
+        if (!(most <= 3.9)) return {false, 0, 0, 0};
         all = std::fmax(all, most);
     }
     factor = std::fmax(factor, 1.0) * kMargin;
     const auto exponent = [](double bound) { return std::ilogb(60000.0 / bound); };
-    return {true, exponent(all), exponent(all * all),
-            {exponent(factor), exponent(factor * factor), exponent(factor * factor * factor)}};
+    return {true, exponent(all), exponent(all * all), exponent(factor)};
 }
 
 float power(int exponent) { return std::ldexp(1.0f, exponent); }
 
 template <typename T>
 int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, const Ranges& range, float scale,
-        float eps, const Layout& w, int dtype, void* workspace, hipStream_t stream) {
+        float eps, const Layout& w, void* workspace, hipStream_t stream) {
     const auto coefficients = [&](int s) {
-        return Coefficients{k[3 * s] * power(range.p[0]), k[3 * s + 1] * power(range.p[0] - range.a),
-                            k[3 * s + 2] * power(range.p[0] - 2 * range.a)};
+        return Coefficients{k[3 * s] * power(range.p), k[3 * s + 1] * power(range.p - range.a),
+                            k[3 * s + 2] * power(range.p - 2 * range.a)};
     };
     const float gram = power(range.a - 2 * range.x);
-    const SmallFactors factors{range.x, gram, power(-range.p[0]), scale * power(-range.p[0] - range.x)};
+    const SmallFactors factors{range.x, gram, power(-range.p), scale * power(-range.p - range.x)};
     if (w.small) {
         SmallSteps s;
         s.steps = steps;
@@ -1190,59 +1135,36 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
         }
         return launch_status();
     }
-    const Tiles tiles = tiles_of(batch, w.m, w.n, counts_of(k, steps, dtype, w.m, w.n));
+    const Tiles tiles = tiles_of(batch, w.m, w.n);
     const int m = (int)padded(w.m, tiles.pad()), n = (int)padded(w.n, tiles.pad());
     const auto planes = [&](int64_t offset, int64_t rows, int ld) {
         f16* hi = reinterpret_cast<f16*>(base + offset);
         return Planes{hi, hi + batch * rows * ld, rows * ld, ld};
     };
     float* shares = reinterpret_cast<float*>(base + w.shares);
-    Planes x[2], xt[2], a[2], q[2];
+    Planes x[2], xt[2];
     for (int i = 0; i < 2; ++i) {
         x[i] = planes(w.x[i], m, n);
         xt[i] = planes(w.xt[i], n, m);
-        a[i] = planes(w.square[i], m, m);
-        q[i] = planes(w.square[2 + i], m, m);
     }
-    const Planes next = planes(w.square[4], m, m), pp = planes(w.square[5], m, m);
+    const Planes a = planes(w.a, m, m), p = planes(w.p, m, m);
     split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(in, parts, nparts, x[0], xt[0], range.x, k0, eps,
                                                                     first);
     int rc = launch_status();
     const Output<f16> none{};
-    const auto square = [&](const Planes& l, const Planes& r, const Planes& c, float factor) {
-        return product<Product::kSquare>({l, r, m, m, m, c, c, factor, a[0], {}, nullptr}, none, batch,
-                                         tiles.symmetric, Depth::kBoth, shares, stream);
-    };
-    int turn = 0;  // of X
-    for (int s = 0; s < steps && !rc;) {
-        const int group = group_of(k, s, steps, dtype, w.m, w.n);
-        const Depth both = sizeof(T) == 4 ? Depth::kPrecise : Depth::kBoth;
-        const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : both;
-        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a[0], a[0], gram, a[0], {}, nullptr},
-                                     none, batch, tiles.symmetric, depth, shares, stream);
-        int at = 0, qt = 0;
-        for (int g = 0; g < group && !rc; ++g) {
-            const Planes p = g == 0 ? q[0] : next;
+    for (int s = 0; s < steps && !rc; ++s) {
+        const int turn = s % 2;  // of X
+        const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : Depth::kBoth;
+        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a, a, gram, a, {}, nullptr}, none, batch,
+                                     tiles.symmetric, depth, shares, stream);
+        if (!rc)
             rc = product<Product::kPolynomial>(
-                {a[at], a[at], m, m, m, p, p, 1.0f, a[at], coefficients(s + g), s + g == 0 ? first : nullptr}, none,
-                batch, tiles.symmetric, both, shares, stream);
-            if (g > 0 && !rc) {  // Q's scale is that of g + 1 factors
-                rc = square(p, q[qt], q[1 - qt], power(range.p[g] - range.p[0] - range.p[g - 1]));
-                qt = 1 - qt;
-            }
-            if (g + 1 < group && !rc) {  // A <- A (P P)
-                rc = square(p, p, pp, power(range.p[1] - 2 * range.p[0]));
-                if (!rc) rc = square(a[at], pp, a[1 - at], power(-range.p[1]));
-                at = 1 - at;
-            }
-        }
-        s += group;
+                {a, a, m, m, m, p, p, 1.0f, a, coefficients(s), s == 0 ? first : nullptr}, none, batch,
+                tiles.symmetric, Depth::kBoth, shares, stream);
         if (rc) break;
-        Operands update{q[qt], xt[turn], m, m, n, x[1 - turn], xt[1 - turn],
-                        power(-range.p[group - 1]), a[0], {}, nullptr};
-        if (s < steps) {
+        Operands update{p, xt[turn], m, m, n, x[1 - turn], xt[1 - turn], power(-range.p), a, {}, nullptr};
+        if (s + 1 < steps) {
             rc = product<Product::kUpdate>(update, none, batch, tiles.update, depth, shares, stream);
-            turn = 1 - turn;
         } else {
             update.factor *= scale * power(-range.x);
             rc = product<Product::kLast>(update, out, batch, tiles.update, depth, shares, stream);
@@ -1293,7 +1215,7 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
                        tall ? x_row_stride : 1, m, n},
                       {static_cast<T*>(out), out_batch_stride, tall ? 1 : out_row_stride,
                        tall ? out_row_stride : 1, m, n},
-                      batch, steps, coefficients, range, (float)scale, (float)eps, w, dtype, workspace, s);
+                      batch, steps, coefficients, range, (float)scale, (float)eps, w, workspace, s);
     };
     return dtype == TRIVANCE_F32 ? go(float{}) : dtype == TRIVANCE_BF16 ? go(bf16{}) : go(f16{});
 }

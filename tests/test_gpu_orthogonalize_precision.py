@@ -38,10 +38,12 @@ def _measure(size, kind, dtype, coefficients=ref.QUINTIC, factor=1.0, eps=1e-7):
 SMALL = [(2, 64, 250), (1, 48, 3001), (3, 130, 77), (1, 257, 130), (2, 515, 300)]
 # single steps whose last product stands alone
 SQUARE = [(1, 600, 640), (3, 770, 515), (1, 1030, 1500)]
+# the larger side twice the smaller or more
+WIDE = [(1, 600, 5000), (1, 1024, 4096), (1, 4100, 1030), (1, 2033, 8100)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("size", SMALL + SQUARE, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("size", SMALL + SQUARE + WIDE, ids=lambda s: "x".join(map(str, s)))
 def test_as_near_as_fp32_products(size, kind, dtype):
     assert _measure(size, kind, dtype) <= 1.0
