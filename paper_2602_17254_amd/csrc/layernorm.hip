@@ -47,7 +47,9 @@ __device__ __forceinline__ F row_sum(F x, F* slot) {
     return s;
 }
 
-// Both row sums of the backward pass with one barrier; `slots` alternate from row to row.
+// Both row sums of the backward pass with one barrier; `slots` alternate from each row of a workgroup to its next,
+// whatever their ranks: a row's barrier stands between the reads of the row before it and the writes of
+// the row after it.
 template <int LANES>
 __device__ __forceinline__ void row_sums(float& x, float& y, float2* slots) {
     x = lanes_sum<LANES <= 64 ? LANES : 64>(x);
@@ -287,11 +289,11 @@ __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1))
 #pragma unroll
             for (int k = 0; k < V; ++k) gammas[(j * LANES + lane) * V + k] = gamma[j][k];
     }
+    int turn = 0;  // goes on from one rank to the next: no barrier stands between their rows
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         const int64_t c = blockIdx.x, t1 = c * a.per;
         const int64_t t2 = t1 + a.per < a.tokens ? t1 + a.per : a.tokens;
         float dg[NV][V] = {}, db[NV][V] = {};
-        int turn = 0;
         struct Ahead {
             Some<T, V> x[NV], dy[NV];
             float mean, rstd;
@@ -389,6 +391,7 @@ __global__ __launch_bounds__(kWide) void norm_backward_long_kernel(Backward<T> a
     __shared__ float2 slots[2][kWide / 64];
     const float inv = 1.0f / (float)a.width;
     const int64_t i0 = (int64_t)threadIdx.x * V;
+    int turn = 0;  // goes on from one rank to the next
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         const int64_t c = blockIdx.x, t1 = c * a.per;
         const int64_t t2 = t1 + a.per < a.tokens ? t1 + a.per : a.tokens;
@@ -400,7 +403,6 @@ __global__ __launch_bounds__(kWide) void norm_backward_long_kernel(Backward<T> a
             if (dgamma) store_row<float, V>(dgamma, i, a.width, zero);
             if (dbeta) store_row<float, V>(dbeta, i, a.width, zero);
         }
-        int turn = 0;
         for (int64_t t = t1; t < t2; ++t) {
             const T* x = a.x + r * a.x_rank + t * a.x_token;
             const T* dy = a.dy + r * a.dy_rank + t * a.dy_token;

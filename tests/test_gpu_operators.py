@@ -584,6 +584,38 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("tokens,width", [(1, 1030), (3, 1030), (1, 2500), (1, 16400)])
+def test_layernorm_of_more_ranks_than_a_grid_has_rows(tokens, width):
+    """Workgroups that go on to another rank: the rows, and the gradients of every rank, have the bits that they
+    have in calls of fewer ranks."""
+    import paper_2602_17254_amd as T
+
+    ranks, dev = 65535 + 70, _gen(width + tokens)
+    # the rows of the workgroups' first and second ranks, and some between
+    some = list(range(70)) + [30000] + list(range(65535, ranks))
+    x = torch.empty((ranks, tokens, width), dtype=torch.bfloat16, device="cuda")
+    dy = torch.empty_like(x)
+    for t in (x, dy):
+        for part in t.split(8192):
+            part.copy_(torch.randn(part.shape, **dev))
+    dx = torch.empty_like(x)
+    gamma = 1 + 0.3 * torch.randn(width, **dev)
+    y = torch.empty_like(x)
+    mean, rstd = torch.empty((ranks, tokens), device="cuda"), torch.empty((ranks, tokens), device="cuda")
+    T.trivance_layernorm_forward(x, gamma, None, y, mean, rstd)
+    sums = torch.full((2, ranks, width), math.nan, device="cuda")
+    ws = torch.empty(T.trivance_layernorm_workspace_bytes(ranks, tokens, width), dtype=torch.uint8, device="cuda")
+    T.trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, sums[0], sums[1], ws)
+    x1, dy1, n = x[some].contiguous(), dy[some].contiguous(), len(some)
+    y1, dx1 = torch.empty_like(x1), torch.empty_like(x1)
+    m1, r1 = torch.empty((n, tokens), device="cuda"), torch.empty((n, tokens), device="cuda")
+    s1 = torch.full((2, n, width), math.nan, device="cuda")
+    T.trivance_layernorm_forward(x1, gamma, None, y1, m1, r1)
+    T.trivance_layernorm_backward(dy1, x1, gamma, m1, r1, dx1, s1[0], s1[1], ws)
+    assert torch.equal(mean[some], m1) and torch.equal(rstd[some], r1) and torch.equal(y[some], y1)
+    assert torch.equal(dx[some], dx1) and torch.equal(sums[:, some], s1)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_tensors_beyond_the_caches(dtype):
     """Large tensors take other loads and stores: every row has the bits that it has in a call of its rank alone,
