@@ -512,12 +512,12 @@ def trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, wor
     sp = _array(rstd, "rstd", (ranks, tokens), f32, dev)
     dgp, dgs = _rank_rows(dgamma, "dgamma", ranks, width, f32, dev)
     dbp, dbs = _rank_rows(dbeta, "dbeta", ranks, width, f32, dev)
-    if dgs and dbs and dgs != dbs:
+    if dgamma is not None and dbeta is not None and dgs != dbs:
         raise ValueError("the rows of dgamma and dbeta must be equally far apart")
     wp, wb = _workspace_args(workspace)
     _check(_lib().trivance_layernorm_backward(dyp, xp, gp, mp, sp, dxp, dgp, dbp, ranks, tokens, width,
                                               dyr, dyt, xr, xt, dxr, dxt,
-                                              dgs or dbs, dt, wt, wp, wb,
+                                              dbs if dgamma is None else dgs, dt, wt, wp, wb,
                                               _stream_ptr(stream)),
            "trivance_layernorm_backward")
 

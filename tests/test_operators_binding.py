@@ -1,0 +1,77 @@
+"""What the binding of the operators around the AllReduce hands to the library and what it refuses, without a
+GPU: host tensors that say they are on one, and a library that records its arguments."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2602_17254_amd as T
+
+B = T.binding
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that passes for one on GPU 0."""
+
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+def gpu(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+
+
+class Library:
+    """Takes every call, launches nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(B, "_lib", lambda: lib)
+    monkeypatch.setattr(B, "_stream_ptr", lambda stream: 0)
+    return lib
+
+
+def _backward(dgamma, dbeta):
+    x, s = gpu(4, 3, 8), gpu(4, 3)
+    T.trivance_layernorm_backward(x, x, None, s, s, x, dgamma, dbeta)
+
+
+GRAD_STRIDE = 17  # the place of grad_rank_stride among the C call's arguments
+
+
+def test_gradient_rows_with_strides_of_their_own(library):
+    apart, dense = gpu(4, 20)[:, :8], gpu(4, 8)
+    for dgamma, dbeta, stride in ((apart, gpu(4, 20)[:, 8:16], 20), (apart, None, 20), (None, dense, 8)):
+        _backward(dgamma, dbeta)
+        assert library.calls[-1][1][GRAD_STRIDE] == stride
+    _backward(None, None)
+    for dgamma, dbeta in ((apart, dense), (dense, apart)):
+        with pytest.raises(ValueError):
+            _backward(dgamma, dbeta)
+
+
+def test_one_gradient_row_for_all_ranks_is_refused(library):
+    """A stride of zero is a stride: beside another it is unequal, and alone it reaches the library, which
+    refuses rows that overlap."""
+    one, rows = gpu(1, 8).expand(4, 8), gpu(4, 8)
+    for dgamma, dbeta in ((one, rows), (rows, one)):
+        with pytest.raises(ValueError):
+            _backward(dgamma, dbeta)
+    assert not library.calls
+    for dgamma, dbeta in ((one, None), (None, one), (one, one)):
+        _backward(dgamma, dbeta)
+        assert library.calls[-1][1][GRAD_STRIDE] == 0
