@@ -32,6 +32,7 @@
 
 #include "device.h"
 #include "operators.h"
+#include "orthogonalize_plan.h"
 
 namespace trivance {
 namespace {
@@ -485,8 +486,6 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, O
 // order, and leave each part of a tile's sum in memory, in the order of the registers; the part of
 // worker w in tile t is part t + w. 38 us for a product of 2048 x 2048 from 2048 (136 tiles, 2.7e10 flop, 0.72
 // PFLOP/s) and 11 to join its parts, 15 where the polynomial reads A as well.
-constexpr int kMostWorkers = 256;
-
 struct Shares {
     float* parts;
     int stages;   // of 64 values of the summed index, of all tiles
@@ -575,7 +574,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
 // whatever they compute. Instructions bound it, so a lane's places in the permuted rows are worked out
 // once: rows of a tile start at multiples of 16, and what a permutation takes from them is the lane's own. Five
 // steps of 64 x 256 take 39 us, of 64 x 64 20.
-constexpr int kSmallSide = 64, kSmallLong = 256, kSmallThreads = 1024;
+constexpr int kSmallThreads = 1024;
 
 struct SmallSteps {
     int steps;
@@ -823,8 +822,6 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
 // A, which they left in memory in the launch before; every workgroup adds all parts in order and
 // forms P for itself. Latency bounds it. 64 x 2048 takes 64 us, and 149 with the product kernels, whose only tile of A runs
 // through 2048 columns on one CU.
-constexpr int kMostStrips = 32;
-
 struct Strips {
     float* parts;  // [batch][strips][64 x 64], in the order of the registers: read; `made`: written
     float* made;
@@ -888,56 +885,6 @@ __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out
 #pragma unroll
     for (int q = 0; q < kStripPlanes; q += kSmallThreads)
         s.planes[strip * kStripPlanes + q + threadIdx.x] = local[q + threadIdx.x];
-}
-
-// The tiles of a call: of the symmetric products and of the others. Sides are padded to the larger.
-struct Tiles {
-    int symmetric, update;
-    int pad() const { return symmetric > update ? symmetric : update; }
-};
-
-int64_t padded(int64_t side, int tile) { return (side + tile - 1) / tile * tile; }
-
-// Over how many workgroups a symmetric product's stages are shared out; 0: a workgroup takes a tile. It leaves
-// no CU idle, and costs a launch and the parts' way through memory, 6 to 14 us. With tiles of 128 the
-// idle CUs of the last round decide: a round takes 30 us for 1000 values of the summed index. 136 tiles from
-// 2048 measured 60 us as they are and 53 shared out, from 8192 200 and 130. Tiles of 64 take 0.4 us for 64
-// values; a worker has 128 or more.
-int workers_of(int tile, int64_t tiles, int64_t depth) {
-    const int64_t all = tiles * (depth / 64);
-    if (all > INT32_MAX / 2) return 0;
-    const double rounds = tiles / 256.0;
-    if (tile == 128) return all >= kMostWorkers && (std::ceil(rounds) - rounds) * depth >= 512.0 ? kMostWorkers : 0;
-    if (tile != 64 || all < 4) return 0;
-    const int64_t w = all / 2 < kMostWorkers ? all / 2 : kMostWorkers;
-    return 0.4 * all / w + 6.0 < 0.4 * std::ceil(rounds) * (depth / 64) ? (int)w : 0;
-}
-
-// The pair that takes the least time by the measured rates, counting whole rounds of the 256 CUs and the
-// padding.
-Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
-    const auto cost = [&](int tile, int64_t tiles, int64_t depth, bool symmetric) {
-        const double rate = tile == 256 ? 1.0 : tile == 128 ? 0.76 : 0.5;
-        const bool share = symmetric && workers_of(tile, batch * tiles, depth);
-        const double rounds = share ? batch * tiles / 256.0 : (double)((batch * tiles + 255) / 256);
-        // in units of 1/720000 us; the second launch of shared products takes 10 us
-        return rounds * tile * tile * depth / rate + (share ? 7.2e6 : 0.0);
-    };
-    Tiles best{64, 64};
-    double least = INFINITY;
-    for (const int s : {64, 128})
-        for (const int u : {64, 128, 256}) {
-            if (u == 256 && m <= 128) continue;  // the workspace has no such padding
-            const Tiles t{s, u};
-            const int64_t pm = padded(m, t.pad()), pn = padded(n, t.pad());
-            const int64_t ms = pm / s, half = ms * (ms + 1) / 2;
-            const double c = cost(s, half, pn, true) + cost(s, half, pm, true) + cost(u, pm / u * (pn / u), pm, false);
-            if (c < least) {
-                least = c;
-                best = t;
-            }
-        }
-    return best;
 }
 
 // The workspace: norm parts and first coefficients, then the planes of X and X' twice, of A and P, and the parts
@@ -1004,24 +951,22 @@ bool allow_local(K kernel, size_t local) {
 }
 
 template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
-int launch_product(const Operands& o, const Output<T>& out, int64_t batch, float* parts, hipStream_t stream) {
+int launch_product(const Operands& o, const Output<T>& out, const ProductForm& form, float* parts, hipStream_t stream) {
     using S = Shape<TILE>;
-    constexpr bool kSymmetric = is_symmetric(KIND);
     constexpr size_t local = (size_t)2 * (LP + RP) * S::kSide * S::kDepth * sizeof(f16);
-    const int64_t tiles = batch * (kSymmetric ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols);
-    if constexpr (kSymmetric) {
-        if (const int workers = workers_of(S::kSide, tiles, o.depth)) {
+    if constexpr (is_symmetric(KIND)) {
+        if (form.workers) {
             const auto kernel = shared_product_kernel<TILE, LP, RP, PRECISE>;
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
-            const Shares s{parts, (int)tiles * (o.depth / 64), o.depth / 64, workers};
-            kernel<<<workers, kThreadsOf<TILE>, local, stream>>>(o, s);
-            join_product_kernel<KIND, TILE><<<(unsigned)(tiles * (S::kSide / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
+            const Shares s{parts, (int)form.tiles * (o.depth / 64), o.depth / 64, form.workers};
+            kernel<<<form.workers, kThreadsOf<TILE>, local, stream>>>(o, s);
+            join_product_kernel<KIND, TILE><<<(unsigned)(form.tiles * (S::kSide / S::kCols / 16)), kThreadsOf<TILE>, 0, stream>>>(o, s);
             return launch_status();
         }
     }
     const auto kernel = product_kernel<KIND, TILE, LP, RP, PRECISE, T>;
     if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
-    kernel<<<(unsigned)tiles, kThreadsOf<TILE>, local, stream>>>(o, out);
+    kernel<<<(unsigned)form.tiles, kThreadsOf<TILE>, local, stream>>>(o, out);
     return launch_status();
 }
 
@@ -1032,13 +977,13 @@ enum class Depth { kBoth, kExact };
 template <Product KIND, typename T>
 int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth depth, float* parts,
             hipStream_t stream) {
+    const ProductForm form = form_of(batch, o.rows, o.cols, o.depth, tile, is_symmetric(KIND));
     o.rows = o.rows / tile;
     o.cols = o.cols / tile;
-    const bool few = batch * (is_symmetric(KIND) ? (int64_t)o.rows * (o.rows + 1) / 2 : (int64_t)o.rows * o.cols) <= 256;
-#define LAUNCH(TILE, LP, RP, P) return launch_product<KIND, Tile::TILE, LP, RP, P>(o, out, batch, parts, stream)
+#define LAUNCH(TILE, LP, RP, P) return launch_product<KIND, Tile::TILE, LP, RP, P>(o, out, form, parts, stream)
 #define LAUNCH_SMALLER(LP, RP, P)              \
     if (tile == 128) LAUNCH(k128, LP, RP, P);  \
-    if (few) LAUNCH(k64Few, LP, RP, P);        \
+    if (form.few) LAUNCH(k64Few, LP, RP, P);   \
     LAUNCH(k64, LP, RP, P)
     if constexpr (KIND == Product::kGram) {
         if (depth == Depth::kExact) {

@@ -13,6 +13,33 @@ QUINTIC = ((3.4445, -4.7750, 2.0315),) * 5
 NEAR = 3.0  # times the plain form's error
 FAR_SUMS = 2.0  # the same from 512 rows on, where the sums' roundings weigh as much in both
 
+# A size for every way that a call can run (what tests/c/orthogonalize_plan.cpp prints), none of which fills its
+# tiles; some taller than wide.
+FORMS = {
+    "small": (2, 61, 250),
+    "strips": (1, 8100, 50),
+    "gram-64few polynomial-64few update-64few": (1, 65, 66),
+    "gram-64few polynomial-64few update-64": (64, 129, 66),
+    "gram-64few polynomial-64few update-128": (64, 67, 322),
+    "gram-64few-shared polynomial-64few update-64few": (1, 8193, 3),
+    "gram-64few-shared polynomial-64few update-64": (1, 33, 20003),
+    "gram-64few-shared polynomial-64few update-128": (3, 5452, 68),
+    "gram-64few-shared polynomial-64few update-256": (1, 193, 49365),
+    "gram-64 polynomial-64 update-64": (64, 130, 132),
+    "gram-64 polynomial-64 update-128": (16, 344, 332),
+    "gram-64-shared polynomial-64 update-64": (4, 673, 1290),
+    "gram-64-shared polynomial-64-shared update-64": (1, 1547, 2486),
+    "gram-128 polynomial-128 update-64": (8, 740, 656),
+    "gram-128 polynomial-128 update-128": (64, 193, 203),
+    "gram-128 polynomial-128 update-256": (64, 780, 197),
+    "gram-128-shared polynomial-128 update-64": (8, 509, 1054),
+    "gram-128-shared polynomial-128 update-128": (8, 917, 457),
+    "gram-128-shared polynomial-128 update-256": (8, 728, 1307),
+    "gram-128-shared polynomial-128-shared update-64": (1, 833, 1552),
+    "gram-128-shared polynomial-128-shared update-128": (1, 2413, 838),
+    "gram-128-shared polynomial-128-shared update-256": (3, 643, 5415),
+}
+
 
 def spectrum(kind, size, generator, device):
     b, m, n = size

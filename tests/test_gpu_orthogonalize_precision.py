@@ -47,3 +47,16 @@ WIDE = [(1, 600, 5000), (1, 1024, 4096), (1, 4100, 1030), (1, 2033, 8100)]
 @pytest.mark.parametrize("size", SMALL + SQUARE + WIDE, ids=lambda s: "x".join(map(str, s)))
 def test_as_near_as_fp32_products(size, kind, dtype):
     assert _measure(size, kind, dtype) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", ref.FORMS)
+def test_every_form(form, dtype):
+    assert _measure(ref.FORMS[form], "falling", dtype) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(1, 2176, 1600), (3, 1030, 1030), (1, 3990, 4010), (1, 8100, 2033)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_large(size, dtype):
+    assert _measure(size, "steep", dtype) <= 1.0
