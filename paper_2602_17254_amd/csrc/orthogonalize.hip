@@ -1,6 +1,6 @@
 // Orthogonalises matrices by Newton-Schulz products: X0 = G / (|G|_F + eps), and per step
 //
-//   A = X X'     P = a I + b A + c A A     X <- P X
+//   A = X X'     P = b A + c A A     X <- a X + P X
 //
 // on the smaller side of G (X = G' where G is taller than wide), so that every singular value s of X0
 // passes the odd polynomial a s + b s^3 + c s^5 of each step and the singular vectors stay.
@@ -11,16 +11,18 @@
 // 22 bits together, and a product is three MFMA products hi hi + hi lo + lo hi in fp32 sums: fp32
 // accuracy for every spectrum at a third of the fp16 rate, five times the rate of fp32 MFMA. Small
 // entries, which lo holds with a fixed spacing, decide how near that comes: X, A and P are each held times
-// the largest power of two that their range allows, 2^15, 2^15 and 2^13 for the usual coefficients. The sums of
-// the small products are kept apart: five steps of 2176 x 1600 are 3.3e-6 off, fp32 products 3.2e-6. X is
+// the largest power of two that their range allows, 2^15, 2^15 and 2^13 for the usual coefficients. a X, the largest
+// term of an early step, joins when the sum is done, which would round at its size in every addition
+// (one step of 4000 x 4000 fp32: 5 times the error of fp32 products with a in P, 0.6 times without). Five steps
+// are 0.5 to 0.8 times as far off as fp32 products from 512 rows on. X is
 // formed in every step: a form that carried A <- A P P through three steps, at two thirds of the time,
-// lost the singular values whose squares fall into A's rounding (8.0e-6 off at 2048 x 8192, where this
-// one is 3.3e-6 and fp32 products 3.7e-6). G enters scaled by a power
+// lost the singular values whose squares fall into A's rounding (2.2 times the error of fp32 products at
+// 2048 x 8192). G enters scaled by a power
 // of two, exactly where it has 16 bits; the rest of the norm goes into the first step's coefficients.
 //
 // What bounds it: the MFMA rate, for matrices of some hundred rows and more; below that the latency of the steps'
-// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 2.03 ms, 0.28 PFLOP/s
-// of the products' own and three times that of MFMA; 1024 x 4096 0.46 ms; 512 x 512 fp32 0.14;
+// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 2.07 ms, 0.27 PFLOP/s
+// of the products' own and three times that of MFMA; 1024 x 4096 0.47 ms; 512 x 512 fp32 0.14;
 // 64 x 2048 0.062; 64 x 256 0.039.
 // Layout. X is kept both ways round, so that both operands of every product have their summed index
 // contiguous; sides are padded with zeros to whole tiles. A and A A are symmetric: only tiles on and
@@ -53,7 +55,7 @@ struct Planes {
 };
 
 // Of a step, times the scales of what they multiply and make: P as stored is
-// a + b (A as stored) + c (the sums of products of A as stored).
+// b (A as stored) + c (the sums of products of A as stored), X as stored becomes a X + P X.
 struct Coefficients {
     float a, b, c;
 };
@@ -234,18 +236,20 @@ struct Operands {
     int rows, cols;  // tiles of C
     Planes c, ct;    // C and its transpose
     float factor;    // of the sums, from the scales of both operands to that of C
-    Planes a;        // of the polynomial
+    Planes own;      // what the sums join: A in the polynomial, X in an update; no lower plane: it is zero
     Coefficients k;
     const Coefficients* first;  // in place of k, for each matrix
+    float last;      // from X as stored to the caller's values
 };
 
 // A workgroup's tile: the sums over values d0 .. d1 of the summed index of rows i0 of L and j0 of R; d1 - d0 is a
 // multiple of 64, and a last stage of 128 may be half one. LP and RP: the planes that are not zero. While the
 // waves multiply one stage of the operands the next one is on its way into the other half of local
-// memory, so a stage has one barrier. The products with a lower plane go into `cross`, which may be `acc`.
-template <Tile TILE, int LP, int RP, bool UPPER, int MI, int NI>
+// memory, so a stage has one barrier. The small terms join the large ones' sums: sums of their own would take
+// the error from 0.6 to 0.4 times that of fp32 products, and 5% more time at 2048 x 8192.
+template <Tile TILE, int LP, int RP, int MI, int NI>
 __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
-                                         half8* stages, float4v (&acc)[MI][NI], float4v (&cross)[MI][NI]) {
+                                         half8* stages, float4v (&acc)[MI][NI]) {
     using S = Shape<TILE>;
     constexpr int kThreads = kThreadsOf<TILE>, kDepth = S::kDepth, kPieces = kDepth / 8;
     constexpr int kPlane = S::kSide * kPieces, kStage = (LP + RP) * kPlane;
@@ -308,37 +312,9 @@ __device__ __forceinline__ void multiply(const Operands& o, int64_t b, int i0, i
 #pragma unroll
                     for (int x = 0; x < MI; ++x)
 #pragma unroll
-                        for (int y = 0; y < NI; ++y) {
-                            if (!UPPER && pl + pr == 0) continue;
-                            float4v& sum = pl + pr ? cross[x][y] : acc[x][y];
-                            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[pr][y], l[pl][x], sum, 0, 0, 0);
-                        }
+                        for (int y = 0; y < NI; ++y)
+                            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[pr][y], l[pl][x], acc[x][y], 0, 0, 0);
         }
-    }
-}
-
-// The sums of a tile. Each matrix instruction rounds its sum, and there are three for each 32 values of the summed
-// index where one has the large terms. PRECISE spares the large sum the roundings of
-// the small terms: they have sums of their own, or where there are no registers for those (tiles of
-// 256), all the small terms come first and the operands' upper planes are read twice. Without it five
-// steps of 2176 x 1600 were 5.0e-6 off in place of 3.3e-6. Products with X0 from 16 bits do without: with a
-// single plane on one side there are two instructions, or one.
-template <Tile TILE, int LP, int RP, bool PRECISE, int MI, int NI>
-__device__ __forceinline__ void multiply_tile(const Operands& o, int64_t b, int i0, int j0, int d0, int d1,
-                                              half8* stages, float4v (&acc)[MI][NI]) {
-    if constexpr (!PRECISE) {
-        multiply<TILE, LP, RP, true>(o, b, i0, j0, d0, d1, stages, acc, acc);
-    } else if constexpr (TILE == Tile::k256) {
-        multiply<TILE, LP, RP, false>(o, b, i0, j0, d0, d1, stages, acc, acc);
-        __syncthreads();  // every wave has read the last stage
-        multiply<TILE, 1, 1, true>(o, b, i0, j0, d0, d1, stages, acc, acc);
-    } else {
-        float4v cross[MI][NI] = {};
-        multiply<TILE, LP, RP, true>(o, b, i0, j0, d0, d1, stages, acc, cross);
-#pragma unroll
-        for (int x = 0; x < MI; ++x)
-#pragma unroll
-            for (int y = 0; y < NI; ++y) acc[x][y] += cross[x][y];
     }
 }
 
@@ -361,13 +337,13 @@ template <Product KIND, int MI, typename T>
 __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, int64_t b, Coefficients k,
                                        int i, int j, bool mirrored, const float4v (&sum)[MI], f16* turn) {
     const int lane = threadIdx.x % 64;
-    half4 ah[MI], aw[MI];  // all on their way before the first store
-    if constexpr (KIND == Product::kPolynomial) {
+    half4 own[MI], low[MI] = {};  // all on their way before the first store
+    if constexpr (KIND != Product::kGram) {
 #pragma unroll
         for (int x = 0; x < MI; ++x) {
-            const int64_t at = b * o.a.batch + (int64_t)(i + x * 16) * o.a.ld + j;
-            ah[x] = *reinterpret_cast<const half4*>(o.a.hi + at);
-            aw[x] = *reinterpret_cast<const half4*>(o.a.lo + at);
+            const int64_t at = b * o.own.batch + (int64_t)(i + x * 16) * o.own.ld + j;
+            own[x] = *reinterpret_cast<const half4*>(o.own.hi + at);
+            if (o.own.lo) low[x] = *reinterpret_cast<const half4*>(o.own.lo + at);
         }
     }
 #pragma unroll
@@ -376,10 +352,11 @@ __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, 
         float v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if constexpr (KIND == Product::kPolynomial)
-                v[q] = k.b * ((float)ah[x][q] + (float)aw[x][q]) + k.c * sum[x][q] + (row == j + q ? k.a : 0.0f);
-            else
-                v[q] = sum[x][q] * o.factor;
+            if constexpr (KIND == Product::kGram) v[q] = sum[x][q] * o.factor;
+            else if constexpr (KIND == Product::kPolynomial)
+                v[q] = k.b * ((float)own[x][q] + (float)low[x][q]) + k.c * sum[x][q];
+            else v[q] = __builtin_fmaf(k.a, (float)own[x][q] + (float)low[x][q], sum[x][q] * o.factor);
+            if constexpr (KIND == Product::kLast) v[q] *= o.last;
         }
         if constexpr (KIND == Product::kLast) {
             T* to = out.x + b * out.batch + row * out.si + j * out.sj;
@@ -448,7 +425,7 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
 // C = L R', a workgroup a tile. Bound by the MFMA rate and what each stage waits for: P X at 2048 x 8192 from
 // 2048 takes 183 us with three products (2.1e11 flop, 1.13 PFLOP/s) and 155 with two (0.89): reading the
 // operands weighs more. With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
-template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
+template <Product KIND, Tile TILE, int LP, int RP, typename T>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
     constexpr bool kSymmetric = is_symmetric(KIND);
@@ -462,9 +439,9 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, O
     int ti = tile % o.rows, tj = tile / o.rows;
     if constexpr (kSymmetric) triangle(tile, ti, tj);
     float4v acc[MI][NI] = {};
-    multiply_tile<TILE, LP, RP, PRECISE>(o, b, ti * S::kSide, tj * S::kSide, 0, o.depth, stages, acc);
+    multiply<TILE, LP, RP>(o, b, ti * S::kSide, tj * S::kSide, 0, o.depth, stages, acc);
     Coefficients k = o.k;
-    if (KIND == Product::kPolynomial && o.first) k = o.first[b];
+    if (KIND != Product::kGram && o.first) k = o.first[b];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int i = ti * S::kSide + wave / S::kCols * (MI * 16) + lane % 16;
     const int j = tj * S::kSide + wave % S::kCols * (NI * 16) + lane / 16 * 4;
@@ -503,7 +480,7 @@ struct Shares {
     }
 };
 
-template <Tile TILE, int LP, int RP, bool PRECISE>
+template <Tile TILE, int LP, int RP>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void shared_product_kernel(Operands o, Shares s) {
     using S = Shape<TILE>;
     constexpr int MI = S::kSide / S::kRows / 16, NI = S::kSide / S::kCols / 16, kThreads = kThreadsOf<TILE>;
@@ -517,7 +494,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void shared_product_kernel(Operan
         int ti, tj;
         triangle(t % tiles, ti, tj);
         float4v acc[MI][NI] = {};
-        multiply_tile<TILE, LP, RP, PRECISE>(o, t / tiles, ti * S::kSide, tj * S::kSide, (at - t * s.depth) * 64,
+        multiply<TILE, LP, RP>(o, t / tiles, ti * S::kSide, tj * S::kSide, (at - t * s.depth) * 64,
                                              (stop - t * s.depth) * 64, stages, acc);
         float* part = s.parts + (int64_t)(t + w) * (S::kSide * S::kSide) + threadIdx.x * 4;
 #pragma unroll
@@ -584,7 +561,8 @@ struct SmallSteps {
 // From sums of products to what is stored, and to the caller's values.
 struct SmallFactors {
     int x;  // the exponent of X's scale
-    float gram, update, last;
+    float gram, update;
+    float last;  // of X as stored
 };
 
 // Matrices in local memory lie in panels of 64 columns: 8 pieces a row, permuted as a stage's.
@@ -653,6 +631,15 @@ __device__ __forceinline__ void local_store(LocalPlanes m, const LocalPlanes* t,
             reinterpret_cast<f16*>(t->lo)[too] = w[q];
         }
     }
+}
+
+// The tile's values, each lane its own four.
+__device__ __forceinline__ void local_load(LocalPlanes m, int i, int j, const LaneOffsets& at, float (&v)[4]) {
+    const int from = (j / 64 * m.panel + (i + at.row) * 8 + ((j % 64 + at.column) / 8 ^ at.flip)) * 8 + at.column % 8;
+    const half4 h = *reinterpret_cast<const half4*>(reinterpret_cast<const f16*>(m.hi) + from);
+    const half4 w = *reinterpret_cast<const half4*>(reinterpret_cast<const f16*>(m.lo) + from);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = (float)h[q] + (float)w[q];
 }
 
 // pieces of X (either way round) and of A or P in one plane
@@ -741,14 +728,14 @@ __device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a,
     acc[0] += cross[0];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        poly[c] = k.b * gram[c] + k.c * acc[0][c] + (ti + at.row == tj + at.column + c ? k.a : 0.0f);
+        poly[c] = k.b * gram[c] + k.c * acc[0][c];
     local_store(m.p, nullptr, ti, tj, at, poly);
     __syncthreads();
 }
 
-// X <- P X in local memory, or with `last` to the caller, whose columns begin at j0.
+// X <- a X + P X in local memory, or with `last` to the caller, whose columns begin at j0.
 template <typename T>
-__device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col, const LaneOffsets& at, bool last,
+__device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col, float a, const LaneOffsets& at, bool last,
                                              const Output<T>& out, int64_t b, int j0, SmallFactors f) {
     constexpr int kTiles = kSmallSide / 16;
     float4v next[kTiles] = {};
@@ -758,8 +745,9 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
 #pragma unroll
         for (int y = 0; y < kTiles; ++y) {
             float w[4];
+            local_load(m.x, y * 16, col, at, w);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) w[c] = next[y][c] * (last ? f.last : f.update);
+            for (int c = 0; c < 4; ++c) w[c] = __builtin_fmaf(a, w[c], next[y][c] * f.update) * (last ? f.last : 1.0f);
             if (!last) {
                 local_store(m.x, &m.xt, y * 16, col, at, w);
                 continue;
@@ -812,8 +800,9 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
     __syncthreads();
     const int ti = wave / kTiles * 16, tj = wave % kTiles * 16;  // the wave's tile of A and P
     for (int step = 0; step < s.steps; ++step) {
-        small_polynomial(m, small_gram(m, n, ti, tj, at), step == 0 ? first : s.k[step], f.gram, ti, tj, at);
-        small_update(m, n, wave * 16, at, step + 1 == s.steps, out, blockIdx.x, 0, f);
+        const Coefficients k = step == 0 ? first : s.k[step];
+        small_polynomial(m, small_gram(m, n, ti, tj, at), k, f.gram, ti, tj, at);
+        small_update(m, n, wave * 16, k.a, at, step + 1 == s.steps, out, blockIdx.x, 0, f);
     }
 }
 
@@ -878,7 +867,7 @@ __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out
     if (first) k = first[b];
     const int ti = wave / 4 * 16, tj = wave % 4 * 16;
     small_polynomial(m, a, k, f.gram, ti, tj, at);
-    small_update(m, kSmallLong, wave * 16, at, last, out, b, blockIdx.x * kSmallLong, f);
+    small_update(m, kSmallLong, wave * 16, k.a, at, last, out, b, blockIdx.x * kSmallLong, f);
     if (last) return;
     a = small_gram(m, kSmallLong, ti, tj, at);
     reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
@@ -950,13 +939,13 @@ bool allow_local(K kernel, size_t local) {
                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)local) == hipSuccess;
 }
 
-template <Product KIND, Tile TILE, int LP, int RP, bool PRECISE, typename T>
+template <Product KIND, Tile TILE, int LP, int RP, typename T>
 int launch_product(const Operands& o, const Output<T>& out, const ProductForm& form, float* parts, hipStream_t stream) {
     using S = Shape<TILE>;
     constexpr size_t local = (size_t)2 * (LP + RP) * S::kSide * S::kDepth * sizeof(f16);
     if constexpr (is_symmetric(KIND)) {
         if (form.workers) {
-            const auto kernel = shared_product_kernel<TILE, LP, RP, PRECISE>;
+            const auto kernel = shared_product_kernel<TILE, LP, RP>;
             if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
             const Shares s{parts, (int)form.tiles * (o.depth / 64), o.depth / 64, form.workers};
             kernel<<<form.workers, kThreadsOf<TILE>, local, stream>>>(o, s);
@@ -964,7 +953,7 @@ int launch_product(const Operands& o, const Output<T>& out, const ProductForm& f
             return launch_status();
         }
     }
-    const auto kernel = product_kernel<KIND, TILE, LP, RP, PRECISE, T>;
+    const auto kernel = product_kernel<KIND, TILE, LP, RP, T>;
     if (!allow_local(kernel, local)) return TRIVANCE_EHIP;
     kernel<<<(unsigned)form.tiles, kThreadsOf<TILE>, local, stream>>>(o, out);
     return launch_status();
@@ -980,32 +969,32 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
     const ProductForm form = form_of(batch, o.rows, o.cols, o.depth, tile, is_symmetric(KIND));
     o.rows = o.rows / tile;
     o.cols = o.cols / tile;
-#define LAUNCH(TILE, LP, RP, P) return launch_product<KIND, Tile::TILE, LP, RP, P>(o, out, form, parts, stream)
-#define LAUNCH_SMALLER(LP, RP, P)              \
-    if (tile == 128) LAUNCH(k128, LP, RP, P);  \
-    if (form.few) LAUNCH(k64Few, LP, RP, P);   \
-    LAUNCH(k64, LP, RP, P)
+#define LAUNCH(TILE, LP, RP) return launch_product<KIND, Tile::TILE, LP, RP>(o, out, form, parts, stream)
+#define LAUNCH_SMALLER(LP, RP)              \
+    if (tile == 128) LAUNCH(k128, LP, RP);  \
+    if (form.few) LAUNCH(k64Few, LP, RP);   \
+    LAUNCH(k64, LP, RP)
     if constexpr (KIND == Product::kGram) {
         if (depth == Depth::kExact) {
-            LAUNCH_SMALLER(1, 1, false);
+            LAUNCH_SMALLER(1, 1);
         }
     }
     if constexpr (KIND == Product::kUpdate || (KIND == Product::kLast && sizeof(T) == 2)) {
         if (depth == Depth::kExact) {
-            if (tile == 256) LAUNCH(k256, 2, 1, false);
-            LAUNCH_SMALLER(2, 1, false);
+            if (tile == 256) LAUNCH(k256, 2, 1);
+            LAUNCH_SMALLER(2, 1);
         }
     }
     if constexpr (!is_symmetric(KIND)) {
-        if (tile == 256) LAUNCH(k256, 2, 2, true);
+        if (tile == 256) LAUNCH(k256, 2, 2);
     }
-    LAUNCH_SMALLER(2, 2, true);
+    LAUNCH_SMALLER(2, 2);
 #undef LAUNCH_SMALLER
 #undef LAUNCH
 }
 
 // The ranges that the coefficients give: the largest singular value of X in any step, from values in [0, 1] on,
-// and the largest factor of one, and the powers of two by which X, A and P can be held in fp16. The first step's factors may be doubled (what is left of the norm).
+// and the largest factor that P takes it by, and the powers of two by which X, A and P can be held in fp16. The first step's factors may be doubled (what is left of the norm).
 struct Ranges {
     bool ok;
     int x, a, p;  // exponents
@@ -1021,7 +1010,8 @@ Ranges ranges_of(const float* k, int steps) {
         for (int i = 0; i <= kSamples; ++i) {
             const double v = most * i / kSamples, p = std::fabs(a + v * v * (b + v * v * c));
             if (!(p <= 15.0)) return {false, 0, 0, 0};
-            factor = std::fmax(factor, s == 0 ? 2.0 * p : p);
+            const double f = v * v * std::fabs(b + v * v * c);
+            factor = std::fmax(factor, s == 0 ? 2.0 * f : f);
             next = std::fmax(next, p * v);
         }
         most = next * kMargin;
@@ -1039,11 +1029,11 @@ template <typename T>
 int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, const Ranges& range, float scale,
         float eps, const Layout& w, void* workspace, hipStream_t stream) {
     const auto coefficients = [&](int s) {
-        return Coefficients{k[3 * s] * power(range.p), k[3 * s + 1] * power(range.p - range.a),
+        return Coefficients{k[3 * s], k[3 * s + 1] * power(range.p - range.a),
                             k[3 * s + 2] * power(range.p - 2 * range.a)};
     };
     const float gram = power(range.a - 2 * range.x);
-    const SmallFactors factors{range.x, gram, power(-range.p), scale * power(-range.p - range.x)};
+    const SmallFactors factors{range.x, gram, power(-range.p), scale * power(-range.x)};
     if (w.small) {
         SmallSteps s;
         s.steps = steps;
@@ -1100,20 +1090,20 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
     for (int s = 0; s < steps && !rc; ++s) {
         const int turn = s % 2;  // of X
         const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : Depth::kBoth;
-        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a, a, gram, a, {}, nullptr}, none, batch,
+        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a, a, gram, {}, {}, nullptr, 0.0f}, none, batch,
                                      tiles.symmetric, depth, shares, stream);
+        const Coefficients ks = coefficients(s);
+        const Coefficients* each = s == 0 ? first : nullptr;
         if (!rc)
-            rc = product<Product::kPolynomial>(
-                {a, a, m, m, m, p, p, 1.0f, a, coefficients(s), s == 0 ? first : nullptr}, none, batch,
-                tiles.symmetric, Depth::kBoth, shares, stream);
+            rc = product<Product::kPolynomial>({a, a, m, m, m, p, p, 1.0f, a, ks, each, 0.0f}, none, batch,
+                                               tiles.symmetric, Depth::kBoth, shares, stream);
         if (rc) break;
-        Operands update{p, xt[turn], m, m, n, x[1 - turn], xt[1 - turn], power(-range.p), a, {}, nullptr};
-        if (s + 1 < steps) {
-            rc = product<Product::kUpdate>(update, none, batch, tiles.update, depth, shares, stream);
-        } else {
-            update.factor *= scale * power(-range.x);
-            rc = product<Product::kLast>(update, out, batch, tiles.update, depth, shares, stream);
-        }
+        Planes own = x[turn];
+        if (depth == Depth::kExact) own.lo = nullptr;
+        const Operands update{p, xt[turn], m, m, n, x[1 - turn], xt[1 - turn], power(-range.p), own, ks, each,
+                              scale * power(-range.x)};
+        if (s + 1 < steps) rc = product<Product::kUpdate>(update, none, batch, tiles.update, depth, shares, stream);
+        else rc = product<Product::kLast>(update, out, batch, tiles.update, depth, shares, stream);
     }
     return rc;
 }

@@ -129,7 +129,7 @@ def simulated(g, coefficients, dtype, drop=None):
         lost = {kind: side for step, kind, side in [drop or (-1, "", "")] if step == i}
         q = planes(product(x, t(x), lost.get("gram", "")))
         s = product(q, t(q), lost.get("square", ""))
-        p = planes(a * torch.eye(len(s), dtype=torch.float64) + b * (q[0] + q[1]) + c * s)
-        v = product(p, x, lost.get("update", ""))
+        p = planes(b * (q[0] + q[1]) + c * s)
+        v = a * (x[0] + x[1]) + product(p, x, lost.get("update", ""))
         x = planes(v)
     return v.to(dtype)

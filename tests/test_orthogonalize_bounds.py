@@ -30,8 +30,8 @@ def test_two_planes_pass(size, kind):
 @pytest.mark.parametrize("what", ["gram", "square", "update"])
 @pytest.mark.parametrize("side", ["l", "r"])
 def test_a_plane_missing_anywhere_shows(step, what, side):
-    """In some spectrum: where A is small beside the identity, or a later step covers an error, a single one
-    has nothing to show. 16-bit results show those of the products with X."""
+    """In some spectrum: where P is small beside a, or a later step covers an error, a single one has nothing to
+    show. 16-bit results show those from the second step on."""
     worst = {torch.float32: 0.0, torch.bfloat16: 0.0}
     for size in SIZES:
         for kind in KINDS:
@@ -40,4 +40,4 @@ def test_a_plane_missing_anywhere_shows(step, what, side):
                 out = ref.simulated(x, ref.QUINTIC, dtype, (step, what, side))
                 worst[dtype] = max(worst[dtype], ref.excess(out, want, plain, ref.NEAR))
     assert worst[torch.float32] > 1.0
-    assert worst[torch.bfloat16] > 1.0 or what != "update"
+    assert worst[torch.bfloat16] > 1.0 or step == 0
