@@ -523,7 +523,7 @@ int64_t trivance_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int6
  * The norm is a 64-bit sum. Matrices are held in two fp16 numbers, 22 bits and a sign, between products, which
  * are summed in fp32, and out is rounded once: the error before that is 0.5 to 1.3 times that of plain
  * fp32 products (measured; up to 2 times for matrices of fewer than 16 rows), whatever the type.
- * Entries below 2^-36 of the norm are lost. A zero matrix gives zeros,
+ * That holds for norms far below eps too. Entries below 2^-36 of the norm are lost. A zero matrix gives zeros,
  * one that holds a NaN or an infinity gives NaN throughout.
  * batch, rows or cols == 0 does nothing.
  * Errors: EINVAL for unknown types, negative sizes, steps < 1, NULL pointers, eps negative or NaN, scale

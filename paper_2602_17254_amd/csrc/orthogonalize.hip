@@ -60,6 +60,23 @@ struct Coefficients {
     float a, b, c;
 };
 
+// Of one matrix: the first step's coefficients, and where its norm lies below eps, by which power of two X is
+// held larger than it is: held as it is, it would sink into the fixed spacing of lo (1e-3 off for norms of
+// 1e-14 and eps 1e-7).
+struct Start {
+    Coefficients k;
+    int shift;
+};
+
+// A step of matrices held 2^shift too large at the start. What the steps before this one and it itself
+// raise X by at most, 2^before and 2^after, is taken off until nothing is left, so that X stays near one.
+__device__ __forceinline__ int shift_left(int shift, int grown) { return shift > grown ? shift - grown : 0; }
+
+__device__ __forceinline__ Coefficients shifted(Coefficients k, int shift, int before, int after) {
+    const int s = shift_left(shift, before), t = shift_left(shift, after);
+    return {ldexpf(k.a, t - s), ldexpf(k.b, t - 3 * s), ldexpf(k.c, t - 5 * s)};
+}
+
 template <typename T>
 struct Input {
     const T* x;
@@ -100,15 +117,16 @@ __global__ __launch_bounds__(256) void norm_parts_kernel(Input<T> in, double* pa
 }
 
 // The power of two 2^e above the norm, and the first step's coefficients, which hold what is left of it:
-// zeros for a zero matrix, not a number where the norm is none.
-__device__ __forceinline__ void scale_of(double squares, Coefficients c, float eps, int& e, Coefficients& first) {
+// zeros for a zero matrix, not a number where the norm is none. `grown`: of the first step.
+__device__ __forceinline__ void scale_of(double squares, Coefficients c, double eps, int grown, int& e, Start& start) {
     const double norm = sqrt(squares);
     e = norm > 0.0 && norm < __builtin_inf() ? ilogb(norm) + 1 : 0;
     const double alpha = norm == 0.0 ? 0.0
                          : norm < __builtin_inf() ? ldexp(1.0, e) / (norm + eps)
                                                   : __builtin_nan("");
-    const double cube = alpha * alpha * alpha;
-    first = {(float)(c.a * alpha), (float)(c.b * cube), (float)(c.c * (cube * alpha * alpha))};
+    start.shift = alpha > 0.0 && alpha < 0.5 ? -ilogb(alpha) - 1 : 0;
+    const double first = ldexp(alpha, shift_left(start.shift, grown)), square = alpha * alpha;
+    start.k = {(float)(c.a * first), (float)(c.b * first * square), (float)(c.c * first * square * square)};
 }
 
 // X both ways round, scaled by 2^scale over the power of two above the norm and padded with zeros, and the
@@ -116,8 +134,8 @@ __device__ __forceinline__ void scale_of(double squares, Coefficients c, float e
 // bf16, 34 MB read and 67 written (3 TB/s, 3% of the call): stores of 128 bytes a row bound it.
 template <typename T>
 __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* parts, int nparts,
-                                                    Planes x, Planes xt, int scale, Coefficients c, float eps,
-                                                    Coefficients* first) {
+                                                    Planes x, Planes xt, int scale, Coefficients c, double eps,
+                                                    int grown, Start* start) {
     constexpr int V = kVec<T>, kRow = 64 + 8;
     __shared__ half8 tiles[2][64 * kRow / 8];
     const int64_t b = blockIdx.z;
@@ -126,10 +144,10 @@ __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* p
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     int e;
-    Coefficients mine;
-    scale_of(sum, c, eps, e, mine);
+    Start mine;
+    scale_of(sum, c, eps, grown, e, mine);
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-    if (i0 == 0 && j0 == 0 && threadIdx.x == 0) first[b] = mine;
+    if (i0 == 0 && j0 == 0 && threadIdx.x == 0) start[b] = mine;
     // rows and columns as in memory: X's, or those of its transpose
     const bool tall = in.sj != 1;
     const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0, rows = tall ? in.n : in.m, cols = tall ? in.m : in.n;
@@ -238,9 +256,18 @@ struct Operands {
     float factor;    // of the sums, from the scales of both operands to that of C
     Planes own;      // what the sums join: A in the polynomial, X in an update; no lower plane: it is zero
     Coefficients k;
-    const Coefficients* first;  // in place of k, for each matrix
-    float last;      // from X as stored to the caller's values
+    const Start* start;  // of each matrix
+    int before, after;   // what the steps raise X by; before < 0: the first one, whose coefficients are start's
+    int exponent;        // from X as stored to the caller's values
+    float last;
 };
+
+// A step's coefficients for one matrix, and what it is still held too large by after it.
+__device__ __forceinline__ Coefficients coefficients_of(const Operands& o, int64_t b, int& left) {
+    const Start s = o.start[b];
+    left = shift_left(s.shift, o.after);
+    return o.before < 0 ? s.k : shifted(o.k, s.shift, o.before, o.after);
+}
 
 // A workgroup's tile: the sums over values d0 .. d1 of the summed index of rows i0 of L and j0 of R; d1 - d0 is a
 // multiple of 64, and a last stage of 128 may be half one. LP and RP: the planes that are not zero. While the
@@ -335,7 +362,7 @@ constexpr int kTurn = 2 * 16 * kTurnRow<MI>;
 // the product is for, and its places. `mirrored`: in C's transpose too, through the wave's `turn`.
 template <Product KIND, int MI, typename T>
 __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, int64_t b, Coefficients k,
-                                       int i, int j, bool mirrored, const float4v (&sum)[MI], f16* turn) {
+                                       int left, int i, int j, bool mirrored, const float4v (&sum)[MI], f16* turn) {
     const int lane = threadIdx.x % 64;
     half4 own[MI], low[MI] = {};  // all on their way before the first store
     if constexpr (KIND != Product::kGram) {
@@ -356,7 +383,7 @@ __device__ __forceinline__ void finish(const Operands& o, const Output<T>& out, 
             else if constexpr (KIND == Product::kPolynomial)
                 v[q] = k.b * ((float)own[x][q] + (float)low[x][q]) + k.c * sum[x][q];
             else v[q] = __builtin_fmaf(k.a, (float)own[x][q] + (float)low[x][q], sum[x][q] * o.factor);
-            if constexpr (KIND == Product::kLast) v[q] *= o.last;
+            if constexpr (KIND == Product::kLast) v[q] = ldexpf(v[q], o.exponent - left) * o.last;
         }
         if constexpr (KIND == Product::kLast) {
             T* to = out.x + b * out.batch + row * out.si + j * out.sj;
@@ -440,8 +467,9 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, O
     if constexpr (kSymmetric) triangle(tile, ti, tj);
     float4v acc[MI][NI] = {};
     multiply<TILE, LP, RP>(o, b, ti * S::kSide, tj * S::kSide, 0, o.depth, stages, acc);
-    Coefficients k = o.k;
-    if (KIND != Product::kGram && o.first) k = o.first[b];
+    Coefficients k = {};
+    int left = 0;
+    if (KIND != Product::kGram) k = coefficients_of(o, b, left);
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int i = ti * S::kSide + wave / S::kCols * (MI * 16) + lane % 16;
     const int j = tj * S::kSide + wave % S::kCols * (NI * 16) + lane / 16 * 4;
@@ -455,7 +483,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, O
         float4v column[MI];
 #pragma unroll
         for (int x = 0; x < MI; ++x) column[x] = acc[x][y];
-        finish<KIND, MI, T>(o, out, b, k, i, j + y * 16, !kSymmetric || ti != tj, column, turn);
+        finish<KIND, MI, T>(o, out, b, k, left, i, j + y * 16, !kSymmetric || ti != tj, column, turn);
     }
 }
 
@@ -538,10 +566,11 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
                 for (int x = 0; x < MI; ++x) sum[x] += v[q][x];
             }
     }
-    Coefficients k = o.k;
-    if (KIND == Product::kPolynomial && o.first) k = o.first[b];
+    Coefficients k = {};
+    int left = 0;
+    if (KIND != Product::kGram) k = coefficients_of(o, b, left);
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    finish<KIND, MI>(o, Output<f16>{}, b, k, ti * S::kSide + wave / S::kCols * (MI * 16) + lane % 16,
+    finish<KIND, MI>(o, Output<f16>{}, b, k, left, ti * S::kSide + wave / S::kCols * (MI * 16) + lane % 16,
                      tj * S::kSide + wave % S::kCols * (NI * 16) + y * 16 + lane / 16 * 4, ti != tj, sum,
                      reinterpret_cast<f16*>(turns) + wave * kTurn<MI>);
 }
@@ -556,13 +585,15 @@ constexpr int kSmallThreads = 1024;
 struct SmallSteps {
     int steps;
     Coefficients k[kMaxSteps];
+    int grown[kMaxSteps + 1];  // before each step, and after the last
 };
 
 // From sums of products to what is stored, and to the caller's values.
 struct SmallFactors {
     int x;  // the exponent of X's scale
     float gram, update;
-    float last;  // of X as stored
+    int exponent;  // from X as stored to the caller's values
+    float last;
 };
 
 // Matrices in local memory lie in panels of 64 columns: 8 pieces a row, permuted as a stage's.
@@ -736,7 +767,7 @@ __device__ __forceinline__ void small_polynomial(const SmallLocal& m, float4v a,
 // X <- a X + P X in local memory, or with `last` to the caller, whose columns begin at j0.
 template <typename T>
 __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col, float a, const LaneOffsets& at, bool last,
-                                             const Output<T>& out, int64_t b, int j0, SmallFactors f) {
+                                             int left, const Output<T>& out, int64_t b, int j0, SmallFactors f) {
     constexpr int kTiles = kSmallSide / 16;
     float4v next[kTiles] = {};
     if (col < n) local_product<kTiles>(m.p, 0, m.xt, col, 0, at, next, next);
@@ -747,7 +778,10 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
             float w[4];
             local_load(m.x, y * 16, col, at, w);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) w[c] = __builtin_fmaf(a, w[c], next[y][c] * f.update) * (last ? f.last : 1.0f);
+            for (int c = 0; c < 4; ++c) {
+                w[c] = __builtin_fmaf(a, w[c], next[y][c] * f.update);
+                if (last) w[c] = ldexpf(w[c], f.exponent - left) * f.last;
+            }
             if (!last) {
                 local_store(m.x, &m.xt, y * 16, col, at, w);
                 continue;
@@ -771,7 +805,7 @@ __device__ __forceinline__ void small_update(const SmallLocal& m, int n, int col
 // n: X's columns padded to whole panels.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Output<T> out, int n, SmallSteps s,
-                                                              SmallFactors f, float eps) {
+                                                              SmallFactors f, double eps) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     constexpr int kWaves = kSmallThreads / 64, kTiles = kSmallSide / 16;
@@ -794,15 +828,17 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) sum += sums[w];
     int e;
-    Coefficients first;
-    scale_of(sum, s.k[0], eps, e, first);
+    Start start;
+    scale_of(sum, s.k[0], eps, s.grown[1], e, start);
     small_split<kVec<T>>(m, in.sj != 1, n, f.x - e, v);
     __syncthreads();
     const int ti = wave / kTiles * 16, tj = wave % kTiles * 16;  // the wave's tile of A and P
     for (int step = 0; step < s.steps; ++step) {
-        const Coefficients k = step == 0 ? first : s.k[step];
+        const Coefficients k =
+            step == 0 ? start.k : shifted(s.k[step], start.shift, s.grown[step], s.grown[step + 1]);
         small_polynomial(m, small_gram(m, n, ti, tj, at), k, f.gram, ti, tj, at);
-        small_update(m, n, wave * 16, k.a, at, step + 1 == s.steps, out, blockIdx.x, 0, f);
+        small_update(m, n, wave * 16, k.a, at, step + 1 == s.steps, shift_left(start.shift, s.grown[step + 1]), out,
+                     blockIdx.x, 0, f);
     }
 }
 
@@ -822,8 +858,8 @@ constexpr int kStripPlanes = 4 * small_x(kSmallLong);  // pieces
 
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in, const double* norm, int nparts,
-                                                                    int scale, Coefficients k, float eps, Strips s,
-                                                                    Coefficients* first) {
+                                                                    int scale, Coefficients k, double eps, int grown,
+                                                                    Strips s, Start* start) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t b = blockIdx.y, strip = b * s.strips + blockIdx.x;
@@ -836,9 +872,9 @@ __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in,
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     int e;
-    Coefficients mine;
-    scale_of(sum, k, eps, e, mine);
-    if (blockIdx.x == 0 && threadIdx.x == 0) first[b] = mine;
+    Start mine;
+    scale_of(sum, k, eps, grown, e, mine);
+    if (blockIdx.x == 0 && threadIdx.x == 0) start[b] = mine;
     small_split<kVec<T>>(m, in.sj != 1, kSmallLong, scale - e, v);
     __syncthreads();
     const float4v a = small_gram(m, kSmallLong, wave / 4 * 16, wave % 4 * 16, at);
@@ -850,8 +886,8 @@ __global__ __launch_bounds__(kSmallThreads) void strip_start_kernel(Input<T> in,
 
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out, Strips s, Coefficients k,
-                                                                   const Coefficients* first, bool last,
-                                                                   SmallFactors f) {
+                                                                   const Start* start, int before, int after,
+                                                                   bool last, SmallFactors f) {
     extern __shared__ half8 local[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t b = blockIdx.y, strip = b * s.strips + blockIdx.x;
@@ -864,10 +900,11 @@ __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out
     float4v a = {};
 #pragma unroll 8
     for (int q = 0; q < s.strips; ++q) a += parts[q * kSmallThreads];
-    if (first) k = first[b];
+    const Start mine = start[b];
+    k = before < 0 ? mine.k : shifted(k, mine.shift, before, after);
     const int ti = wave / 4 * 16, tj = wave % 4 * 16;
     small_polynomial(m, a, k, f.gram, ti, tj, at);
-    small_update(m, kSmallLong, wave * 16, k.a, at, last, out, b, blockIdx.x * kSmallLong, f);
+    small_update(m, kSmallLong, wave * 16, k.a, at, last, shift_left(mine.shift, after), out, b, blockIdx.x * kSmallLong, f);
     if (last) return;
     a = small_gram(m, kSmallLong, ti, tj, at);
     reinterpret_cast<float4v*>(s.made)[strip * kSmallThreads + threadIdx.x] = a;
@@ -876,16 +913,16 @@ __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out
         s.planes[strip * kStripPlanes + q + threadIdx.x] = local[q + threadIdx.x];
 }
 
-// The workspace: norm parts and first coefficients, then the planes of X and X' twice, of A and P, and the parts
+// The workspace: norm parts and what each matrix starts from, then the planes of X and X' twice, of A and P, and the parts
 // of shared products. It is laid out for the largest padding.
 constexpr int kMostPad = 256;
 
 struct Layout {
-    int64_t parts, first, x[2], xt[2], a, p, shares, bytes;  // byte offsets
+    int64_t parts, start, x[2], xt[2], a, p, shares, bytes;  // byte offsets
     int64_t strip_parts[2], strip_planes;
     int64_t m, n;
     bool small;   // nothing else then
-    int strips;   // 0: the product kernels; otherwise norm, first and strips only
+    int strips;   // 0: the product kernels; otherwise norm, start and strips only
 };
 
 Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
@@ -908,7 +945,7 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     const int64_t pm = padded(m, m > 128 ? kMostPad : 128), pn = padded(n, n > 128 ? kMostPad : 128);
     const int64_t xs = batch * pm * pn * 2 * (int64_t)sizeof(f16), as = batch * pm * pm * 2 * (int64_t)sizeof(f16);
     w.parts = take(batch * kNormParts * (int64_t)sizeof(double));
-    w.first = take(batch * (int64_t)sizeof(Coefficients));
+    w.start = take(batch * (int64_t)sizeof(Start));
     if (w.strips) {
         for (int64_t& p : w.strip_parts) p = take(batch * w.strips * kSmallSide * kSmallSide * (int64_t)sizeof(float));
         w.strip_planes = take(batch * w.strips * kStripPlanes * (int64_t)sizeof(half8));
@@ -994,50 +1031,63 @@ int product(Operands o, const Output<T>& out, int64_t batch, int tile, Depth dep
 }
 
 // The ranges that the coefficients give: the largest singular value of X in any step, from values in [0, 1] on,
-// and the largest factor that P takes it by, and the powers of two by which X, A and P can be held in fp16. The first step's factors may be doubled (what is left of the norm).
+// and the largest factor that P takes it by, and the powers of two by which X, A and P can be held in fp16.
+// The first step's factors may be doubled (what is left of the norm).
 struct Ranges {
     bool ok;
     int x, a, p;  // exponents
+    int grown[kMaxSteps + 1];  // singular values are raised by 2^grown at most before each step, and after the last
 };
 
 Ranges ranges_of(const float* k, int steps) {
     constexpr double kMargin = 1.01;  // between the samples, and the rounding of the products
-    double most = 1.0, all = 1.0, factor = 0.0;
+    double most = 1.0, all = 1.0, factor = 0.0, growth = 0.0;
+    Ranges r;
+    r.ok = false;
+    r.grown[0] = 0;
     for (int s = 0; s < steps; ++s) {
         const double a = k[3 * s], b = k[3 * s + 1], c = k[3 * s + 2];
-        double next = 0.0;
+        double next = 0.0, raised = 1.0;
         constexpr int kSamples = 256;
         for (int i = 0; i <= kSamples; ++i) {
             const double v = most * i / kSamples, p = std::fabs(a + v * v * (b + v * v * c));
-            if (!(p <= 15.0)) return {false, 0, 0, 0};
+            if (!(p <= 15.0)) return r;
             const double f = v * v * std::fabs(b + v * v * c);
             factor = std::fmax(factor, s == 0 ? 2.0 * f : f);
             next = std::fmax(next, p * v);
+            raised = std::fmax(raised, p * kMargin);
         }
+        growth += std::log2(raised);
+        r.grown[s + 1] = (int)std::ceil(growth);
         most = next * kMargin;
-        if (!(most <= 3.9)) return {false, 0, 0, 0};
+        if (!(most <= 3.9)) return r;
         all = std::fmax(all, most);
     }
     factor = std::fmax(factor, 1.0) * kMargin;
     const auto exponent = [](double bound) { return std::ilogb(60000.0 / bound); };
-    return {true, exponent(all), exponent(all * all), exponent(factor)};
+    r.ok = true;
+    r.x = exponent(all);
+    r.a = exponent(all * all);
+    r.p = exponent(factor);
+    return r;
 }
 
 float power(int exponent) { return std::ldexp(1.0f, exponent); }
 
 template <typename T>
 int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, const Ranges& range, float scale,
-        float eps, const Layout& w, void* workspace, hipStream_t stream) {
+        double eps, const Layout& w, void* workspace, hipStream_t stream) {
     const auto coefficients = [&](int s) {
         return Coefficients{k[3 * s], k[3 * s + 1] * power(range.p - range.a),
                             k[3 * s + 2] * power(range.p - 2 * range.a)};
     };
     const float gram = power(range.a - 2 * range.x);
-    const SmallFactors factors{range.x, gram, power(-range.p), scale * power(-range.x)};
+    const SmallFactors factors{range.x, gram, power(-range.p), -range.x, scale};
     if (w.small) {
         SmallSteps s;
         s.steps = steps;
         for (int i = 0; i < steps; ++i) s.k[i] = coefficients(i);
+        for (int i = 0; i <= steps; ++i) s.grown[i] = range.grown[i];
         const int n = (int)padded(w.n, 64);
         const size_t local = sizeof(half8) * (4 * small_x(n) + 4 * kSmallA);
         if (!allow_local(&small_kernel<T>, local)) return TRIVANCE_EHIP;
@@ -1046,7 +1096,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
     }
     char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
     double* parts = reinterpret_cast<double*>(base + w.parts);
-    Coefficients* first = reinterpret_cast<Coefficients*>(base + w.first);
+    Start* start = reinterpret_cast<Start*>(base + w.start);
     const unsigned nb = (unsigned)batch;
     const int rows = in.sj != 1 ? in.n : in.m;
     const int64_t pieces = (int64_t)rows * (((rows == in.n ? in.m : in.n) + 256 * kVec<T> - 1) / (256 * kVec<T>));
@@ -1060,13 +1110,14 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
         Strips s{reinterpret_cast<float*>(base + w.strip_parts[0]), reinterpret_cast<float*>(base + w.strip_parts[1]),
                  reinterpret_cast<half8*>(base + w.strip_planes), w.strips};
         const dim3 grid(w.strips, nb);
-        strip_start_kernel<T><<<grid, kSmallThreads, local, stream>>>(in, parts, nparts, range.x, k0, eps, s, first);
+        strip_start_kernel<T><<<grid, kSmallThreads, local, stream>>>(in, parts, nparts, range.x, k0, eps, range.grown[1], s,
+                                                                        start);
         for (int i = 0; i < steps; ++i) {
             float* read = s.made;
             s.made = s.parts;
             s.parts = read;
             strip_step_kernel<T><<<grid, kSmallThreads, local, stream>>>(
-                out, s, coefficients(i), i == 0 ? first : nullptr, i + 1 == steps, factors);
+                out, s, coefficients(i), start, i == 0 ? -1 : range.grown[i], range.grown[i + 1], i + 1 == steps, factors);
         }
         return launch_status();
     }
@@ -1084,24 +1135,24 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
     }
     const Planes a = planes(w.a, m, m), p = planes(w.p, m, m);
     split_kernel<T><<<dim3(n / 64, m / 64, nb), 256, 0, stream>>>(in, parts, nparts, x[0], xt[0], range.x, k0, eps,
-                                                                    first);
+                                                                    range.grown[1], start);
     int rc = launch_status();
     const Output<f16> none{};
     for (int s = 0; s < steps && !rc; ++s) {
         const int turn = s % 2;  // of X
         const Depth depth = s == 0 && sizeof(T) == 2 ? Depth::kExact : Depth::kBoth;
-        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a, a, gram, {}, {}, nullptr, 0.0f}, none, batch,
+        rc = product<Product::kGram>({x[turn], x[turn], n, m, m, a, a, gram, {}, {}, nullptr, 0, 0, 0, 0.0f}, none, batch,
                                      tiles.symmetric, depth, shares, stream);
         const Coefficients ks = coefficients(s);
-        const Coefficients* each = s == 0 ? first : nullptr;
+        const int before = s == 0 ? -1 : range.grown[s], after = range.grown[s + 1];
         if (!rc)
-            rc = product<Product::kPolynomial>({a, a, m, m, m, p, p, 1.0f, a, ks, each, 0.0f}, none, batch,
+            rc = product<Product::kPolynomial>({a, a, m, m, m, p, p, 1.0f, a, ks, start, before, after, 0, 0.0f}, none, batch,
                                                tiles.symmetric, Depth::kBoth, shares, stream);
         if (rc) break;
         Planes own = x[turn];
         if (depth == Depth::kExact) own.lo = nullptr;
-        const Operands update{p, xt[turn], m, m, n, x[1 - turn], xt[1 - turn], power(-range.p), own, ks, each,
-                              scale * power(-range.x)};
+        const Operands update{p, xt[turn], m, m, n, x[1 - turn], xt[1 - turn], power(-range.p), own, ks, start,
+                              before, after, -range.x, scale};
         if (s + 1 < steps) rc = product<Product::kUpdate>(update, none, batch, tiles.update, depth, shares, stream);
         else rc = product<Product::kLast>(update, out, batch, tiles.update, depth, shares, stream);
     }
@@ -1150,7 +1201,7 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
                        tall ? x_row_stride : 1, m, n},
                       {static_cast<T*>(out), out_batch_stride, tall ? 1 : out_row_stride,
                        tall ? out_row_stride : 1, m, n},
-                      batch, steps, coefficients, range, (float)scale, (float)eps, w, workspace, s);
+                      batch, steps, coefficients, range, (float)scale, eps, w, workspace, s);
     };
     return dtype == TRIVANCE_F32 ? go(float{}) : dtype == TRIVANCE_BF16 ? go(bf16{}) : go(f16{});
 }

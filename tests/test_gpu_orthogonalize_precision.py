@@ -62,3 +62,14 @@ def test_every_form(form, steps, dtype):
 def test_large(size, dtype):
     assert _measure(size, "falling", dtype, ref.QUINTIC[:1]) <= 1.0
     assert _measure(size, "steep", dtype) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 64, 250), (1, 48, 3001), (1, 130, 300), (1, 600, 1300)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("factor,eps", [(1e-8, 1e-7), (1e-10, 1e-7), (1e-13, 1e-7), (1e-17, 1e-7), (1e-30, 1e-20),
+                                        (1.0, 1e25)])
+def test_norms_far_below_eps(size, factor, eps, dtype):
+    """X starts far below one, and the steps raise it by their a."""
+    assert _measure(size, "falling", dtype, ref.QUINTIC, factor, eps) <= 1.0
+    assert _measure(size, "even", dtype, ((1.5, -0.5, 0.0),) * 12, factor, eps) <= 1.0
