@@ -527,7 +527,7 @@ int64_t trivance_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int6
  * one that holds a NaN or an infinity gives NaN throughout.
  * batch, rows or cols == 0 does nothing.
  * Errors: EINVAL for unknown types, negative sizes, steps < 1, NULL pointers, eps negative or NaN, scale
- * not finite, bad strides; EUNSUPPORTED for sides above 65536, more than 65535 matrices or 64 steps,
+ * not finite as an fp32 number, bad strides; EUNSUPPORTED for sides above 65536, more than 65535 matrices or 64 steps,
  * and coefficients that take a singular value in [0, 1] beyond 3.9 or a step's factor
  * a + b s^2 + c s^4 beyond 15 in size; ESIZE for the workspace; EHIP.
  */

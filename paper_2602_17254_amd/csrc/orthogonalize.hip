@@ -1178,7 +1178,7 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
                            int64_t out_row_stride, const float* coefficients, int steps, double scale,
                            double eps, int dtype, void* workspace, int64_t workspace_bytes,
                            void* stream) {
-    if (!is_float_type(dtype) || !coefficients || steps < 1 || !(eps >= 0.0) || !std::isfinite(scale))
+    if (!is_float_type(dtype) || !coefficients || steps < 1 || !(eps >= 0.0) || !std::isfinite((float)scale))
         return TRIVANCE_EINVAL;
     const int64_t need = trivance_orthogonalize_workspace_bytes(batch, rows, cols);
     if (need < 0) return (int)need;

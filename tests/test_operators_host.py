@@ -164,3 +164,8 @@ def test_binding_refuses_host_tensors():
         T.trivance_balance_backward(x, c, 2, x)
     with pytest.raises(TypeError):
         T.trivance_orthogonalize(x, x, None)
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e300, math.nan, -math.inf])
+def test_orthogonalize_refuses_scales_that_fp32_does_not_hold(scale):
+    assert orthogonalize(scale=scale) == EINVAL
