@@ -593,24 +593,19 @@ def trivance_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> 
 
 # a, b, c of five steps that bring singular values from [0.003, 1] to about [0.7, 1.2]
 QUINTIC_5 = ((3.4445, -4.7750, 2.0315),) * 5
-_HOST_COEFFICIENTS = {}
 
 
 def _coefficients(steps):
-    """The steps' coefficients as a host array (made once for each tuple of tuples)."""
-    key = steps if isinstance(steps, tuple) else None
-    try:
-        got = _HOST_COEFFICIENTS.get(key) if key is not None else None
-    except TypeError:  # a tuple of lists
-        key = got = None
-    if got is None:
-        flat = [float(v) for abc in steps for v in abc]
-        if len(flat) != 3 * len(steps):
-            raise ValueError("coefficients must be three numbers for each step")
-        got = (ctypes.c_float * max(len(flat), 1))(*flat), len(steps)
-        if key is not None and len(_HOST_COEFFICIENTS) < 64:
-            _HOST_COEFFICIENTS[key] = got
-    return got
+    """The steps' coefficients as a host array."""
+    if steps is QUINTIC_5:
+        return _HOST_QUINTIC_5
+    flat = [float(v) for abc in steps for v in abc]
+    if len(flat) != 3 * len(steps):
+        raise ValueError("coefficients must be three numbers for each step")
+    return (ctypes.c_float * max(len(flat), 1))(*flat), len(steps)
+
+
+_HOST_QUINTIC_5 = _coefficients(list(QUINTIC_5))
 
 
 def trivance_orthogonalize(x, out, workspace, coefficients=QUINTIC_5, scale=1.0, eps=1e-7,

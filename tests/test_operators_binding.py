@@ -75,3 +75,24 @@ def test_one_gradient_row_for_all_ranks_is_refused(library):
     for dgamma, dbeta in ((one, None), (None, one), (one, one)):
         _backward(dgamma, dbeta)
         assert library.calls[-1][1][GRAD_STRIDE] == 0
+
+
+COEFFICIENTS, STEPS = 9, 10  # their places among the arguments
+
+
+def _orthogonalize(library, steps):
+    x = gpu(1, 4, 4)
+    T.trivance_orthogonalize(x, x, gpu(8), steps)
+    args = library.calls[-1][1]
+    return list(args[COEFFICIENTS])[:3 * args[STEPS]]
+
+
+def test_coefficients_are_those_of_the_call(library):
+    """Also where the same numbers' objects held other values in the call before."""
+    a, b, c = (torch.tensor(v, dtype=torch.float64) for v in (3.0, -4.0, 2.0))
+    steps = ((a, b, c), (1.5, b, 0))
+    assert _orthogonalize(library, steps) == [3.0, -4.0, 2.0, 1.5, -4.0, 0.0]
+    b.fill_(-0.5)
+    assert _orthogonalize(library, steps) == [3.0, -0.5, 2.0, 1.5, -0.5, 0.0]
+    assert _orthogonalize(library, [[1, 2, 3]]) == [1.0, 2.0, 3.0]
+    assert len(_orthogonalize(library, T.QUINTIC_5)) == 15
