@@ -599,9 +599,9 @@ def _coefficients(steps):
     """The steps' coefficients as a host array."""
     if steps is QUINTIC_5:
         return _HOST_QUINTIC_5
-    flat = [float(v) for abc in steps for v in abc]
-    if len(flat) != 3 * len(steps):
+    if any(len(abc) != 3 for abc in steps):
         raise ValueError("coefficients must be three numbers for each step")
+    flat = [float(v) for abc in steps for v in abc]
     return (ctypes.c_float * max(len(flat), 1))(*flat), len(steps)
 
 

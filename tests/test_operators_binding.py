@@ -96,3 +96,10 @@ def test_coefficients_are_those_of_the_call(library):
     assert _orthogonalize(library, steps) == [3.0, -0.5, 2.0, 1.5, -0.5, 0.0]
     assert _orthogonalize(library, [[1, 2, 3]]) == [1.0, 2.0, 3.0]
     assert len(_orthogonalize(library, T.QUINTIC_5)) == 15
+
+
+@pytest.mark.parametrize("steps", [((1, 2), (3, 4, 5, 6)), ((1, 2, 3, 4),), ((1, 2),), [[1.0, 2.0, 3.0], []]], ids=str)
+def test_each_step_has_three_coefficients(library, steps):
+    with pytest.raises(ValueError):
+        _orthogonalize(library, steps)
+    assert not library.calls
