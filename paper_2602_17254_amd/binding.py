@@ -412,6 +412,29 @@ def trivance_cost_model(plan: Plan, bytes_per_rank: float, alpha: float = 0.0,
 # rank and may be slices of a buffer that an AllReduce sums.
 
 
+def _current_device():
+    try:
+        return _TORCH._C._cuda_getDevice()
+    except AttributeError:  # as in _stream_ptr
+        return _TORCH.cuda.current_device()
+
+
+def _device(t, name):
+    """The tensor's GPU, which has to be the current one: its stream takes the kernels."""
+    dev = t.get_device()
+    if dev != _current_device():
+        raise ValueError(f"{name} is on GPU {dev}, which is not the current device")
+    return dev
+
+
+def _work(workspace, device):
+    """(pointer, bytes) of a workspace on that GPU, (None, 0) for None."""
+    args = _workspace_args(workspace)
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"workspace must be on GPU {device}")
+    return args
+
+
 def _rows(t, name):
     """(pointer, rank stride, token stride, type, device) of a [ranks, tokens, width] tensor."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
@@ -424,7 +447,7 @@ def _rows(t, name):
     s0, s1, s2 = t.stride()
     if s2 != 1 and t.shape[2] > 1:
         raise ValueError(f"the values of a row of {name} must be consecutive")
-    return t.data_ptr(), s0, s1, dt, t.get_device()
+    return t.data_ptr(), s0, s1, dt, _device(t, name)
 
 
 def _rows_like(t, name, shape, dtype, device):
@@ -514,7 +537,7 @@ def trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, wor
     dbp, dbs = _rank_rows(dbeta, "dbeta", ranks, width, f32, dev)
     if dgamma is not None and dbeta is not None and dgs != dbs:
         raise ValueError("the rows of dgamma and dbeta must be equally far apart")
-    wp, wb = _workspace_args(workspace)
+    wp, wb = _work(workspace, dev)
     _check(_lib().trivance_layernorm_backward(dyp, xp, gp, mp, sp, dxp, dgp, dbp, ranks, tokens, width,
                                               dyr, dyt, xr, xt, dxr, dxt,
                                               dbs if dgamma is None else dgs, dt, wt, wp, wb,
@@ -553,7 +576,7 @@ def trivance_balance_counts(logits, chosen, counts, probs, workspace=None, mask=
     mp = _mask(mask, (ranks, tokens), dev)
     cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, dev)
     pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, dev)
-    wp, wb = _workspace_args(workspace)
+    wp, wb = _work(workspace, dev)
     _check(_lib().trivance_balance_counts(lp, ip, mp, cp, pp, ranks, tokens, experts, k, lr, lt,
                                           cs, ps, dt, it, wp, wb, _stream_ptr(stream)),
            "trivance_balance_counts")
@@ -564,7 +587,7 @@ def trivance_balance_loss(counts, probs, top_k: int, loss, scale=1.0, stream=Non
     if not isinstance(probs, _torch().Tensor) or not probs.is_cuda or probs.dim() != 2:
         raise TypeError("probs must be a two-dimensional CUDA (HIP) torch tensor")
     ranks, experts = probs.shape
-    dev = probs.get_device()
+    dev = _device(probs, "probs")
     pp, ps = _rank_rows(probs, "probs", ranks, experts, _TORCH.float32, dev)
     cp, cs = _rank_rows(counts, "counts", ranks, experts + 1, _TORCH.int32, dev)
     op = _array(loss, "loss", (ranks,), _TORCH.float32, dev)
@@ -616,7 +639,7 @@ def trivance_orthogonalize(x, out, workspace, coefficients=QUINTIC_5, scale=1.0,
     op, ob, orow = _rows_like(out, "out", x.shape, x.dtype, dev)
     batch, rows, cols = x.shape
     k, steps = _coefficients(coefficients)
-    wp, wb = _workspace_args(workspace)
+    wp, wb = _work(workspace, dev)
     _check(_lib().trivance_orthogonalize(xp, op, batch, rows, cols, xb, xr, ob, orow, k, steps, scale,
                                          eps, dt, wp, wb, _stream_ptr(stream)),
            "trivance_orthogonalize")

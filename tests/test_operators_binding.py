@@ -19,6 +19,11 @@ class OnGpu(torch.Tensor):
         return 0
 
 
+class OnOtherGpu(OnGpu):
+    def get_device(self):
+        return 1
+
+
 def gpu(*shape, dtype=torch.float32):
     return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
 
@@ -42,6 +47,7 @@ def library(monkeypatch):
     lib = Library()
     monkeypatch.setattr(B, "_lib", lambda: lib)
     monkeypatch.setattr(B, "_stream_ptr", lambda stream: 0)
+    monkeypatch.setattr(B, "_current_device", lambda: 0, raising=False)
     return lib
 
 
@@ -103,3 +109,32 @@ def test_each_step_has_three_coefficients(library, steps):
     with pytest.raises(ValueError):
         _orthogonalize(library, steps)
     assert not library.calls
+
+
+def _calls():
+    """Every call of the operators, as (name, call of its arguments, the arguments)."""
+    x, s, w, g = gpu(2, 3, 8), gpu(2, 3), gpu(8), gpu(2, 8)
+    counts, ids = gpu(2, 9, dtype=torch.int32), gpu(2, 3, 2, dtype=torch.int64)
+    return [("forward", T.trivance_layernorm_forward, [x, w, w, x, s, s]),
+            ("backward", T.trivance_layernorm_backward, [x, x, w, s, s, x, g, g, gpu(8)]),
+            ("counts", T.trivance_balance_counts, [x, ids, counts, g, gpu(8), s.bool()]),
+            ("loss", T.trivance_balance_loss, [counts, g, 2, gpu(2)]),
+            ("gradient", T.trivance_balance_backward, [x, counts, 2, x, s.bool(), 1.0, gpu(2)]),
+            ("orthogonalize", T.trivance_orthogonalize, [x, x, gpu(8)])]
+
+
+def test_tensors_of_several_gpus_are_refused(library):
+    """Any one tensor elsewhere, the workspace among them, and all of them on a GPU that is not the current
+    one, on whose stream the kernels would run."""
+    for name, call, args in _calls():
+        call(*args)
+        launched = len(library.calls)
+        tensors = [i for i, a in enumerate(args) if isinstance(a, torch.Tensor)]
+        for i in tensors:
+            other = list(args)
+            other[i] = args[i].as_subclass(OnOtherGpu)
+            with pytest.raises((TypeError, ValueError)):
+                call(*other)
+        with pytest.raises((TypeError, ValueError)):
+            call(*[a.as_subclass(OnOtherGpu) if i in tensors else a for i, a in enumerate(args)])
+        assert len(library.calls) == launched, name
