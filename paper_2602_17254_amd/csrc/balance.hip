@@ -32,13 +32,23 @@ constexpr int kMaxExperts = 4096;
 constexpr int64_t kMaxGridX = 1 << 20;
 constexpr int64_t kMaxGridY = 65535;
 
-// A row's logits, as fp32, become exp(x - max); returns their maximum's place in it, minus infinity where every
-// expert is excluded (all are zero then). Exponents are taken to base two: one multiplication and the
-// hardware's instruction, which is good to a unit in the last place.
+// exp(d) for d <= 0, to a few units in the last place at any distance from zero: two to the rounded product
+// t = d log2(e), times exp of what the rounding left, d - t ln 2, which two terms of its series hold. NaN stays;
+// below -104 the result is zero, and minus infinity would leave no number to correct with.
+__device__ __forceinline__ float exp_below(float d) {
+    constexpr float kLog2E = 1.44269504088896340736f;
+    constexpr float kLn2 = 0.69314718055994530942f;
+    constexpr float kLn2Low = (float)(0.69314718055994530942 - (double)kLn2);
+    d = __builtin_elementwise_maximum(d, -104.0f);
+    const float t = d * kLog2E, p = __builtin_amdgcn_exp2f(t);
+    const float left = __builtin_fmaf(-t, kLn2Low, __builtin_fmaf(-t, kLn2, d));
+    return __builtin_fmaf(p, left, p);
+}
+
+// A row's logits, as fp32, become exp(x - max); where every expert is excluded, by minus infinity, all are zero.
 template <typename T, int L, int NV>
 __device__ __forceinline__ void row_exp(float (&v)[NV][kVec<T>]) {
     constexpr int V = kVec<T>;
-    constexpr float kLog2E = 1.44269504088896340736f;
     float m = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -49,7 +59,7 @@ __device__ __forceinline__ void row_exp(float (&v)[NV][kVec<T>]) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[j][k] = __builtin_amdgcn_exp2f((v[j][k] - m) * kLog2E);
+        for (int k = 0; k < V; ++k) v[j][k] = exp_below(v[j][k] - m);
 }
 
 // One over a sum of exponentials; zero for the sum of none.

@@ -337,6 +337,30 @@ def test_balance_numbers_that_are_none_show():
                 assert bool(torch.isfinite(d[0, t]).all()) == (t not in (7, 9))
 
 
+@pytest.mark.parametrize("experts", [5, 64, 300])
+def test_balance_probabilities_far_below_the_largest(experts):
+    """Logits in steps of 2^-10, whose distance from the maximum fp32 holds exactly and which is 25 or more: the
+    sum is 1 but for a rounding or two, and a probability's relative error that of its exponential (4
+    units at most), of the sum, of a division and of a product, at any distance."""
+    import paper_2602_17254_amd as T
+
+    tokens, near = 400, 16 * ref.U
+    logits = torch.randint(-80 * 1024, -25 * 1024, (tokens, 1, experts), **_gen(experts)) / 1024
+    logits[:, :, experts // 2] = 0.0
+    chosen = torch.zeros((tokens, 1, 1), dtype=torch.int32, device="cuda")
+    counts = torch.empty((tokens, experts + 1), dtype=torch.int32, device="cuda")
+    probs = torch.empty((tokens, experts), device="cuda")
+    T.trivance_balance_counts(logits, chosen, counts, probs)
+    want = torch.softmax(logits.double(), 2)[:, 0]
+    ref.assert_within(probs, want, near * want, "probs")
+    d = torch.empty_like(logits)
+    T.trivance_balance_backward(logits, counts, 1, d, scale=1e6)
+    w = 1e6 * experts * counts[:, None, :experts].double() / counts[:, None, experts:].double() ** 2
+    p = want[:, None]
+    mean = (p * w).sum(2, keepdim=True)
+    ref.assert_within(d, p * (w - mean), 2 * near * p * (w + mean) + 1e-45, "dlogits")
+
+
 @pytest.mark.parametrize("experts", [8, 72, 300])
 def test_balance_gradient_of_the_sum_over_ranks_against_differences(experts):
     """Counts and sums through the framework's AllReduce; every rank's gradient is that of the loss over
