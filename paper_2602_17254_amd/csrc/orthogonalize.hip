@@ -914,13 +914,12 @@ __global__ __launch_bounds__(kSmallThreads) void strip_step_kernel(Output<T> out
 }
 
 // The workspace: norm parts and what each matrix starts from, then the planes of X and X' twice, of A and P, and the parts
-// of shared products. It is laid out for the largest padding.
-constexpr int kMostPad = 256;
-
+// of products that are shared.
 struct Layout {
     int64_t parts, start, x[2], xt[2], a, p, shares, bytes;  // byte offsets
     int64_t strip_parts[2], strip_planes;
     int64_t m, n;
+    Tiles tiles;
     bool small;   // nothing else then
     int strips;   // 0: the product kernels; otherwise norm, start and strips only
 };
@@ -941,9 +940,6 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    // tiles of 256 are taken where a side has that many
-    const int64_t pm = padded(m, m > 128 ? kMostPad : 128), pn = padded(n, n > 128 ? kMostPad : 128);
-    const int64_t xs = batch * pm * pn * 2 * (int64_t)sizeof(f16), as = batch * pm * pm * 2 * (int64_t)sizeof(f16);
     w.parts = take(batch * kNormParts * (int64_t)sizeof(double));
     w.start = take(batch * (int64_t)sizeof(Start));
     if (w.strips) {
@@ -952,6 +948,9 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
         w.bytes = at + 256;
         return w;
     }
+    w.tiles = tiles_of(batch, m, n);
+    const int64_t pm = padded(m, w.tiles.pad()), pn = padded(n, w.tiles.pad());
+    const int64_t xs = batch * pm * pn * 2 * (int64_t)sizeof(f16), as = batch * pm * pm * 2 * (int64_t)sizeof(f16);
     for (int i = 0; i < 2; ++i) {
         w.x[i] = take(xs);
         w.xt[i] = take(xs);
@@ -959,9 +958,9 @@ Layout layout_of(int64_t batch, int64_t rows, int64_t cols) {
     w.a = take(as);
     w.p = take(as);
     int64_t most = 0;
-    for (const int64_t tile : {64, 128}) {
-        const int64_t ms = pm / tile;
-        const int64_t bytes = (batch * ms * (ms + 1) / 2 + kMostWorkers) * tile * tile * (int64_t)sizeof(float);
+    for (const int64_t depth : {pn, pm}) {
+        const ProductForm f = form_of(batch, pm, pm, depth, w.tiles.symmetric, true);
+        const int64_t bytes = f.workers ? (f.tiles + f.workers) * f.tile * f.tile * (int64_t)sizeof(float) : 0;
         most = bytes > most ? bytes : most;
     }
     w.shares = take(most);
@@ -1121,7 +1120,7 @@ int run(Input<T> in, Output<T> out, int64_t batch, int steps, const float* k, co
         }
         return launch_status();
     }
-    const Tiles tiles = tiles_of(batch, w.m, w.n);
+    const Tiles tiles = w.tiles;
     const int m = (int)padded(w.m, tiles.pad()), n = (int)padded(w.n, tiles.pad());
     const auto planes = [&](int64_t offset, int64_t rows, int ld) {
         f16* hi = reinterpret_cast<f16*>(base + offset);

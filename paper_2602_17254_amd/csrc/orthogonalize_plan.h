@@ -49,7 +49,7 @@ inline Tiles tiles_of(int64_t batch, int64_t m, int64_t n) {
     double least = INFINITY;
     for (const int s : {64, 128})
         for (const int u : {64, 128, 256}) {
-            if (u == 256 && m <= 128) continue;  // the workspace has no such padding
+            if (u == 256 && m <= 128) continue;  // half of every tile and more would be padding
             const Tiles t{s, u};
             const int64_t pm = padded(m, t.pad()), pn = padded(n, t.pad());
             const int64_t ms = pm / s, half = ms * (ms + 1) / 2;

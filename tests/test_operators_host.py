@@ -169,3 +169,14 @@ def test_binding_refuses_host_tensors():
 @pytest.mark.parametrize("scale", [1e39, -1e300, math.nan, -math.inf])
 def test_orthogonalize_refuses_scales_that_fp32_does_not_hold(scale):
     assert orthogonalize(scale=scale) == EINVAL
+
+
+@pytest.mark.parametrize("size,shared", [((1, 512, 512), 0), ((4, 256, 512), 0), ((1, 2048, 8192), 136 + 256),
+                                         ((64, 256, 768), 0)], ids=str)
+def test_orthogonalize_workspace_holds_what_the_call_uses(size, shared):
+    """X both ways round twice and two products of its smaller side, in two fp16 numbers; where symmetric products
+    are shared (tiles of 128 here), a part for each tile and worker; norms and coefficients."""
+    b, m, n = size
+    need = b * (16 * m * n + 8 * m * m) + 4 * shared * 128 * 128
+    got = T.trivance_orthogonalize_workspace_bytes(*size)
+    assert need <= got <= need + b * (1024 * 8 + 16) + 4096
