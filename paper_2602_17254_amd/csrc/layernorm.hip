@@ -262,7 +262,9 @@ __device__ __forceinline__ float* sums_of(const Backward<T>& a, int64_t r, int64
 
 // Whether gamma stays in local memory, so that the registers suffice for two workgroups of 512 lanes on a CU, or four of
 // 256: some go on while others wait for their row's sums. With 256 lanes 2 x 8192 x 2200 bf16 takes 57 us in place of
-// 66, 8 x 4096 x 4096 161 in place of 166, 4 x 500 x 4000 18.6 in place of 18.0.
+// 66, 8 x 4096 x 2048 85 in place of 104, 8 x 4096 x 4096 161 in place of 166; sizes whose workgroups have
+// a few rows each lose up to 2%, as 4 x 500 x 4000 fp16 (20.8 in place of 20.4) and 16 x 128 x 1536 bf16
+// (14.0 in place of 13.8).
 template <int V, int LANES, int NV>
 constexpr bool kLocalGamma = (LANES == 256 || LANES == 512) && V == 8 && NV == 2;
 
@@ -533,13 +535,15 @@ int64_t imax(int64_t a, int64_t b) { return a > b ? a : b; }
 
 // The tokens that a chunk of the backward pass takes. Two workgroups a CU (512; one where a row takes 512
 // lanes), of four rows at least for each group of lanes, so that few tokens still spread over the GPU;
-// four a CU where each then has 8 rows or more, as each chunk's sums take a way through memory: 9 x 1001 x 2051 fp16
-// takes 36 us with 1008 workgroups and 39 with 504, 27 x 333 x 2500 41 with 999 and 40 with 486. A few
+// four a CU where each then has 16 rows or more, as each chunk's sums take a way through memory. With 8 rows
+// enough for that, 19 sizes between the two took 2% more in all: 8 x 1200 x 16000 bf16 262 us in place of 219,
+// 8 x 5000 x 768 bf16 51 in place of 44, 1 x 9000 x 4000 bf16 59 in place of 54; 1 x 16000 x 1100 bf16 46 in
+// place of 54 and 8 x 1500 x 1536 bf16 35 in place of 39, whose lanes' second vectors are void. A few
 // workgroups above a multiple of what the CUs hold would cost a round.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
     const int64_t rows = group_rows(s), wide = block_lanes(s) / kThreads;
     const int64_t many = imax(1, 1024 / ranks), few = imax(1, 512 / wide / ranks);
-    const int64_t chunks = imax(1, many * 8 * rows <= tokens ? many : imin(few, tokens / (4 * rows)));
+    const int64_t chunks = imax(1, many * 16 * rows <= tokens ? many : imin(few, tokens / (4 * rows)));
     const int64_t per = (tokens + chunks - 1) / chunks;
     return imax(rows, (per + rows - 1) / rows * rows);
 }
