@@ -33,16 +33,14 @@ constexpr int64_t kMaxGridX = 1 << 20;
 constexpr int64_t kMaxGridY = 65535;
 
 // exp(d) for d <= 0, to a few units in the last place at any distance from zero: two to the rounded product
-// t = d log2(e), times exp of what the rounding left, d - t ln 2, which two terms of its series hold. NaN stays;
-// below -104 the result is zero, and minus infinity would leave no number to correct with.
+// t = d log2(e), times exp of what the rounding left, d - t ln 2, which two terms of its series hold (ln 2's
+// own rounding adds 5 units at the far end). NaN stays; below -104 the result is zero, and minus
+// infinity would leave no number to correct with.
 __device__ __forceinline__ float exp_below(float d) {
-    constexpr float kLog2E = 1.44269504088896340736f;
-    constexpr float kLn2 = 0.69314718055994530942f;
-    constexpr float kLn2Low = (float)(0.69314718055994530942 - (double)kLn2);
+    constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
     d = __builtin_elementwise_maximum(d, -104.0f);
     const float t = d * kLog2E, p = __builtin_amdgcn_exp2f(t);
-    const float left = __builtin_fmaf(-t, kLn2Low, __builtin_fmaf(-t, kLn2, d));
-    return __builtin_fmaf(p, left, p);
+    return __builtin_fmaf(p, __builtin_fmaf(-t, kLn2, d), p);
 }
 
 // A row's logits, as fp32, become exp(x - max); where every expert is excluded, by minus infinity, all are zero.
