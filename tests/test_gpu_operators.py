@@ -608,6 +608,67 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(y, want)
 
 
+def _large(shape, seed):
+    """bf16 values drawn one rank at a time."""
+    t = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    dev = _gen(seed)
+    for part in t:
+        part.copy_(torch.randn(part.shape, **dev))
+    return t
+
+
+def test_layernorm_of_more_than_2_31_values():
+    import paper_2602_17254_amd as T
+
+    ranks, tokens, width = 8, 65537, 4100
+    x, dy = _large((ranks, tokens, width), 1), _large((ranks, tokens, width), 2)
+    assert x.numel() > 2 ** 31
+    gamma = 1 + 0.3 * torch.randn(width, **_gen(3))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty((ranks, tokens), device="cuda"), torch.empty((ranks, tokens), device="cuda")
+    sums = torch.full((2, ranks, width), math.nan, device="cuda")
+    ws = torch.empty(T.trivance_layernorm_workspace_bytes(ranks, tokens, width), dtype=torch.uint8, device="cuda")
+    T.trivance_layernorm_forward(x, gamma, None, y, mean, rstd)
+    T.trivance_layernorm_backward(dy, x, gamma, mean, rstd, dx, sums[0], sums[1], ws)
+    for r in (0, ranks - 1):
+        for part in (slice(0, 50), slice(tokens - 50, tokens)):
+            x1, dy1 = x[r:r + 1, part].contiguous(), dy[r:r + 1, part].contiguous()
+            y1, dx1 = torch.empty_like(x1), torch.empty_like(x1)
+            m1, r1 = torch.empty((1, 50), device="cuda"), torch.empty((1, 50), device="cuda")
+            T.trivance_layernorm_forward(x1, gamma, None, y1, m1, r1)
+            T.trivance_layernorm_backward(dy1, x1, gamma, m1, r1, dx1, None, None)
+            assert torch.equal(y[r:r + 1, part], y1) and torch.equal(mean[r:r + 1, part], m1)
+            assert torch.equal(dx[r:r + 1, part], dx1) and torch.equal(rstd[r:r + 1, part], r1)
+        d, h = dy[r].double(), (x[r].double() - mean[r, :, None].double()) * rstd[r, :, None].double()
+        n = (tokens + 40) * ref.U
+        ref.assert_within(sums[1, r], d.sum(0), n * d.abs().sum(0), "dbeta")
+        d *= h
+        ref.assert_within(sums[0, r], d.sum(0), n * d.abs().sum(0), "dgamma")
+
+
+def test_balance_of_more_than_2_31_values():
+    import paper_2602_17254_amd as T
+
+    ranks, tokens, experts, k = 8, 1048577, 257, 2
+    logits = _large((ranks, tokens, experts), 4)
+    assert logits.numel() > 2 ** 31
+    chosen = torch.randint(-1, experts, (ranks, tokens, k), **_gen(5))
+    counts = torch.empty((ranks, experts + 1), dtype=torch.int32, device="cuda")
+    probs = torch.full((ranks, experts), math.nan, device="cuda")
+    ws = torch.empty(T.trivance_balance_workspace_bytes(ranks, tokens, experts), dtype=torch.uint8, device="cuda")
+    T.trivance_balance_counts(logits, chosen, counts, probs, ws)
+    d = torch.empty_like(logits)
+    T.trivance_balance_backward(logits, counts, k, d, scale=1e6)
+    for r in (0, ranks - 1):
+        want, (wp, bp) = ref.balance_counts(logits[r:r + 1].double(), chosen[r:r + 1], None)
+        assert torch.equal(counts[r:r + 1].cpu().long(), want)
+        ref.assert_within(probs[r:r + 1], wp, bp, "probs")
+        near = logits[r:r + 1, -300:].contiguous()
+        d1 = torch.empty_like(near)
+        T.trivance_balance_backward(near, counts[r:r + 1], k, d1, scale=1e6)
+        assert torch.equal(d[r:r + 1, -300:], d1)
+
+
 @pytest.mark.parametrize("tokens,width", [(1, 1030), (3, 1030), (1, 2500), (1, 16400)])
 def test_layernorm_of_more_ranks_than_a_grid_has_rows(tokens, width):
     """Workgroups that go on to another rank: the rows, and the gradients of every rank, have the bits that they

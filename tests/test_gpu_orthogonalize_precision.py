@@ -73,3 +73,22 @@ def test_norms_far_below_eps(size, factor, eps, dtype):
     """X starts far below one, and the steps raise it by their a."""
     assert _measure(size, "falling", dtype, ref.QUINTIC, factor, eps) <= 1.0
     assert _measure(size, "even", dtype, ((1.5, -0.5, 0.0),) * 12, factor, eps) <= 1.0
+
+
+def test_more_than_2_31_values():
+    import paper_2602_17254_amd as T
+
+    size = (520, 2049, 2030)
+    x = torch.empty(size, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2 ** 31
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    for part in x:
+        part.copy_(ref.spectrum("falling", (1, *size[1:]), g, "cuda")[0])
+    out = torch.empty_like(x)
+    ws = torch.empty(T.trivance_orthogonalize_workspace_bytes(*size), dtype=torch.uint8, device="cuda")
+    T.trivance_orthogonalize(x, out, ws, ref.QUINTIC[:2])
+    for b in (0, 263, 519):
+        want = ref.steps(x[b], ref.QUINTIC[:2], 1.0, 1e-7, torch.float64)
+        plain = ref.steps(x[b], ref.QUINTIC[:2], 1.0, 1e-7, torch.float32)
+        assert ref.excess(out[b], want, plain, ref.FAR_SUMS) <= 1.0
