@@ -229,17 +229,20 @@ _TORCH = None
 _DTYPES = {}
 _FLOATS = {}  # the element types of activations, logits, weights and matrices
 _IDS = {}  # of expert numbers
+_current_device = None  # torch's call, without the checks of its public form where it has the private one
 
 
 def _torch():
     """The torch module, and the element types it maps to; imported on the first call."""
-    global _TORCH
+    global _TORCH, _current_device
     if _TORCH is None:
         import torch
 
         _DTYPES.update({torch.float32: F32, torch.int32: I32})
         _FLOATS.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
         _IDS.update({torch.int32: I32, torch.int64: I64})
+        if _current_device is None:
+            _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _TORCH = torch
     return _TORCH
 
@@ -412,13 +415,6 @@ def trivance_cost_model(plan: Plan, bytes_per_rank: float, alpha: float = 0.0,
 # rank and may be slices of a buffer that an AllReduce sums.
 
 
-def _current_device():
-    try:
-        return _TORCH._C._cuda_getDevice()
-    except AttributeError:  # as in _stream_ptr
-        return _TORCH.cuda.current_device()
-
-
 def _device(t, name):
     """The tensor's GPU, which has to be the current one: its stream takes the kernels."""
     dev = t.get_device()
@@ -429,8 +425,10 @@ def _device(t, name):
 
 def _work(workspace, device):
     """(pointer, bytes) of a workspace on that GPU, (None, 0) for None."""
+    if workspace is None:
+        return None, 0
     args = _workspace_args(workspace)
-    if workspace is not None and workspace.get_device() != device:
+    if workspace.get_device() != device:
         raise ValueError(f"workspace must be on GPU {device}")
     return args
 
