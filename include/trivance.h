@@ -403,7 +403,8 @@ int trivance_plan_with_dispatch_limit(const trivance_plan_t* plan, int64_t work_
  *   gamma, beta  device arrays of `width` values of weight_dtype; NULL means ones and zeros.
  *   mean, rstd   device fp32 arrays [ranks][tokens] for the backward pass; NULL: not written.
  *
- * Statistics are fp32 sums, y is rounded once. A row that holds a NaN or an infinity gives NaN.
+ * The mean is a 64-bit sum, the variance an fp32 one: rows whose values lie 1e19 or more from their mean give
+ * beta. y is rounded once. A row that holds a NaN or an infinity gives NaN.
  * tokens == 0 does nothing.
  * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, width outside [1, 2^24], eps negative or
  * NaN, NULL x or y, bad strides; EHIP.

@@ -12,8 +12,8 @@
 // exchanges between lanes. A lane holds the same experts of every row: a workgroup's sums of
 // probabilities add up in registers, its counts in local memory (integers: the order of
 // additions does not matter); a second kernel joins the workgroups' sums in a fixed order, in 64 bits.
-// Measured at 8 ranks of 32768 tokens: counts of 256 bf16 experts with two tokens in five unmasked, some 60 MB, 24
-// us and 4 to join; gradient of 256 fp32 experts, 537 MB, 93 us (5.8 TB/s).
+// Measured at 8 ranks of 32768 tokens: counts of 256 bf16 experts with two tokens in five unmasked, some 60 MB, 25
+// us and 5 to join; gradient of 256 fp32 experts, 537 MB, 93 us (5.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -99,7 +99,7 @@ struct Counts {
 // A chunk's tokens are those of every `chunks`th group of rows, so that padding at the end of a rank's tokens
 // leaves all workgroups the same work (28 us in place of 31 with contiguous chunks, at the size above). There the
 // rows take half the time and what stands before and after them, with the join, the other half; more rows
-// of a lane on their way at once were slower (30 us for two, 35 for four). With few tokens latency bounds it: 4.9 us
+// of a lane on their way at once were slower (30 us for two, 35 for four). With few tokens latency bounds it: 5.0 us
 // at 9 ranks of 512 tokens and 64 experts.
 template <typename T, int L, int NV>
 __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
@@ -339,8 +339,7 @@ int row_lanes(int experts, int vec) {
     return l;
 }
 
-// The most tokens of a chunk: enough chunks to fill the GPU, but four rows at least for each group of lanes;
-// so few that a chunk's slots are counted in 31 bits.
+// The most tokens of a chunk: enough chunks to fill the GPU, but four rows at least for each group of lanes.
 int64_t chunk_tokens(int64_t ranks, int64_t tokens, int lanes) {
     const int64_t rows = kThreads / lanes;
     const int64_t chunks = imax(1, imin((2048 + ranks - 1) / ranks, tokens / (4 * rows)));

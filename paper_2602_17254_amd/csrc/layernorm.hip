@@ -269,7 +269,7 @@ template <int V, int LANES, int NV>
 constexpr bool kLocalGamma = (LANES == 256 || LANES == 512) && V == 8 && NV == 2;
 
 // Bound by the bytes of x, dy and dx: 298 us at 8 x 4096 x 8192 bf16, 1.6 GB, 5.4 TB/s (and 67 MB of
-// workgroups' sums, which take another 11 us to join); 33 us and 6 at 9 x 1001 x 2051 fp16, 111 MB (3.3 TB/s). With few rows the
+// workgroups' sums, which take another 11 us to join); 36 us and 5 at 9 x 1001 x 2051 fp16, 111 MB (3.1 TB/s). With few rows the
 // latency of a lane's rows one after another bounds it: 8.6 us at 81 x 16 tokens of 768 fp32.
 template <typename T, int V, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1)) void norm_backward_kernel(Backward<T> a) {

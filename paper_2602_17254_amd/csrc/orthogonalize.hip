@@ -21,9 +21,9 @@
 // of two, exactly where it has 16 bits; the rest of the norm goes into the first step's coefficients.
 //
 // What bounds it: the MFMA rate, for matrices of some hundred rows and more; below that the latency of the steps'
-// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 2.07 ms, 0.27 PFLOP/s
-// of the products' own and three times that of MFMA; 1024 x 4096 0.47 ms; 512 x 512 fp32 0.14;
-// 64 x 2048 0.062; 64 x 256 0.039.
+// launches one after another, or of one workgroup's. Five steps measured: 2048 x 8192 bf16 2.05 ms, 0.27 PFLOP/s
+// of the products' own and 0.56 to 1.0 of MFMA in each kernel; 1024 x 4096 0.47 ms; 512 x 512 fp32 0.14;
+// 64 x 2048 0.066; 64 x 256 0.041.
 // Layout. X is kept both ways round, so that both operands of every product have their summed index
 // contiguous; sides are padded with zeros to whole tiles. A and A A are symmetric: only tiles on and
 // above the diagonal are computed and each is written to both places.
@@ -130,7 +130,7 @@ __device__ __forceinline__ void scale_of(double squares, Coefficients c, double 
 }
 
 // X both ways round, scaled by 2^scale over the power of two above the norm and padded with zeros, and the
-// first step's coefficients. A workgroup takes 64 x 64 values, read as they lie in memory. 33 us at 2048 x 8192
+// first step's coefficients. A workgroup takes 64 x 64 values, read as they lie in memory. 32 us at 2048 x 8192
 // bf16, 34 MB read and 67 written (3 TB/s, 3% of the call): stores of 128 bytes a row bound it.
 template <typename T>
 __global__ __launch_bounds__(256) void split_kernel(Input<T> in, const double* parts, int nparts,
@@ -449,9 +449,9 @@ __device__ __forceinline__ void triangle(int t, int& ti, int& tj) {
     ti = t - tj * (tj + 1) / 2;
 }
 
-// C = L R', a workgroup a tile. Bound by the MFMA rate and what each stage waits for: P X at 2048 x 8192 from
-// 2048 takes 183 us with three products (2.1e11 flop, 1.13 PFLOP/s) and 155 with two (0.89): reading the
-// operands weighs more. With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
+// C = L R', a workgroup a tile. Bound by the MFMA rate and what each stage waits for, and in an update by X's way to
+// memory and back: a X + P X at 2048 x 8192 takes 239 us with three products (2.1e11 flop, 0.86 PFLOP/s), 206 where
+// it goes to the caller alone (1.0), and 168 with two products, from X0 in 16 bits (0.82). With too few tiles latency does: 11 us for A of three matrices of 515 x 770, 135 tiles.
 template <Product KIND, Tile TILE, int LP, int RP, typename T>
 __global__ __launch_bounds__(kThreadsOf<TILE>) void product_kernel(Operands o, Output<T> out) {
     using S = Shape<TILE>;
@@ -579,7 +579,7 @@ __global__ __launch_bounds__(kThreadsOf<TILE>) void join_product_kernel(Operands
 // round, A and P, 160 KiB at the largest. The product kernels would take three launches a step of 4 us each,
 // whatever they compute. Instructions bound it, so a lane's places in the permuted rows are worked out
 // once: rows of a tile start at multiples of 16, and what a permutation takes from them is the lane's own. Five
-// steps of 64 x 256 take 39 us, of 64 x 64 20.
+// steps of 64 x 256 take 41 us.
 constexpr int kSmallThreads = 1024;
 
 struct SmallSteps {
@@ -845,7 +845,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(Input<T> in, Outpu
 // Matrices of up to 64 rows and some thousand columns: strips of 256 columns, each with a workgroup that keeps
 // it as the one above does, and one launch a step. What a step needs of the other strips is their part of
 // A, which they left in memory in the launch before; every workgroup adds all parts in order and
-// forms P for itself. Latency bounds it. 64 x 2048 takes 64 us, and 149 with the product kernels, whose only tile of A runs
+// forms P for itself. Latency bounds it. 64 x 2048 takes 66 us, and 149 with the product kernels, whose only tile of A runs
 // through 2048 columns on one CU.
 struct Strips {
     float* parts;  // [batch][strips][64 x 64], in the order of the registers: read; `made`: written
