@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
                                     : a.probs + r * a.probs_rank;
         int* counts = a.chunks > 1 ? a.part_counts + (r * a.chunks + c) * (a.experts + 1)
                                    : a.counts + r * a.counts_rank;
-        // the groups' sums in the groups' order, one vector of each lane at a time
+        // the groups' sums in the groups' order, up to 256 of them, in 64 bits; one vector of each lane at a time
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             __syncthreads();
@@ -180,9 +180,9 @@ __global__ __launch_bounds__(kThreads) void balance_counts_kernel(Counts<T> a) {
             for (int i = threadIdx.x; i < L * V; i += kThreads) {
                 const int e = j * L * V + i;
                 if (e >= a.experts) break;
-                float s = 0.0f;
+                double s = 0.0;
                 for (int g = 0; g < G; ++g) s += join[g * L * V + i];
-                probs[e] = s;
+                probs[e] = (float)s;
             }
         }
         for (int e = threadIdx.x; e <= a.experts; e += kThreads) counts[e] = hist[e];

@@ -337,6 +337,26 @@ def test_balance_numbers_that_are_none_show():
                 assert bool(torch.isfinite(d[0, t]).all()) == (t not in (7, 9))
 
 
+@pytest.mark.parametrize("experts", [3, 5, 7, 11, 100])
+def test_balance_sums_of_equal_probabilities(experts):
+    """Equal terms round the same way in a long sum. A lane adds four tokens here: four roundings, two of the
+    probability and one of the result; the lanes' sums are joined in 64 bits."""
+    import paper_2602_17254_amd as T
+
+    lanes = 1
+    while lanes * 4 < experts and lanes < 64:
+        lanes *= 2
+    tokens = 4 * 256 // lanes
+    logits = torch.zeros((1, tokens, experts), device="cuda")
+    chosen = torch.zeros((1, tokens, 1), dtype=torch.int32, device="cuda")
+    counts = torch.empty((1, experts + 1), dtype=torch.int32, device="cuda")
+    probs = torch.empty((1, experts), device="cuda")
+    ws = torch.empty(T.trivance_balance_workspace_bytes(1, tokens, experts), dtype=torch.uint8, device="cuda")
+    T.trivance_balance_counts(logits, chosen, counts, probs, ws)
+    want = torch.full((1, experts), tokens / experts, dtype=torch.float64, device="cuda")
+    ref.assert_within(probs, want, 7 * ref.U * want, "probs")
+
+
 @pytest.mark.parametrize("experts", [5, 64, 300])
 def test_balance_probabilities_far_below_the_largest(experts):
     """Logits in steps of 2^-10, whose distance from the maximum fp32 holds exactly and which is 25 or more: the
