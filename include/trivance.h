@@ -45,8 +45,9 @@ typedef enum {
     TRIVANCE_F32 = 0,
     TRIVANCE_I32 = 1,
     TRIVANCE_BF16 = 2, /* the 16-bit types and 64-bit integers are for the operators around the */
-    TRIVANCE_F16 = 3,  /* AllReduce (layer norm, balance loss, orthogonalisation); an AllReduce */
-    TRIVANCE_I64 = 4   /* takes F32 and I32                                                     */
+    TRIVANCE_F16 = 3,  /* AllReduce (norms, experts, embedding and the like); an AllReduce      */
+    TRIVANCE_I64 = 4,  /* takes F32 and I32                                                     */
+    TRIVANCE_E4M3 = 5  /* 8 bits, four of them exponent: a result of trivance_rmsnorm_forward    */
 } trivance_dtype;
 
 typedef enum {
@@ -537,6 +538,217 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
                            int64_t out_row_stride, const float* coefficients, int steps, double scale,
                            double eps, int dtype, void* workspace, int64_t workspace_bytes,
                            void* stream);
+
+/*
+ * trivance_rmsnorm_forward -- y = s rstd gamma for every row of s = x + residual, with
+ * rstd = 1 / sqrt(mean of the row's s^2 + eps).
+ *
+ *   x, residual  device rows of `dtype`; residual NULL: s = x.
+ *   gamma        device array of `width` values of weight_dtype; NULL means ones.
+ *   total        device rows of `dtype` for s, rounded; NULL: not written. It may be x or residual
+ *                (with the same strides). y comes from s before it is rounded.
+ *   y            device rows of y_dtype: `dtype`, and then y may be x or residual (with the same
+ *                strides, and not total's place too); or TRIVANCE_E4M3 (8-bit numbers up to 448,
+ *                strides in bytes), and then no input.
+ *   rstd         device fp32 array [ranks][tokens] for the backward pass; NULL: not written.
+ *   scales       device fp32 array [ranks][tokens], with TRIVANCE_E4M3 only: a row's largest |y| over
+ *                448, or 2^-126 where that is less; the row stands for y times its scale.
+ *
+ * Sums are in fp32: rows with values of 1e19 or more give zeros. A row that holds a NaN gives NaN; an
+ * infinity gives NaN in its place and zeros elsewhere, NaN throughout with TRIVANCE_E4M3.
+ * tokens == 0 does nothing.
+ * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, width outside [1, 2^24], eps negative or
+ * NaN, NULL x or y, y in total's place, scales without TRIVANCE_E4M3 or the other way round, bad
+ * strides; EHIP.
+ */
+int trivance_rmsnorm_forward(const void* x, const void* residual, const void* gamma, void* total,
+                             void* y, float* rstd, float* scales, int64_t ranks, int64_t tokens,
+                             int64_t width, int64_t x_rank_stride, int64_t x_token_stride,
+                             int64_t residual_rank_stride, int64_t residual_token_stride,
+                             int64_t total_rank_stride, int64_t total_token_stride,
+                             int64_t y_rank_stride, int64_t y_token_stride, double eps, int dtype,
+                             int y_dtype, int weight_dtype, void* stream);
+
+/* Workspace bytes of trivance_rmsnorm_backward for these sizes, for every dtype; 0 where a rank's
+ * tokens are summed in one piece. EINVAL for sizes that the call refuses. */
+int64_t trivance_rmsnorm_workspace_bytes(int64_t ranks, int64_t tokens, int64_t width);
+
+/*
+ * trivance_rmsnorm_backward -- the gradients of trivance_rmsnorm_forward. With h = s rstd and
+ * g = dy gamma:
+ *     dx = rstd (g - h mean(g h)) + dtotal            per row; the residual's gradient is the same
+ *     dgamma_r = sum over rank r's tokens of dy h
+ *
+ *   dy, total, dx  device rows of `dtype`; total is s as the forward pass wrote it (or x, where there
+ *                  was no residual). dx may be dy, total or dtotal (with the same strides).
+ *   gamma          as in the forward pass (NULL: ones).
+ *   rstd           what the forward pass wrote, [ranks][tokens].
+ *   dtotal         device rows of `dtype`, the gradient that reaches s by other ways than y; NULL: none.
+ *   dgamma         device fp32 rows of `width` values, one per rank, grad_rank_stride elements apart;
+ *                  NULL: not wanted. Written, not added to (zeros for a rank without tokens).
+ *   workspace      4-byte aligned, at least trivance_rmsnorm_workspace_bytes (unused, and may be NULL,
+ *                  where dgamma is NULL).
+ *
+ * Errors: those of the forward pass, EINVAL for NULL dy, total, rstd or dx, ESIZE for the workspace.
+ */
+int trivance_rmsnorm_backward(const void* dy, const void* total, const void* gamma, const float* rstd,
+                              const void* dtotal, void* dx, float* dgamma, int64_t ranks,
+                              int64_t tokens, int64_t width, int64_t dy_rank_stride,
+                              int64_t dy_token_stride, int64_t total_rank_stride,
+                              int64_t total_token_stride, int64_t dtotal_rank_stride,
+                              int64_t dtotal_token_stride, int64_t dx_rank_stride,
+                              int64_t dx_token_stride, int64_t grad_rank_stride, int dtype,
+                              int weight_dtype, void* workspace, int64_t workspace_bytes,
+                              void* stream);
+
+/* Workspace bytes of trivance_experts_sort for these sizes, for both types of numbers. EINVAL or
+ * EUNSUPPORTED for sizes that the call refuses. */
+int64_t trivance_experts_workspace_bytes(int64_t ranks, int64_t tokens, int64_t top_k,
+                                         int64_t experts);
+
+/*
+ * trivance_experts_sort -- where each rank's tokens lie once they are sorted by expert. A rank's slots,
+ * numbered token * top_k + j, are taken in the order of their experts, those of one expert in the order
+ * of their numbers; empty slots and those of masked tokens are left out.
+ *
+ *   chosen   device array [ranks][tokens][top_k] of id_dtype (TRIVANCE_I32 or TRIVANCE_I64), the chosen
+ *            experts; a value outside [0, experts) is an empty slot.
+ *   mask     device bytes [ranks][tokens]: a token whose byte is zero is left out. NULL: all count.
+ *   offsets  device int32 [ranks][experts + 1]: the first sorted row of each expert, then the number of
+ *            sorted rows.
+ *   places   device int32 [ranks][tokens][top_k]: each slot's sorted row, -1 for those left out.
+ *   slots    device int32 [ranks][tokens * top_k]: the slot of each sorted row, -1 behind the last;
+ *            NULL: not written.
+ *   workspace  4-byte aligned, at least trivance_experts_workspace_bytes.
+ *
+ * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, experts < 1, top_k < 1, more than 2^31 - 1
+ * slots over all ranks, NULL pointers; EUNSUPPORTED for more than 4096 experts; ESIZE for the
+ * workspace; EHIP.
+ */
+int trivance_experts_sort(const void* chosen, const uint8_t* mask, int32_t* offsets, int32_t* places,
+                          int32_t* slots, int64_t ranks, int64_t tokens, int64_t top_k,
+                          int64_t experts, int id_dtype, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
+/*
+ * trivance_experts_dispatch -- copies every token's row to the sorted rows of its slots:
+ *     rows[r][places[r][t][j]] = x[r][t].
+ *
+ *   x       device rows [ranks][tokens][width] of `dtype`.
+ *   places  as trivance_experts_sort wrote them; a place outside [0, capacity) is passed over. No two
+ *           slots of a rank share one.
+ *   rows    device rows [ranks][capacity][width]; those of no slot are left as they were. Not x.
+ *
+ * Errors: EINVAL for unknown types, sizes as in trivance_experts_sort, width outside [1, 2^24], capacity
+ * outside [0, 2^31 - 1], NULL pointers, bad strides; EHIP.
+ */
+int trivance_experts_dispatch(const void* x, const int32_t* places, void* rows, int64_t ranks,
+                              int64_t tokens, int64_t top_k, int64_t width, int64_t capacity,
+                              int64_t x_rank_stride, int64_t x_token_stride, int64_t rows_rank_stride,
+                              int64_t rows_row_stride, int dtype, void* stream);
+
+/*
+ * trivance_experts_combine -- the way back, and without weights the gradient of
+ * trivance_experts_dispatch: every token's weighted sum of its slots' rows,
+ *     y[r][t] = sum over j of weights[r][t][j] rows[r][places[r][t][j]].
+ *
+ *   rows, places  as in trivance_experts_dispatch; a slot whose place is passed over adds nothing.
+ *   weights       device array [ranks][tokens][top_k] of weight_dtype; NULL: ones.
+ *   y             device rows [ranks][tokens][width] of `dtype`, zeros for a token without a slot. Not
+ *                 rows.
+ *
+ * Sums are in fp32, in the order of j, rounded once.
+ * Errors: as trivance_experts_dispatch.
+ */
+int trivance_experts_combine(const void* rows, const int32_t* places, const void* weights, void* y,
+                             int64_t ranks, int64_t tokens, int64_t top_k, int64_t width,
+                             int64_t capacity, int64_t rows_rank_stride, int64_t rows_row_stride,
+                             int64_t y_rank_stride, int64_t y_token_stride, int dtype,
+                             int weight_dtype, void* stream);
+
+/*
+ * trivance_experts_combine_backward -- the gradients of trivance_experts_combine:
+ *     drows[r][places[r][t][j]] = weights[r][t][j] dy[r][t]
+ *     dweights[r][t][j] = dy[r][t] . rows[r][places[r][t][j]]     (zero for a slot that is passed over)
+ *
+ *   dy        device rows [ranks][tokens][width] of `dtype`.
+ *   drows     device rows [ranks][capacity][width]; those of no slot are left as they were. It may be
+ *             rows (with the same strides).
+ *   dweights  device fp32 [ranks][tokens][top_k].
+ *
+ * Errors: as trivance_experts_dispatch.
+ */
+int trivance_experts_combine_backward(const void* dy, const void* rows, const int32_t* places,
+                                      const void* weights, void* drows, float* dweights, int64_t ranks,
+                                      int64_t tokens, int64_t top_k, int64_t width, int64_t capacity,
+                                      int64_t dy_rank_stride, int64_t dy_token_stride,
+                                      int64_t rows_rank_stride, int64_t rows_row_stride,
+                                      int64_t drows_rank_stride, int64_t drows_row_stride, int dtype,
+                                      int weight_dtype, void* stream);
+
+/*
+ * trivance_embedding_forward -- y[r][t] = scale table[ids[r][t]], rows of a table that all ranks hold.
+ *
+ *   ids    device array [ranks][tokens] of id_dtype (TRIVANCE_I32 or TRIVANCE_I64); a value outside
+ *          [0, vocab) is padding and gives zeros.
+ *   table  device rows [vocab][width] of table_dtype, table_row_stride elements apart.
+ *   y      device rows [ranks][tokens][width] of `dtype`.
+ *
+ * scale is used as an fp32 number.
+ * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, more than 2^31 - 1 tokens over all ranks,
+ * width outside [1, 2^24], vocab < 1, NULL pointers, bad strides; EHIP.
+ */
+int trivance_embedding_forward(const void* ids, const void* table, void* y, int64_t ranks,
+                               int64_t tokens, int64_t width, int64_t vocab, int64_t table_row_stride,
+                               int64_t y_rank_stride, int64_t y_token_stride, double scale, int dtype,
+                               int table_dtype, int id_dtype, void* stream);
+
+/* Workspace bytes of trivance_embedding_backward for these sizes, for every type. EINVAL or EUNSUPPORTED
+ * for sizes that the call refuses. */
+int64_t trivance_embedding_workspace_bytes(int64_t ranks, int64_t tokens, int64_t width,
+                                           int64_t vocab);
+
+/*
+ * trivance_embedding_backward -- each rank's gradient of the table:
+ *     dtable[r][v] = scale (sum of dy[r][t] over the rank's tokens with ids[r][t] == v).
+ *
+ *   dy, ids    as y and ids of the forward pass; padding adds nothing, and its dy is not read.
+ *   dtable     device fp32 [vocab][width] of each rank, dtable_rank_stride elements apart; all of it is
+ *              written, not added to (zeros for numbers that no token has).
+ *   workspace  4-byte aligned, at least trivance_embedding_workspace_bytes.
+ *
+ * Sums go in the order of the tokens, in fp32, those of numbers that many tokens have in pieces that are
+ * joined in 64 bits.
+ * Errors: those of the forward pass; EUNSUPPORTED for vocab above 2^24; ESIZE for the workspace.
+ */
+int trivance_embedding_backward(const void* dy, const void* ids, float* dtable, int64_t ranks,
+                                int64_t tokens, int64_t width, int64_t vocab, int64_t dy_rank_stride,
+                                int64_t dy_token_stride, int64_t dtable_rank_stride, double scale,
+                                int dtype, int id_dtype, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+
+/*
+ * trivance_dropout -- y = residual + x keep / (1 - q), q being `rate` rounded to a multiple of 2^-16. The
+ * gradient of x is the same call on dy, without a residual and with the same state and rate.
+ *
+ *   x, residual, y  device rows of `dtype`; residual NULL: none. y may be x or residual (with the same
+ *                   strides). A dropped value counts as zero, whatever it is.
+ *   state           device array of two 64-bit numbers, 8-byte aligned: the seed, and the number of the
+ *                   call, of which the lower 32 bits count. It is read when the kernel runs, so a captured
+ *                   graph draws new values after the program has counted the call up.
+ *
+ * Value i of token t of rank r is kept where half i mod 2 (the lower first) of word (i mod 8) div 2 of a
+ * block of Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw 2011), key seed, counter (i div 8, t, r,
+ * call), is at least 65536 q: the kept places depend on nothing else.
+ * tokens == 0 does nothing.
+ * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, either above 2^32 - 1, width outside [1, 2^24],
+ * a rate outside [0, 1) or that rounds to 1, NULL or misaligned pointers, bad strides; EHIP.
+ */
+int trivance_dropout(const void* x, const void* residual, void* y, const uint64_t* state,
+                     int64_t ranks, int64_t tokens, int64_t width, int64_t x_rank_stride,
+                     int64_t x_token_stride, int64_t residual_rank_stride,
+                     int64_t residual_token_stride, int64_t y_rank_stride, int64_t y_token_stride,
+                     double rate, int dtype, void* stream);
 
 /* Static description of a status code. */
 const char* trivance_strerror(int status);

@@ -19,7 +19,8 @@ OBJDIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtrivance.so")
 
 HIP_SOURCES = ["executor.hip", "api.hip", "slot.hip", "fold.hip", "sweep.hip", "tile.hip", "congestion.hip", "fill.hip",
-               "layernorm.hip", "balance.hip", "orthogonalize.hip"]
+               "layernorm.hip", "balance.hip", "orthogonalize.hip",
+               "rmsnorm.hip", "experts.hip", "embedding.hip", "dropout.hip", "sort.hip"]
 CXX_SOURCES = ["plan.cpp", "cost.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -18,7 +18,7 @@ import numpy as np
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtrivance.so")
 
 LATENCY_OPT, BANDWIDTH_OPT, BRUCK_REF = 0, 1, 2
-F32, I32, BF16, F16, I64 = 0, 1, 2, 3, 4
+F32, I32, BF16, F16, I64, E4M3 = 0, 1, 2, 3, 4, 5
 ROUTE_SCHEDULED, ROUTE_SHORTEST = 0, 1
 PHASE_LATENCY, PHASE_REDUCE_SCATTER, PHASE_ALLGATHER = 0, 1, 2
 MAX_DIMS = 8
@@ -109,6 +109,23 @@ def _lib():
         "trivance_orthogonalize": (ctypes.c_int, [P] * 2 + [i64] * 7 +
                                    [ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_double,
                                     ctypes.c_double, ctypes.c_int, P, i64, P]),
+        "trivance_rmsnorm_forward": (ctypes.c_int, [P] * 7 + [i64] * 11 +
+                                     [ctypes.c_double, ctypes.c_int, ctypes.c_int, ctypes.c_int, P]),
+        "trivance_rmsnorm_workspace_bytes": (i64, [i64] * 3),
+        "trivance_rmsnorm_backward": (ctypes.c_int, [P] * 7 + [i64] * 12 +
+                                      [ctypes.c_int, ctypes.c_int, P, i64, P]),
+        "trivance_experts_workspace_bytes": (i64, [i64] * 4),
+        "trivance_experts_sort": (ctypes.c_int, [P] * 5 + [i64] * 4 + [ctypes.c_int, P, i64, P]),
+        "trivance_experts_dispatch": (ctypes.c_int, [P] * 3 + [i64] * 9 + [ctypes.c_int, P]),
+        "trivance_experts_combine": (ctypes.c_int, [P] * 4 + [i64] * 9 + [ctypes.c_int, ctypes.c_int, P]),
+        "trivance_experts_combine_backward": (ctypes.c_int, [P] * 6 + [i64] * 11 +
+                                              [ctypes.c_int, ctypes.c_int, P]),
+        "trivance_embedding_forward": (ctypes.c_int, [P] * 3 + [i64] * 7 +
+                                       [ctypes.c_double, ctypes.c_int, ctypes.c_int, ctypes.c_int, P]),
+        "trivance_embedding_workspace_bytes": (i64, [i64] * 4),
+        "trivance_embedding_backward": (ctypes.c_int, [P] * 3 + [i64] * 7 +
+                                        [ctypes.c_double, ctypes.c_int, ctypes.c_int, P, i64, P]),
+        "trivance_dropout": (ctypes.c_int, [P] * 4 + [i64] * 9 + [ctypes.c_double, ctypes.c_int, P]),
         "trivance_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     }
     for name, (res, args) in sig.items():
@@ -134,7 +151,12 @@ def exported_symbols() -> list:
              "trivance_layernorm_forward", "trivance_layernorm_workspace_bytes",
              "trivance_layernorm_backward", "trivance_balance_workspace_bytes",
              "trivance_balance_counts", "trivance_balance_loss", "trivance_balance_backward",
-             "trivance_orthogonalize_workspace_bytes", "trivance_orthogonalize"]
+             "trivance_orthogonalize_workspace_bytes", "trivance_orthogonalize",
+             "trivance_rmsnorm_forward", "trivance_rmsnorm_workspace_bytes", "trivance_rmsnorm_backward",
+             "trivance_experts_workspace_bytes", "trivance_experts_sort", "trivance_experts_dispatch",
+             "trivance_experts_combine", "trivance_experts_combine_backward",
+             "trivance_embedding_forward", "trivance_embedding_workspace_bytes",
+             "trivance_embedding_backward", "trivance_dropout"]
     return [n for n in names if hasattr(lib, n)]
 
 
@@ -228,7 +250,7 @@ def trivance_pass_bytes(plan: Plan, elems: int, pass_index: int, dtype: int = F3
 _TORCH = None
 _DTYPES = {}
 _FLOATS = {}  # the element types of activations, logits, weights and matrices
-_IDS = {}  # of expert numbers
+_IDS = {}  # of expert numbers and tokens' numbers
 _current_device = None  # torch's call, without the checks of its public form where it has the private one
 
 
@@ -641,3 +663,198 @@ def trivance_orthogonalize(x, out, workspace, coefficients=QUINTIC_5, scale=1.0,
     _check(_lib().trivance_orthogonalize(xp, op, batch, rows, cols, xb, xr, ob, orow, k, steps, scale,
                                          eps, dt, wp, wb, _stream_ptr(stream)),
            "trivance_orthogonalize")
+
+
+def trivance_rmsnorm_forward(x, gamma, y, rstd=None, residual=None, total=None, scales=None, eps=1e-5,
+                             stream=None) -> None:
+    """y = root-mean-square norm of the rows of x + residual [ranks, tokens, width] times gamma (None:
+    ones); total receives the rows' sum, rstd [ranks, tokens] the statistics for the backward pass. Where
+    y is float8_e4m3fn, scales [ranks, tokens] receives what its rows are to be multiplied by."""
+    xp, xr, xt, dt, dev = _rows(x, "x")
+    shape, dtype, f32 = x.shape, x.dtype, _TORCH.float32
+    ranks, tokens, width = shape
+    yd, yt = (dtype, dt) if scales is None else (_TORCH.float8_e4m3fn, E4M3)
+    yp, yr, ys = _rows_like(y, "y", shape, yd, dev)
+    rp, rr, rt = (None, 0, 0) if residual is None else _rows_like(residual, "residual", shape, dtype, dev)
+    tp, tr, tt = (None, 0, 0) if total is None else _rows_like(total, "total", shape, dtype, dev)
+    gp, _, wt = _weights(gamma, None, width, dev)
+    sp = _array(rstd, "rstd", (ranks, tokens), f32, dev)
+    cp = _array(scales, "scales", (ranks, tokens), f32, dev)
+    _check(_lib().trivance_rmsnorm_forward(xp, rp, gp, tp, yp, sp, cp, ranks, tokens, width, xr, xt, rr, rt,
+                                           tr, tt, yr, ys, eps, dt, yt, wt, _stream_ptr(stream)),
+           "trivance_rmsnorm_forward")
+
+
+def trivance_rmsnorm_workspace_bytes(ranks: int, tokens: int, width: int) -> int:
+    return _check(_lib().trivance_rmsnorm_workspace_bytes(ranks, tokens, width),
+                  "trivance_rmsnorm_workspace_bytes")
+
+
+def trivance_rmsnorm_backward(dy, total, gamma, rstd, dx, dgamma, workspace=None, dtotal=None,
+                              stream=None) -> None:
+    """dx, which is the gradient of x and of the residual, and each rank's dgamma [ranks, width] (fp32 rows,
+    or None), from dy, the gradient dtotal that reaches the sum by other ways (None: none), and the
+    forward pass's total (x, where there was no residual) and rstd."""
+    tp, tr, tt, dt, dev = _rows(total, "total")
+    shape, dtype, f32 = total.shape, total.dtype, _TORCH.float32
+    dyp, dyr, dyt = _rows_like(dy, "dy", shape, dtype, dev)
+    dxp, dxr, dxt = _rows_like(dx, "dx", shape, dtype, dev)
+    mp, mr, mt = (None, 0, 0) if dtotal is None else _rows_like(dtotal, "dtotal", shape, dtype, dev)
+    ranks, tokens, width = shape
+    gp, _, wt = _weights(gamma, None, width, dev)
+    sp = _array(rstd, "rstd", (ranks, tokens), f32, dev)
+    dgp, dgs = _rank_rows(dgamma, "dgamma", ranks, width, f32, dev)
+    wp, wb = _work(workspace, dev)
+    _check(_lib().trivance_rmsnorm_backward(dyp, tp, gp, sp, mp, dxp, dgp, ranks, tokens, width, dyr, dyt,
+                                            tr, tt, mr, mt, dxr, dxt, dgs, dt, wt, wp, wb,
+                                            _stream_ptr(stream)),
+           "trivance_rmsnorm_backward")
+
+
+def trivance_experts_workspace_bytes(ranks: int, tokens: int, top_k: int, experts: int) -> int:
+    return _check(_lib().trivance_experts_workspace_bytes(ranks, tokens, top_k, experts),
+                  "trivance_experts_workspace_bytes")
+
+
+def _numbers(t, name, dim):
+    """(pointer, type, device) of a contiguous int32 or int64 tensor."""
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
+    it = _IDS.get(t.dtype)
+    if it is None:
+        raise TypeError(f"{name} must be int32 or int64")
+    if t.dim() != dim or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and have {dim} dimensions")
+    return t.data_ptr(), it, _device(t, name)
+
+
+def trivance_experts_sort(chosen, offsets, places, workspace=None, mask=None, slots=None,
+                          stream=None) -> None:
+    """The order of each rank's slots by expert, from the experts chosen [ranks, tokens, top_k] (int32 or
+    int64; negative: an empty slot) and an optional mask [ranks, tokens] of the tokens that count:
+    offsets [ranks, experts + 1], every expert's first sorted row and the number of rows; places [ranks,
+    tokens, top_k], each slot's sorted row (-1: none); slots [ranks, tokens * top_k], each row's slot
+    token * top_k + j (-1 behind the last row; None: not wanted). All three are int32."""
+    ip, it, dev = _numbers(chosen, "chosen", 3)
+    ranks, tokens, k = chosen.shape
+    i32 = _TORCH.int32
+    if not isinstance(offsets, _TORCH.Tensor) or offsets.dim() != 2:
+        raise ValueError("offsets must be [ranks, experts + 1]")
+    experts = offsets.shape[1] - 1
+    op = _array(offsets, "offsets", (ranks, experts + 1), i32, dev)
+    pp = _array(places, "places", (ranks, tokens, k), i32, dev)
+    sp = _array(slots, "slots", (ranks, tokens * k), i32, dev)
+    mp = _mask(mask, (ranks, tokens), dev)
+    wp, wb = _work(workspace, dev)
+    _check(_lib().trivance_experts_sort(ip, mp, op, pp, sp, ranks, tokens, k, experts, it, wp, wb,
+                                        _stream_ptr(stream)), "trivance_experts_sort")
+
+
+def _slots(rows, places, weights):
+    """What the calls on sorted rows have in common: (rows' pointer and strides, places, weights, their type,
+    (ranks, tokens, top_k, width, capacity), the rows' type, the GPU)."""
+    rp, rr, rs, dt, dev = _rows(rows, "rows")
+    if not isinstance(places, _TORCH.Tensor) or places.dim() != 3:
+        raise ValueError("places must be [ranks, tokens, top_k]")
+    _, tokens, k = places.shape
+    ranks, capacity, width = rows.shape
+    pp = _array(places, "places", (ranks, tokens, k), _TORCH.int32, dev)
+    wp, wt = None, F32
+    if weights is not None:
+        wt = _FLOATS.get(getattr(weights, "dtype", None))
+        if wt is None:
+            raise TypeError("weights must be a float32, bfloat16 or float16 tensor")
+        wp = _array(weights, "weights", (ranks, tokens, k), weights.dtype, dev)
+    return (rp, rr, rs), pp, wp, wt, (ranks, tokens, k, width, capacity), dt, dev
+
+
+def trivance_experts_dispatch(x, places, rows, stream=None) -> None:
+    """rows[r, places[r, t, j]] = x[r, t]: copies of the tokens' rows x [ranks, tokens, width] in the order
+    of trivance_experts_sort; rows [ranks, capacity, width] of no slot stay as they are."""
+    (rp, rr, rs), pp, _, _, sizes, dt, dev = _slots(rows, places, None)
+    ranks, tokens, k, width, capacity = sizes
+    xp, xr, xt = _rows_like(x, "x", (ranks, tokens, width), rows.dtype, dev)
+    _check(_lib().trivance_experts_dispatch(xp, pp, rp, ranks, tokens, k, width, capacity, xr, xt, rr, rs, dt,
+                                            _stream_ptr(stream)), "trivance_experts_dispatch")
+
+
+def trivance_experts_combine(rows, places, y, weights=None, stream=None) -> None:
+    """y[r, t] = sum over j of weights[r, t, j] rows[r, places[r, t, j]] (None: ones, which is the gradient
+    of trivance_experts_dispatch); y [ranks, tokens, width]."""
+    (rp, rr, rs), pp, wp, wt, sizes, dt, dev = _slots(rows, places, weights)
+    ranks, tokens, k, width, capacity = sizes
+    yp, yr, yt = _rows_like(y, "y", (ranks, tokens, width), rows.dtype, dev)
+    _check(_lib().trivance_experts_combine(rp, pp, wp, yp, ranks, tokens, k, width, capacity, rr, rs, yr, yt,
+                                           dt, wt, _stream_ptr(stream)), "trivance_experts_combine")
+
+
+def trivance_experts_combine_backward(dy, rows, places, weights, drows, dweights, stream=None) -> None:
+    """drows [ranks, capacity, width] and dweights [ranks, tokens, top_k] (float32), the gradients of
+    trivance_experts_combine, from dy [ranks, tokens, width]; drows of no slot stay as they are."""
+    (rp, rr, rs), pp, wp, wt, sizes, dt, dev = _slots(rows, places, weights)
+    ranks, tokens, k, width, capacity = sizes
+    yp, yr, yt = _rows_like(dy, "dy", (ranks, tokens, width), rows.dtype, dev)
+    dp, dr, ds = _rows_like(drows, "drows", rows.shape, rows.dtype, dev)
+    gp = _array(dweights, "dweights", (ranks, tokens, k), _TORCH.float32, dev)
+    _check(_lib().trivance_experts_combine_backward(yp, rp, pp, wp, dp, gp, ranks, tokens, k, width, capacity,
+                                                    yr, yt, rr, rs, dr, ds, dt, wt, _stream_ptr(stream)),
+           "trivance_experts_combine_backward")
+
+
+def trivance_embedding_forward(ids, table, y, scale=1.0, stream=None) -> None:
+    """y[r, t] = scale * table[ids[r, t]], zeros for numbers outside the table [vocab, width]; ids [ranks,
+    tokens] (int32 or int64), y [ranks, tokens, width]."""
+    yp, yr, yt, dt, dev = _rows(y, "y")
+    ranks, tokens, width = y.shape
+    ip, it, _ = _numbers(ids, "ids", 2)
+    if ids.shape != (ranks, tokens):
+        raise ValueError(f"ids must be {(ranks, tokens)}")
+    if not isinstance(table, _TORCH.Tensor) or table.get_device() != dev or table.dtype not in _FLOATS:
+        raise TypeError(f"table must be a float32, bfloat16 or float16 tensor on GPU {dev}")
+    if table.dim() != 2 or table.shape[1] != width or (width > 1 and table.stride(1) != 1):
+        raise ValueError(f"table must be [vocab, {width}] with consecutive values in a row")
+    vocab = table.shape[0]
+    _check(_lib().trivance_embedding_forward(ip, table.data_ptr(), yp, ranks, tokens, width, vocab,
+                                             table.stride(0) if vocab > 1 else width, yr, yt, scale, dt,
+                                             _FLOATS[table.dtype], it, _stream_ptr(stream)),
+           "trivance_embedding_forward")
+
+
+def trivance_embedding_workspace_bytes(ranks: int, tokens: int, width: int, vocab: int) -> int:
+    return _check(_lib().trivance_embedding_workspace_bytes(ranks, tokens, width, vocab),
+                  "trivance_embedding_workspace_bytes")
+
+
+def trivance_embedding_backward(dy, ids, dtable, workspace, scale=1.0, stream=None) -> None:
+    """dtable [ranks, vocab, width] (float32; a rank's values one after another): every rank's gradient of
+    the table from dy [ranks, tokens, width] and its tokens' numbers, all of it written."""
+    dp, dr, dts, dt, dev = _rows(dy, "dy")
+    ranks, tokens, width = dy.shape
+    ip, it, _ = _numbers(ids, "ids", 2)
+    if ids.shape != (ranks, tokens):
+        raise ValueError(f"ids must be {(ranks, tokens)}")
+    if not isinstance(dtable, _TORCH.Tensor) or dtable.dim() != 3:
+        raise TypeError("dtable must be a [ranks, vocab, width] tensor")
+    vocab = dtable.shape[1]
+    tp, tr, ts = _rows_like(dtable, "dtable", (ranks, vocab, width), _TORCH.float32, dev)
+    if vocab > 1 and ts != width:
+        raise ValueError("the rows of a rank's dtable must follow one another")
+    wp, wb = _work(workspace, dev)
+    _check(_lib().trivance_embedding_backward(dp, ip, tp, ranks, tokens, width, vocab, dr, dts,
+                                              tr if ranks > 1 else vocab * width, scale, dt, it, wp, wb,
+                                              _stream_ptr(stream)), "trivance_embedding_backward")
+
+
+def trivance_dropout(x, y, state, rate: float, residual=None, stream=None) -> None:
+    """y = residual + x with a share `rate` of its values dropped and the others multiplied by 1 / (1 - rate)
+    (rate to a multiple of 2^-16); x, residual and y [ranks, tokens, width]. state: the seed and the
+    number of the call, two int64 values that are read when the kernel runs; the gradient is the same call
+    on dy with the same state."""
+    xp, xr, xt, dt, dev = _rows(x, "x")
+    shape = x.shape
+    yp, yr, yt = _rows_like(y, "y", shape, x.dtype, dev)
+    rp, rr, rt = (None, 0, 0) if residual is None else _rows_like(residual, "residual", shape, x.dtype, dev)
+    sp = _array(state, "state", (2,), _TORCH.int64, dev)
+    ranks, tokens, width = shape
+    _check(_lib().trivance_dropout(xp, rp, yp, sp, ranks, tokens, width, xr, xt, rr, rt, yr, yt, rate, dt,
+                                   _stream_ptr(stream)), "trivance_dropout")

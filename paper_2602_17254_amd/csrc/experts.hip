@@ -1,0 +1,316 @@
+// Tokens sorted by expert and back, over the rows of [ranks][tokens][width].
+//
+//   the slots (token, j) of a rank that hold an expert, in the order of expert, token, j: slot i's place is p_i
+//   dispatch:  rows_{p_tj} = x_t                      combine:  y_t = sum_j w_tj rows_{p_tj}
+//   gradients: drows_{p_tj} = w_tj dy_t               dw_tj = sum over columns of dy_t rows_{p_tj}
+//              of a dispatch: dx_t = sum_j drows_{p_tj}, a combine without weights
+//
+// Memory bounds all three. Every kernel goes by token: a token's row is read (or written) once and its slots' rows,
+// which lie anywhere, in whole runs of consecutive lanes. A slot without a row (a place outside the sorted rows) is passed over and neither
+// read nor written; sums are in fp32, in the order of the slots, rounded once.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "device.h"
+#include "operators.h"
+#include "sort.h"
+#include "vectors.h"
+
+#pragma clang fp contract(fast)
+
+namespace trivance {
+namespace {
+
+template <typename T>
+struct Slots {
+    const int* places;  // [ranks][tokens][top_k]
+    const void* weights;  // the same, of weight_type; NULL: ones
+    T* rows;            // the sorted rows, `capacity` of a rank
+    int64_t ranks, tokens, width, capacity, rows_rank, rows_row;
+    int64_t x_rank, x_token;  // of the tokens' rows
+    int64_t drows_rank, drows_row;
+    int top_k, weight_type;
+    Share share;
+};
+
+// A slot's weight and its row's place, negative for none.
+template <typename T>
+__device__ __forceinline__ int place_of(const Slots<T>& a, int64_t slot) {
+    const int p = a.places[slot];
+    return p < a.capacity ? p : -1;
+}
+
+template <typename T>
+__device__ __forceinline__ float weight_of(const Slots<T>& a, int64_t slot) {
+    if (!a.weights) return 1.0f;
+    if (a.weight_type == TRIVANCE_F32) return static_cast<const float*>(a.weights)[slot];
+    if (a.weight_type == TRIVANCE_BF16) return (float)static_cast<const bf16*>(a.weights)[slot];
+    return (float)static_cast<const f16*>(a.weights)[slot];
+}
+
+// A lane reads a vector of a token's row once and writes it to each of the token's slots' rows.
+template <typename T, int V, bool STREAM>
+__global__ __launch_bounds__(kShareThreads) void dispatch_kernel(Slots<T> a, const T* x) {
+    for_vectors<V>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, int64_t t, int64_t i) {
+        const auto v = load_vector<false, V>(x + r * a.x_rank + t * a.x_token + i);
+        const int64_t slot = (r * a.tokens + t) * a.top_k;
+        T* rows = a.rows + r * a.rows_rank + i;
+        for (int j = 0; j < a.top_k; ++j) {
+            const int p = place_of(a, slot + j);
+            if (p >= 0) store_vector<STREAM, V>(rows + p * a.rows_row, v);
+        }
+    });
+}
+
+// A lane adds up a vector of a token's result, K slots' loads on their way at once.
+template <typename T, int V, int K, bool STREAM>
+__global__ __launch_bounds__(kShareThreads) void combine_kernel(Slots<T> a, T* y) {
+    for_vectors<V>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, int64_t t, int64_t i) {
+        const int64_t slot = (r * a.tokens + t) * a.top_k;
+        const T* rows = a.rows + r * a.rows_rank + i;
+        float sum[V] = {};
+        for (int j0 = 0; j0 < a.top_k; j0 += K) {
+            Some<T, V> v[K];
+            int p[K];
+            float w[K];
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                p[j] = j0 + j < a.top_k ? place_of(a, slot + j0 + j) : -1;
+                if (p[j] >= 0) {
+                    v[j] = load_vector<STREAM, V>(rows + p[j] * a.rows_row);
+                    w[j] = weight_of(a, slot + j0 + j);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (p[j] >= 0) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) sum[k] += w[j] * (float)v[j][k];
+                }
+        }
+        Some<T, V> o;
+#pragma unroll
+        for (int k = 0; k < V; ++k) o[k] = (T)sum[k];
+        store_vector<STREAM, V>(y + r * a.x_rank + t * a.x_token + i, o);
+    });
+}
+
+// L lanes take a token: each adds up its vectors' part of the slots' sums, K slots at a time.
+template <typename T, int V, int L, int K, bool STREAM>
+__global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T> a, const T* dy, T* drows, float* dweights) {
+    constexpr int G = kShareThreads / L;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
+        for (int64_t t = (int64_t)blockIdx.x * G + group; t < a.tokens; t += (int64_t)gridDim.x * G) {
+            const int64_t slot = (r * a.tokens + t) * a.top_k;
+            const T* from = dy + r * a.x_rank + t * a.x_token;
+            for (int j0 = 0; j0 < a.top_k; j0 += K) {
+                int p[K];
+                float w[K], sum[K] = {};
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    p[j] = j0 + j < a.top_k ? place_of(a, slot + j0 + j) : -1;
+                    w[j] = p[j] >= 0 ? weight_of(a, slot + j0 + j) : 0.0f;
+                }
+                for (int64_t i = lane * V; i < a.width; i += L * V) {
+                    const int64_t at = i + V <= a.width ? i : a.width - V;
+                    const int skip = (int)(i - at);  // values of the vector before
+                    const auto d = load_vector<false, V>(from + at);
+                    Some<T, V> v[K];
+#pragma unroll
+                    for (int j = 0; j < K; ++j)
+                        if (p[j] >= 0) v[j] = load_vector<STREAM, V>(a.rows + r * a.rows_rank + p[j] * a.rows_row + at);
+#pragma unroll
+                    for (int j = 0; j < K; ++j)
+                        if (p[j] >= 0) {
+                            Some<T, V> o;
+#pragma unroll
+                            for (int k = 0; k < V; ++k) {
+                                const float g = (float)d[k];
+                                o[k] = (T)(w[j] * g);
+                                sum[j] += k >= skip ? g * (float)v[j][k] : 0.0f;
+                            }
+                            store_vector<STREAM, V>(drows + r * a.drows_rank + p[j] * a.drows_row + at, o);
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    sum[j] = lanes_sum<L>(sum[j]);
+                    if (lane == 0 && j0 + j < a.top_k) dweights[slot + j0 + j] = sum[j];
+                }
+            }
+        }
+    }
+}
+
+template <typename F>
+void with_slots(int64_t top_k, F run) {
+    if (top_k == 1) run(std::integral_constant<int, 1>{});
+    else if (top_k == 2) run(std::integral_constant<int, 2>{});
+    else if (top_k <= 4) run(std::integral_constant<int, 4>{});
+    else run(std::integral_constant<int, 8>{});
+}
+
+template <typename F>
+int with_type(int dtype, F run) {
+    return dtype == TRIVANCE_F32 ? run(float{}) : dtype == TRIVANCE_BF16 ? run(bf16{}) : run(f16{});
+}
+
+// Sizes that every call checks: all slots' numbers fit an int32.
+bool sizes_ok(int64_t ranks, int64_t tokens, int64_t top_k) {
+    if (ranks < 1 || tokens < 0 || top_k < 1) return false;
+    return ranks <= INT32_MAX && top_k <= INT32_MAX && (__int128)ranks * tokens * top_k <= INT32_MAX;
+}
+
+// The tokens' rows and the sorted ones; `written` says which of them a call writes.
+bool rows_ok(int64_t ranks, int64_t tokens, int64_t width, int64_t capacity, int64_t x_rank, int64_t x_token,
+             int64_t rows_rank, int64_t rows_row) {
+    if (width < 1 || width > ((int64_t)1 << 24) || capacity < 0 || capacity > INT32_MAX) return false;
+    return rows_fit(ranks, tokens, width, x_rank, x_token) &&
+           rows_fit(ranks, capacity > 0 ? capacity : 1, width, rows_rank, rows_row);
+}
+
+}  // namespace
+}  // namespace trivance
+
+using namespace trivance;
+
+extern "C" {
+
+int64_t trivance_experts_workspace_bytes(int64_t ranks, int64_t tokens, int64_t top_k, int64_t experts) {
+    if (!sizes_ok(ranks, tokens, top_k) || experts < 1) return TRIVANCE_EINVAL;
+    if (experts > kMaxBins) return TRIVANCE_EUNSUPPORTED;
+    return sort_hist_values(ranks, tokens * top_k, (int)experts) * (int64_t)sizeof(int);
+}
+
+int trivance_experts_sort(const void* chosen, const uint8_t* mask, int32_t* offsets, int32_t* places, int32_t* slots,
+                          int64_t ranks, int64_t tokens, int64_t top_k, int64_t experts, int id_dtype, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+    if (id_dtype != TRIVANCE_I32 && id_dtype != TRIVANCE_I64) return TRIVANCE_EINVAL;
+    const int64_t need = trivance_experts_workspace_bytes(ranks, tokens, top_k, experts);
+    if (need < 0) return (int)need;
+    if (!offsets || (tokens > 0 && (!chosen || !places))) return TRIVANCE_EINVAL;
+    if (workspace_bytes < need || (need > 0 && !workspace)) return TRIVANCE_ESIZE;
+    if (reinterpret_cast<uintptr_t>(workspace) % sizeof(int)) return TRIVANCE_EINVAL;
+    SortPass a{};
+    a.ids = tokens > 0 ? chosen : offsets;  // of no tokens nothing is read
+    a.mask = mask;
+    a.wide = id_dtype == TRIVANCE_I64;
+    a.by_top_k = make_fastdiv32((uint32_t)top_k);
+    a.tokens = tokens;
+    a.ranks = ranks;
+    a.slots = tokens * top_k;
+    a.bound = experts;
+    a.digits = -1;
+    a.bins = (int)experts;
+    a.places = places;
+    a.offsets = offsets;
+    a.to_order = slots;
+    a.hist = static_cast<int*>(workspace);
+    return run_sort_pass(a, reinterpret_cast<hipStream_t>(stream));
+}
+
+int trivance_experts_dispatch(const void* x, const int32_t* places, void* rows, int64_t ranks, int64_t tokens,
+                              int64_t top_k, int64_t width, int64_t capacity, int64_t x_rank_stride,
+                              int64_t x_token_stride, int64_t rows_rank_stride, int64_t rows_row_stride, int dtype,
+                              void* stream) {
+    if (!is_float_type(dtype) || !sizes_ok(ranks, tokens, top_k)) return TRIVANCE_EINVAL;
+    if (tokens == 0) return TRIVANCE_OK;
+    if (!rows_ok(ranks, tokens, width, capacity, x_rank_stride, x_token_stride, rows_rank_stride, rows_row_stride))
+        return TRIVANCE_EINVAL;
+    if (!x || !places || (capacity > 0 && !rows) ||
+        (capacity > 0 && !rows_distinct(ranks, capacity, width, rows_rank_stride, rows_row_stride)))
+        return TRIVANCE_EINVAL;
+    if (capacity == 0) return TRIVANCE_OK;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return with_type(dtype, [&](auto type) {
+        using T = decltype(type);
+        return with_vector<T>(width, [&](auto v) {
+            Slots<T> a{places, nullptr, static_cast<T*>(rows), ranks, tokens, width, capacity, rows_rank_stride,
+                       rows_row_stride, x_rank_stride, x_token_stride, 0, 0, (int)top_k, 0,
+                       share_vectors(ranks, tokens, width, v())};
+            const T* from = static_cast<const T*>(x);
+            if (ranks * tokens * top_k * width * (int64_t)sizeof(T) > kStreamBytes)
+                dispatch_kernel<T, v(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, from);
+            else
+                dispatch_kernel<T, v(), false><<<a.share.grid, kShareThreads, 0, s>>>(a, from);
+            return launch_status();
+        });
+    });
+}
+
+int trivance_experts_combine(const void* rows, const int32_t* places, const void* weights, void* y, int64_t ranks,
+                             int64_t tokens, int64_t top_k, int64_t width, int64_t capacity, int64_t rows_rank_stride,
+                             int64_t rows_row_stride, int64_t y_rank_stride, int64_t y_token_stride, int dtype,
+                             int weight_dtype, void* stream) {
+    if (!is_float_type(dtype) || !is_float_type(weight_dtype) || !sizes_ok(ranks, tokens, top_k)) return TRIVANCE_EINVAL;
+    if (tokens == 0) return TRIVANCE_OK;
+    if (!rows_ok(ranks, tokens, width, capacity, y_rank_stride, y_token_stride, rows_rank_stride, rows_row_stride))
+        return TRIVANCE_EINVAL;
+    if ((capacity > 0 && !rows) || !places || !y || !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride))
+        return TRIVANCE_EINVAL;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return with_type(dtype, [&](auto type) {
+        using T = decltype(type);
+        return with_vector<T>(width, [&](auto v) {
+            Slots<T> a{places, weights, static_cast<T*>(const_cast<void*>(rows)), ranks, tokens, width, capacity,
+                       rows_rank_stride, rows_row_stride, y_rank_stride, y_token_stride, 0, 0, (int)top_k, weight_dtype,
+                       share_vectors(ranks, tokens, width, v())};
+            with_slots(top_k, [&](auto k) {
+                if (ranks * tokens * top_k * width * (int64_t)sizeof(T) > kStreamBytes)
+                    combine_kernel<T, v(), k(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, static_cast<T*>(y));
+                else
+                    combine_kernel<T, v(), k(), false><<<a.share.grid, kShareThreads, 0, s>>>(a, static_cast<T*>(y));
+            });
+            return launch_status();
+        });
+    });
+}
+
+int trivance_experts_combine_backward(const void* dy, const void* rows, const int32_t* places, const void* weights,
+                                      void* drows, float* dweights, int64_t ranks, int64_t tokens, int64_t top_k,
+                                      int64_t width, int64_t capacity, int64_t dy_rank_stride, int64_t dy_token_stride,
+                                      int64_t rows_rank_stride, int64_t rows_row_stride, int64_t drows_rank_stride,
+                                      int64_t drows_row_stride, int dtype, int weight_dtype, void* stream) {
+    if (!is_float_type(dtype) || !is_float_type(weight_dtype) || !sizes_ok(ranks, tokens, top_k)) return TRIVANCE_EINVAL;
+    if (tokens == 0) return TRIVANCE_OK;
+    if (!rows_ok(ranks, tokens, width, capacity, dy_rank_stride, dy_token_stride, rows_rank_stride, rows_row_stride))
+        return TRIVANCE_EINVAL;
+    if (!dy || !places || !dweights || (capacity > 0 && (!rows || !drows)) ||
+        !rows_fit(ranks, capacity > 0 ? capacity : 1, width, drows_rank_stride, drows_row_stride) ||
+        (capacity > 0 && !rows_distinct(ranks, capacity, width, drows_rank_stride, drows_row_stride)))
+        return TRIVANCE_EINVAL;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return with_type(dtype, [&](auto type) {
+        using T = decltype(type);
+        return with_vector<T>(width, [&](auto v) {
+            const Slots<T> a{places, weights, static_cast<T*>(const_cast<void*>(rows)), ranks, tokens, width, capacity,
+                             rows_rank_stride, rows_row_stride, dy_rank_stride, dy_token_stride, drows_rank_stride,
+                             drows_row_stride, (int)top_k, weight_dtype, Share{}};
+            const T* from = static_cast<const T*>(dy);
+            const bool stream_rows = ranks * tokens * top_k * width * (int64_t)sizeof(T) > kStreamBytes;
+            const auto launch = [&](auto l, auto k) {
+                const dim3 grid = share_rows(ranks, tokens, kShareThreads / l());
+                if (stream_rows)
+                    combine_backward_kernel<T, v(), l(), k(), true><<<grid, kShareThreads, 0, s>>>(
+                        a, from, static_cast<T*>(drows), dweights);
+                else
+                    combine_backward_kernel<T, v(), l(), k(), false><<<grid, kShareThreads, 0, s>>>(
+                        a, from, static_cast<T*>(drows), dweights);
+            };
+            with_slots(top_k, [&](auto k) {
+                // lanes of a token: a power of two that holds its vectors, at most a wave
+                const int64_t n = (width + v() - 1) / v();
+                if (n <= 8) launch(std::integral_constant<int, 8>{}, k);
+                else if (n <= 16) launch(std::integral_constant<int, 16>{}, k);
+                else if (n <= 32) launch(std::integral_constant<int, 32>{}, k);
+                else launch(std::integral_constant<int, 64>{}, k);
+            });
+            return launch_status();
+        });
+    });
+}
+
+}  // extern "C"

@@ -23,6 +23,10 @@ struct Packed {
     typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
+// V of them.
+template <typename T, int V>
+using Some = T __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+
 // A vector load or store that, where STREAM, does not stay in the caches: of tensors beyond kStreamBytes,
 // the L2 caches together, which would drop it before its next reader.
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
