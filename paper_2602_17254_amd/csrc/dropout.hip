@@ -54,9 +54,9 @@ __global__ __launch_bounds__(kShareThreads) void dropout_kernel(Dropout<T> a) {
     constexpr int V = kVec<T>, N = kBlock / V;
     const uint64_t seed = a.state[0];
     const uint32_t call = (uint32_t)a.state[1];
-    // no lent values here: a vector's columns are those of its counter, and y may be x
-    for_blocks(a.share, a.ranks, a.tokens, [&](int64_t r, int64_t t, uint32_t block) {
-        const int64_t first = (int64_t)block * kBlock;
+    // no lent values: a block's columns are those of its counter, and y may be x
+    for_vectors<kBlock, 1>(a.share, a.ranks, a.tokens, INT64_MAX, [&](int64_t r, const Item(&item)[1]) {
+        const int64_t t = item[0].token, first = item[0].first;
         const T* x = a.x + r * a.x_rank + t * a.x_token;
         const T* residual = a.residual + r * a.residual_rank + t * a.residual_token;
         T* y = a.y + r * a.y_rank + t * a.y_token;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kShareThreads) void dropout_kernel(Dropout<T> a) {
             v[n] = load_packed<T, STREAM>(x, first + n * V, a.width, (T)0.0f);
             if (a.residual) more[n] = load_packed<T, STREAM>(residual, first + n * V, a.width, (T)0.0f);
         }
-        uint32_t c[4] = {block, (uint32_t)t, (uint32_t)r, call};
+        uint32_t c[4] = {(uint32_t)(first / kBlock), (uint32_t)t, (uint32_t)r, call};
         philox(c, (uint32_t)seed, (uint32_t)(seed >> 32));
 #pragma unroll
         for (int n = 0; n < N; ++n) {

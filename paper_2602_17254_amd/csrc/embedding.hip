@@ -3,10 +3,10 @@
 //   y_t = scale table_{id_t}          dtable_v = scale sum of dy_t over the rank's tokens with id_t = v
 //
 // Memory bounds both: the gradient is dense, a row of the vector that an AllReduce sums, so most of its bytes are
-// zeros. A rank's tokens are sorted by number (sort.hip, one pass for tables of up to 4096 rows, otherwise two); a row's tokens
-// are then a run of the sorted ones, and a group of lanes adds them up in the order of the tokens and writes the row
-// once: no atomics, the same bits in every call. Frequent numbers have long runs: those of more than `piece` tokens are summed
-// by pieces of that many, each by its own lanes, into the workspace, and the pieces' sums joined in order in 64 bits.
+// zeros. A rank's tokens are sorted by number (sort.hip, one pass for tables of up to 4096 rows, otherwise two), and the
+// launches of the sort, which latency bounds, write the zeros on the way. A number's tokens are then a run of the sorted ones.
+// Groups of lanes take equal pieces of these, add up rows in the order of the tokens and write a row of the gradient where its
+// run ends: no atomics, the same bits in every call. Sums of runs that go beyond a piece are joined in order in 64 bits.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -36,17 +36,27 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int wide, int64_t at) 
     return wide ? static_cast<const int64_t*>(ids)[at] : static_cast<const int*>(ids)[at];
 }
 
+constexpr int kLookupItems = 2;  // vectors of a lane: their numbers, then the table's rows, are on their way at once
+
 template <typename T, int V, bool STREAM>
 __global__ __launch_bounds__(kShareThreads) void lookup_kernel(Lookup a, T* y) {
-    for_vectors<V>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, int64_t t, int64_t i) {
-        const int64_t id = id_at(a.ids, a.wide, r * a.tokens + t);
-        float v[V] = {};
-        if (id >= 0 && id < a.vocab)
-            load_weights<V>(a.table, a.table_type, id * a.table_row + i, INT64_MAX, 0.0f, v);
-        Some<T, V> o;
+    constexpr int U = kLookupItems;
+    for_vectors<V, U>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, const Item(&item)[U]) {
+        int64_t id[U];
+        float v[U][V] = {};
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = (T)(v[k] * a.scale);
-        store_vector<STREAM, V>(y + r * a.y_rank + t * a.y_token + i, o);
+        for (int u = 0; u < U; ++u) id[u] = item[u].is ? id_at(a.ids, a.wide, r * a.tokens + item[u].token) : -1;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (id[u] >= 0 && id[u] < a.vocab)
+                load_weights<V>(a.table, a.table_type, id[u] * a.table_row + item[u].first, INT64_MAX, 0.0f, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            Some<T, V> o;
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[k] = (T)(v[u][k] * a.scale);
+            if (item[u].is) store_vector<STREAM, V>(y + r * a.y_rank + item[u].token * a.y_token + item[u].first, o);
+        }
     });
 }
 
@@ -55,172 +65,159 @@ struct Table {
     const T* dy;
     float* dtable;  // a rank's rows follow one another
     const int *keys, *order;  // [ranks][tokens], sorted
-    const int* starts;  // [ranks][vocab + 1]: where each number's run starts
+    const int* counts;  // how many of a rank's tokens have a number, count_stride apart
     float* parts;  // [ranks][pieces][2][width]
-    int64_t ranks, tokens, vocab, width, dy_rank, dy_token, dtable_rank, pieces;
+    int64_t ranks, tokens, width, count_stride, dy_rank, dy_token, dtable_rank, pieces;
     int piece;
     float scale;
 };
 
-// Where the run of each number starts among a rank's sorted keys: the number of keys below it.
-__global__ __launch_bounds__(kThreads) void starts_kernel(const int* keys, const int* counts, int64_t count_stride,
-                                                          int* starts, int64_t ranks, int64_t tokens, int64_t vocab) {
-    const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (v > vocab) return;
-    for (int64_t r = blockIdx.y; r < ranks; r += gridDim.y) {
-        const int* k = keys + r * tokens;
-        int low = 0, high = counts[r * count_stride];
-        while (low < high) {
-            const int mid = low + (high - low) / 2;
-            if (k[mid] < v) low = mid + 1;
-            else high = mid;
-        }
-        starts[r * (vocab + 1) + v] = low;
-    }
+// A value of one of L lanes.
+template <int L>
+__device__ __forceinline__ int of_lane(int x, int lane) {
+    if constexpr (L == 64) return __builtin_amdgcn_readlane(x, lane);
+    return __shfl(x, lane, L);
 }
 
-// The sum of a lane's vector of dy over sorted tokens from .. to, four loads on their way at once.
-template <typename T>
-__device__ __forceinline__ void sum_run(const Table<T>& a, int64_t r, int from, int to, int64_t col, float (&sum)[kVec<T>]) {
-    constexpr int V = kVec<T>, kAhead = 4;
-    const int* order = a.order + r * a.tokens;
-    const T* dy = a.dy + r * a.dy_rank;
-#pragma unroll
-    for (int k = 0; k < V; ++k) sum[k] = 0.0f;
-    for (int p = from; p < to; p += kAhead) {
-        typename Packed<T>::type v[kAhead];
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            const int at = p + q < to ? p + q : to - 1;
-            v[q] = load_packed<T>(dy + (int64_t)order[at] * a.dy_token, col, a.width, (T)0.0f);
-        }
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q)
-#pragma unroll
-            for (int k = 0; k < V; ++k) sum[k] += p + q < to ? (float)v[q][k] : 0.0f;
-    }
-}
-
-// L lanes take a row of the gradient, in tiles of columns where there are few rows.
+// L lanes add up their columns of a piece of the sorted tokens, eight rows on their way at once, and write a sum at the end of
+// each run: to the gradient where the run lies in the piece, otherwise to the piece's parts, the first for a run that began
+// before the piece, the second for one that ends behind it only.
 template <typename T, int L, bool STREAM>
-__global__ __launch_bounds__(kThreads) void table_rows_kernel(Table<T> a, int64_t tile) {
-    constexpr int V = kVec<T>, G = kThreads / L;
+__global__ __launch_bounds__(kThreads) void table_sums_kernel(Table<T> a) {
+    constexpr int V = kVec<T>, G = kThreads / L, kAhead = 8;
     const int lane = threadIdx.x % L;
-    const int64_t v = (int64_t)blockIdx.x * G + threadIdx.x / L;
-    if (v >= a.vocab) return;
-    const int64_t begin = blockIdx.z * tile, end = begin + tile < a.width ? begin + tile : a.width;
+    const int64_t col = ((int64_t)blockIdx.x * L + lane) * V;
+    int64_t piece = (int64_t)blockIdx.z * G + threadIdx.x / L;
+    if constexpr (L == 64) piece = __builtin_amdgcn_readfirstlane((int)piece);  // the same in a wave
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
-        const int* starts = a.starts + r * (a.vocab + 1) + v;
-        const int from = starts[0], to = starts[1];
-        float* row = a.dtable + r * a.dtable_rank + v * a.width;
-        if (from == to) {
-            const float zero[4] = {};
-            for (int64_t i = begin + lane * 4; i < end; i += L * 4) store_row<float, 4, STREAM>(row, i, end, zero);
-        } else if (to - from <= a.piece) {
-            for (int64_t i = begin + lane * V; i < end; i += L * V) {
-                float sum[V];
-                sum_run(a, r, from, to, i, sum);
-#pragma unroll
-                for (int k = 0; k < V; ++k) sum[k] *= a.scale;
-                store_row<float, V, STREAM>(row, i, a.width, sum);
-            }
-        }
-    }
-}
-
-// A piece's part of the long run that holds its first token, and of the one that holds its last.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void table_pieces_kernel(Table<T> a) {
-    constexpr int V = kVec<T>;
-    const int64_t col = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * V, piece = blockIdx.z;
-    for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
-        const int* starts = a.starts + r * (a.vocab + 1);
         const int* keys = a.keys + r * a.tokens;
-        const int used = starts[a.vocab];
+        const int* order = a.order + r * a.tokens;
+        const T* dy = a.dy + r * a.dy_rank;
+        const int used = a.counts[r * a.count_stride];
         const int64_t first = piece * a.piece;
         if (first >= used) continue;
-        const int last = (int)(first + a.piece < used ? first + a.piece : used) - 1;
-        const int k0 = keys[first], k1 = keys[last];
+        const int end = (int)(first + a.piece < used ? first + a.piece : used);
+        bool began = first == 0 || keys[first - 1] != keys[first];  // whether the run did in this piece
         float* part = a.parts + (r * a.pieces + piece) * 2 * a.width;
-        float sum[V];
-        if (starts[k0 + 1] - starts[k0] > a.piece) {
-            const int to = starts[k0 + 1] <= last ? starts[k0 + 1] : last + 1;
-            if (col < a.width) {
-                sum_run(a, r, (int)first, to, col, sum);
-                store_row<float, V>(part, col, a.width, sum);
+        float sum[V] = {};
+        for (int p0 = (int)first; p0 < end; p0 += L) {
+            const int here = end - p0 < L ? end - p0 : L, own = p0 + (lane < here ? lane : 0);
+            const int token = order[own], key = keys[own], after = own + 1 < used ? keys[own + 1] : -1;
+            for (int p = 0; p < here; p += kAhead) {
+                typename Packed<T>::type v[kAhead];
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q)
+                    if (p + q < here)
+                        v[q] = load_packed<T, STREAM>(dy + of_lane<L>(token, p + q) * a.dy_token, col, a.width, (T)0.0f);
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) {
+                    if (p + q >= here) break;
+#pragma unroll
+                    for (int k = 0; k < V; ++k) sum[k] += (float)v[q][k];
+                    const int row = of_lane<L>(key, p + q);
+                    const bool ends = of_lane<L>(after, p + q) != row;
+                    if (!ends && p0 + p + q + 1 < end) continue;
+                    float* to = part + (began ? a.width : 0);
+                    if (began && ends) {
+                        to = a.dtable + r * a.dtable_rank + row * a.width;
+#pragma unroll
+                        for (int k = 0; k < V; ++k) sum[k] *= a.scale;
+                    }
+                    store_row<float, V>(to, col, a.width, sum);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) sum[k] = 0.0f;
+                    began = true;
+                }
             }
-        }
-        if (k1 != k0 && starts[k1 + 1] - starts[k1] > a.piece && col < a.width) {
-            sum_run(a, r, starts[k1], last + 1, col, sum);
-            store_row<float, V>(part + a.width, col, a.width, sum);
         }
     }
 }
 
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 4;
+constexpr int kJoinPieces = 8;
 
-// The row of the long run that starts in a piece, if one does: it holds the piece's last token. A wave adds up every eighth piece,
-// eight loads on their way.
+// The rows of the runs that begin in a workgroup's pieces and end behind them: one at most in each. A wave adds up every
+// eighth part of a run, eight loads on their way.
 template <typename T>
 __global__ __launch_bounds__(64 * kJoinWaves) void table_join_kernel(Table<T> a) {
     __shared__ double sums[kJoinWaves][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane, piece = blockIdx.z;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
-        const int* starts = a.starts + r * (a.vocab + 1);
-        const int used = starts[a.vocab];
-        const int64_t first = piece * a.piece;
-        if (first >= used) continue;
-        const int last = (int)(first + a.piece < used ? first + a.piece : used) - 1;
-        const int key = a.keys[r * a.tokens + last], from = starts[key], to = starts[key + 1];
-        if (to - from <= a.piece || from < first) continue;
-        const int64_t end = (to - 1) / a.piece;  // the run's last piece
-        double s = 0.0;
-        if (col < a.width) {
-            const float* part = a.parts + r * a.pieces * 2 * a.width + col;
-            // of its first piece the second sum, unless the piece starts with it
-            if (wave == 0) s = part[(2 * piece + (from > first ? 1 : 0)) * a.width];
+        const int* keys = a.keys + r * a.tokens;
+        const int used = a.counts[r * a.count_stride];
+        for (int64_t piece0 = blockIdx.z * kJoinPieces; piece0 * a.piece < used; piece0 += gridDim.z * kJoinPieces) {
+            // a lane looks at a piece that others follow; every wave does the same
+            const int64_t first = (piece0 + lane) * a.piece, next = first + a.piece;
+            int key = 0;
+            bool begins = false;
+            if (lane < kJoinPieces && next < used) {
+                key = keys[next - 1];
+                begins = keys[next] == key && (first == 0 || keys[first - 1] != key);
+            }
+            for (uint64_t found = __ballot(begins); found; found &= found - 1) {
+                const int which = __ffsll((unsigned long long)found) - 1, row = __shfl(key, which, 64);
+                const int64_t piece = piece0 + which;
+                // the pieces that begin with the same number
+                int64_t end = piece + 1;
+                for (uint64_t all = ~0ull; all == ~0ull; ) {
+                    const int64_t at = (end + lane) * a.piece;
+                    all = __ballot(at < used && keys[at] == row);
+                    end += all == ~0ull ? 64 : __ffsll((unsigned long long)~all) - 1;
+                }
+                double s = 0.0;
+                if (col < a.width) {
+                    const float* part = a.parts + r * a.pieces * 2 * a.width + col;
+                    if (wave == 0) s = part[(2 * piece + 1) * a.width];
 #pragma unroll 8
-            for (int64_t q = piece + 1 + wave; q <= end; q += kJoinWaves) s += part[2 * q * a.width];
-        }
-        sums[wave][lane] = s;
-        __syncthreads();
-        if (wave == 0 && col < a.width) {
+                    for (int64_t q = piece + 1 + wave; q < end; q += kJoinWaves) s += part[2 * q * a.width];
+                }
+                sums[wave][lane] = s;
+                __syncthreads();
+                if (wave == 0 && col < a.width) {
 #pragma unroll
-            for (int w = 1; w < kJoinWaves; ++w) s += sums[w][lane];
-            a.dtable[r * a.dtable_rank + key * a.width + col] = (float)s * a.scale;
+                    for (int w = 1; w < kJoinWaves; ++w) s += sums[w][lane];
+                    a.dtable[r * a.dtable_rank + row * a.width + col] = (float)s * a.scale;
+                }
+                __syncthreads();
+            }
         }
-        __syncthreads();
     }
 }
 
 int64_t imin(int64_t a, int64_t b) { return a < b ? a : b; }
 int64_t imax(int64_t a, int64_t b) { return a > b ? a : b; }
 
-// Tokens of a piece: a power of two near the root of their number, so that neither a piece's tokens nor a run's pieces are
-// many; at most 32768 pieces, the third dimension of a grid.
+// Tokens of a piece: a power of two, from 32 on near a quarter of the root of the tokens' number, so that neither a piece's
+// tokens nor a run's pieces are many: at most 2^17, of which a workgroup takes four or more.
 int piece_of(int64_t tokens) {
-    int64_t p = 64;
-    while (p * p < tokens) p *= 2;
+    int64_t p = 32;
+    while (16 * p * p < tokens) p *= 2;
     return (int)p;
 }
 
-// The bits of the numbers that the first of two passes sorts by; 0 for one pass.
-int first_bits(int64_t vocab) {
-    if (vocab <= kMaxBins) return 0;
+int64_t pieces_of(int64_t tokens) { return (tokens + piece_of(tokens) - 1) / piece_of(tokens); }
+
+// How the numbers are sorted: by their lower bits first where one pass does not hold them all.
+struct Digits {
+    int bits, bins, more;  // of the first pass (0: all); its digits; those of the second
+};
+
+Digits digits_of(int64_t vocab) {
+    if (vocab <= kMaxBins) return {0, (int)vocab, 0};
     int bits = 0;
     while (((int64_t)1 << bits) < vocab) ++bits;
-    return (bits + 1) / 2;
+    bits = (bits + 1) / 2;
+    return {bits, 1 << bits, (int)((vocab - 1) >> bits) + 1};
 }
 
 // What the workspace holds, in words of 4 bytes.
 struct Places {
-    int64_t starts, keys[2], order[2], offsets, hist, parts, end;
+    int64_t offsets, keys[2], order[2], hist, parts, end;
 };
 
 Places places(int64_t ranks, int64_t tokens, int64_t width, int64_t vocab) {
-    const int bits = first_bits(vocab), passes = bits ? 2 : 1;
-    const int bins = bits ? 1 << bits : (int)vocab, more = bits ? (int)((vocab - 1) >> bits) + 1 : 0;
+    const Digits d = digits_of(vocab);
     Places p;
     int64_t at = 0;
     const auto take = [&](int64_t words) {
@@ -228,15 +225,13 @@ Places places(int64_t ranks, int64_t tokens, int64_t width, int64_t vocab) {
         at += (words + 3) / 4 * 4;
         return from;
     };
-    p.starts = take(ranks * (vocab + 1));
+    p.offsets = take(ranks * (d.bins + 1));
     for (int i = 0; i < 2; ++i) {
-        p.keys[i] = i < passes ? take(ranks * tokens) : p.keys[0];
-        p.order[i] = i < passes ? take(ranks * tokens) : p.order[0];
+        p.keys[i] = i == 0 || d.bits ? take(ranks * tokens) : p.keys[0];
+        p.order[i] = i == 0 || d.bits ? take(ranks * tokens) : p.order[0];
     }
-    p.offsets = bits ? take(ranks * (bins + 1)) : p.starts;
-    p.hist = take(imax(sort_hist_values(ranks, tokens, bins), more ? sort_hist_values(ranks, tokens, more) : 0));
-    const int piece = piece_of(tokens);
-    p.parts = take(tokens > piece ? ranks * ((tokens + piece - 1) / piece) * 2 * width : 0);
+    p.hist = take(imax(sort_hist_values(ranks, tokens, d.bins), d.bits ? sort_hist_values(ranks, tokens, d.more) : 0));
+    p.parts = take(ranks * pieces_of(tokens) * 2 * width);
     p.end = at;
     return p;
 }
@@ -258,23 +253,19 @@ void with_lanes(int64_t width, F run) {
 template <typename T>
 int run_gradient(const Table<T>& a, hipStream_t stream) {
     const unsigned grid_y = (unsigned)imin(a.ranks, kShareMaxY);
-    const bool beyond = (double)a.ranks * a.vocab * a.width * sizeof(float) > kStreamBytes;
     with_lanes<T>(a.width, [&](auto l) {
-        const int64_t blocks = (a.vocab + kThreads / l() - 1) / (kThreads / l());
-        // of tables with few rows several workgroups share a row's columns
-        const int64_t step = (int64_t)l() * kVec<T>, columns = (a.width + step - 1) / step;
-        const int64_t tiles = imin(columns, imax(1, 2048 / (blocks * grid_y)));
-        const int64_t tile = (columns + tiles - 1) / tiles * step;
-        const dim3 grid((unsigned)blocks, grid_y, (unsigned)((a.width + tile - 1) / tile));
-        if (beyond) table_rows_kernel<T, l(), true><<<grid, kThreads, 0, stream>>>(a, tile);
-        else table_rows_kernel<T, l(), false><<<grid, kThreads, 0, stream>>>(a, tile);
+        const int64_t step = (int64_t)l() * kVec<T>, rows = kThreads / l();
+        const dim3 grid((unsigned)((a.width + step - 1) / step), grid_y, (unsigned)((a.pieces + rows - 1) / rows));
+        if (a.ranks * a.tokens * a.width * (int64_t)sizeof(T) > kStreamBytes)
+            table_sums_kernel<T, l(), true><<<grid, kThreads, 0, stream>>>(a);
+        else
+            table_sums_kernel<T, l(), false><<<grid, kThreads, 0, stream>>>(a);
     });
-    if (const int rc = launch_status()) return rc;
-    if (a.tokens <= a.piece) return TRIVANCE_OK;  // no run is longer
-    const int64_t step = (int64_t)kThreads * kVec<T>;
-    table_pieces_kernel<T><<<dim3((unsigned)((a.width + step - 1) / step), grid_y, (unsigned)a.pieces), kThreads, 0, stream>>>(a);
-    if (const int rc = launch_status()) return rc;
-    table_join_kernel<T><<<dim3((unsigned)((a.width + 63) / 64), grid_y, (unsigned)a.pieces), 64 * kJoinWaves, 0, stream>>>(a);
+    const int rc = launch_status();
+    if (rc || a.pieces == 1) return rc;
+    const dim3 grid((unsigned)((a.width + 63) / 64), grid_y,
+                    (unsigned)imin((a.pieces + kJoinPieces - 1) / kJoinPieces, kShareMaxY));
+    table_join_kernel<T><<<grid, 64 * kJoinWaves, 0, stream>>>(a);
     return launch_status();
 }
 
@@ -302,7 +293,8 @@ int trivance_embedding_forward(const void* ids, const void* table, void* y, int6
         using T = decltype(type);
         return with_vector<T>(width, [&](auto v) {
             const Lookup a{ids, table, ranks, tokens, vocab, width, table_row_stride, y_rank_stride, y_token_stride,
-                           id_dtype == TRIVANCE_I64, table_dtype, (float)scale, share_vectors(ranks, tokens, width, v())};
+                           id_dtype == TRIVANCE_I64, table_dtype, (float)scale,
+                           share_vectors(ranks, tokens, width, v(), kLookupItems)};
             if (ranks * tokens * width * (int64_t)sizeof(T) > kStreamBytes)
                 lookup_kernel<T, v(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, static_cast<T*>(y));
             else
@@ -336,45 +328,47 @@ int trivance_embedding_backward(const void* dy, const void* ids, float* dtable, 
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Places at = places(ranks, tokens, width, vocab);
     int* words = static_cast<int*>(workspace);
-    const int bits = first_bits(vocab);
+    const Digits d = digits_of(vocab);
+    const int first = sort_launches(ranks, tokens, d.bins), launches = first + (d.bits ? sort_launches(ranks, tokens, d.more) : 0);
     SortPass pass{};
     pass.ids = tokens > 0 ? ids : workspace;  // of no tokens nothing is read
     pass.wide = id_dtype == TRIVANCE_I64;
     pass.ranks = ranks;
     pass.slots = tokens;
     pass.bound = vocab;
-    pass.digits = bits ? (1 << bits) - 1 : -1;
-    pass.bins = bits ? 1 << bits : (int)vocab;
+    pass.digits = d.bits ? d.bins - 1 : -1;
+    pass.bins = d.bins;
     pass.offsets = words + at.offsets;
     pass.to_keys = words + at.keys[0];
     pass.to_order = words + at.order[0];
     pass.hist = words + at.hist;
-    if (const int rc = run_sort_pass(pass, s)) return rc;
-    if (bits) {
+    pass.zeros.at = dtable;
+    pass.zeros.values = vocab * width;
+    pass.zeros.rank_stride = dtable_rank_stride;
+    if (const int rc = run_sort_pass(pass, s, 0, launches)) return rc;
+    const int* counts = pass.offsets + pass.bins;
+    if (d.bits) {
         SortPass next = pass;
         next.ids = nullptr;
         next.keys = pass.to_keys;
         next.order = pass.to_order;
-        next.counts = pass.offsets + pass.bins;
+        next.counts = counts;
         next.count_stride = pass.bins + 1;
-        next.shift = bits;
+        next.shift = d.bits;
         next.digits = -1;
-        next.bins = (int)((vocab - 1) >> bits) + 1;
+        next.bins = d.more;
         next.offsets = nullptr;
         next.to_keys = words + at.keys[1];
         next.to_order = words + at.order[1];
-        if (const int rc = run_sort_pass(next, s)) return rc;
-        starts_kernel<<<dim3((unsigned)((vocab + kThreads) / kThreads), (unsigned)imin(ranks, kShareMaxY)), kThreads, 0, s>>>(
-            next.to_keys, next.counts, next.count_stride, words + at.starts, ranks, tokens, vocab);
-        if (const int rc = launch_status()) return rc;
+        if (const int rc = run_sort_pass(next, s, first, launches)) return rc;
     }
+    if (tokens == 0) return TRIVANCE_OK;
     const auto run = [&](auto type) {
         using T = decltype(type);
-        const int piece = piece_of(tokens);
         return run_gradient(
-            Table<T>{static_cast<const T*>(dy), dtable, words + at.keys[bits ? 1 : 0], words + at.order[bits ? 1 : 0],
-                     words + at.starts, reinterpret_cast<float*>(words + at.parts), ranks, tokens, vocab, width,
-                     dy_rank_stride, dy_token_stride, dtable_rank_stride, (tokens + piece - 1) / piece, piece, (float)scale},
+            Table<T>{static_cast<const T*>(dy), dtable, words + at.keys[1], words + at.order[1], counts,
+                     reinterpret_cast<float*>(words + at.parts), ranks, tokens, width, pass.bins + 1, dy_rank_stride,
+                     dy_token_stride, dtable_rank_stride, pieces_of(tokens), piece_of(tokens), (float)scale},
             s);
     };
     return dtype == TRIVANCE_F32 ? run(float{}) : dtype == TRIVANCE_BF16 ? run(bf16{}) : run(f16{});

@@ -53,10 +53,10 @@ __device__ __forceinline__ float weight_of(const Slots<T>& a, int64_t slot) {
 // A lane reads a vector of a token's row once and writes it to each of the token's slots' rows.
 template <typename T, int V, bool STREAM>
 __global__ __launch_bounds__(kShareThreads) void dispatch_kernel(Slots<T> a, const T* x) {
-    for_vectors<V>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, int64_t t, int64_t i) {
-        const auto v = load_vector<false, V>(x + r * a.x_rank + t * a.x_token + i);
-        const int64_t slot = (r * a.tokens + t) * a.top_k;
-        T* rows = a.rows + r * a.rows_rank + i;
+    for_vectors<V, 1>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, const Item(&item)[1]) {
+        const auto v = load_vector<false, V>(x + r * a.x_rank + item[0].token * a.x_token + item[0].first);
+        const int64_t slot = (r * a.tokens + item[0].token) * a.top_k;
+        T* rows = a.rows + r * a.rows_rank + item[0].first;
         for (int j = 0; j < a.top_k; ++j) {
             const int p = place_of(a, slot + j);
             if (p >= 0) store_vector<STREAM, V>(rows + p * a.rows_row, v);
@@ -64,43 +64,59 @@ __global__ __launch_bounds__(kShareThreads) void dispatch_kernel(Slots<T> a, con
     });
 }
 
-// A lane adds up a vector of a token's result, K slots' loads on their way at once.
+// A lane adds up vectors of U tokens' results, K slots at a time: all places, then all rows on their way at once.
+template <int K>
+constexpr int kCombineItems = K <= 4 ? 2 : 1;
+
 template <typename T, int V, int K, bool STREAM>
 __global__ __launch_bounds__(kShareThreads) void combine_kernel(Slots<T> a, T* y) {
-    for_vectors<V>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, int64_t t, int64_t i) {
-        const int64_t slot = (r * a.tokens + t) * a.top_k;
-        const T* rows = a.rows + r * a.rows_rank + i;
-        float sum[V] = {};
+    constexpr int U = kCombineItems<K>;
+    for_vectors<V, U>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, const Item(&item)[U]) {
+        const T* rows = a.rows + r * a.rows_rank;
+        float sum[U][V] = {};
         for (int j0 = 0; j0 < a.top_k; j0 += K) {
-            Some<T, V> v[K];
-            int p[K];
-            float w[K];
+            Some<T, V> v[U][K];
+            int p[U][K];
+            float w[U][K];
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
-                p[j] = j0 + j < a.top_k ? place_of(a, slot + j0 + j) : -1;
-                if (p[j] >= 0) {
-                    v[j] = load_vector<STREAM, V>(rows + p[j] * a.rows_row);
-                    w[j] = weight_of(a, slot + j0 + j);
-                }
-            }
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (p[j] >= 0) {
+                for (int j = 0; j < K; ++j)
+                    p[u][j] = item[u].is && j0 + j < a.top_k ? place_of(a, (r * a.tokens + item[u].token) * a.top_k + j0 + j) : -1;
 #pragma unroll
-                    for (int k = 0; k < V; ++k) sum[k] += w[j] * (float)v[j][k];
-                }
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    if (p[u][j] >= 0) {
+                        v[u][j] = load_vector<STREAM, V>(rows + item[u].first + p[u][j] * a.rows_row);
+                        w[u][j] = weight_of(a, (r * a.tokens + item[u].token) * a.top_k + j0 + j);
+                    }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    if (p[u][j] >= 0) {
+#pragma unroll
+                        for (int k = 0; k < V; ++k) sum[u][k] += w[u][j] * (float)v[u][j][k];
+                    }
         }
-        Some<T, V> o;
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = (T)sum[k];
-        store_vector<STREAM, V>(y + r * a.x_rank + t * a.x_token + i, o);
+        for (int u = 0; u < U; ++u) {
+            Some<T, V> o;
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[k] = (T)sum[u][k];
+            if (item[u].is) store_vector<STREAM, V>(y + r * a.x_rank + item[u].token * a.x_token + item[u].first, o);
+        }
     });
 }
 
-// L lanes take a token: each adds up its vectors' part of the slots' sums, K slots at a time.
+// L lanes take a token: each adds up its vectors' part of the slots' sums, K slots at a time. With a workgroup for a token,
+// whose lanes have a vector each or a few, 8 x 8192 tokens of 2048 bf16 in 4 slots take 427 us in place of a wave's 465.
 template <typename T, int V, int L, int K, bool STREAM>
 __global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T> a, const T* dy, T* drows, float* dweights) {
     constexpr int G = kShareThreads / L;
+    __shared__ float sums[L > 64 ? 2 : 1][L > 64 ? L / 64 : 1][K];
+    int turn = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         for (int64_t t = (int64_t)blockIdx.x * G + group; t < a.tokens; t += (int64_t)gridDim.x * G) {
@@ -136,9 +152,24 @@ __global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T
                         }
                 }
 #pragma unroll
-                for (int j = 0; j < K; ++j) {
-                    sum[j] = lanes_sum<L>(sum[j]);
-                    if (lane == 0 && j0 + j < a.top_k) dweights[slot + j0 + j] = sum[j];
+                for (int j = 0; j < K; ++j) sum[j] = lanes_sum<L < 64 ? L : 64>(sum[j]);
+                if constexpr (L > 64) {
+                    if (threadIdx.x % 64 == 0) {
+#pragma unroll
+                        for (int j = 0; j < K; ++j) sums[turn][threadIdx.x / 64][j] = sum[j];
+                    }
+                    __syncthreads();
+                    if (lane < K && j0 + lane < a.top_k) {
+                        float s = 0.0f;
+#pragma unroll
+                        for (int w = 0; w < L / 64; ++w) s += sums[turn][w][lane];
+                        dweights[slot + j0 + lane] = s;
+                    }
+                    turn ^= 1;
+                } else if (lane == 0) {
+#pragma unroll
+                    for (int j = 0; j < K; ++j)
+                        if (j0 + j < a.top_k) dweights[slot + j0 + j] = sum[j];
                 }
             }
         }
@@ -256,9 +287,9 @@ int trivance_experts_combine(const void* rows, const int32_t* places, const void
         using T = decltype(type);
         return with_vector<T>(width, [&](auto v) {
             Slots<T> a{places, weights, static_cast<T*>(const_cast<void*>(rows)), ranks, tokens, width, capacity,
-                       rows_rank_stride, rows_row_stride, y_rank_stride, y_token_stride, 0, 0, (int)top_k, weight_dtype,
-                       share_vectors(ranks, tokens, width, v())};
+                       rows_rank_stride, rows_row_stride, y_rank_stride, y_token_stride, 0, 0, (int)top_k, weight_dtype, Share{}};
             with_slots(top_k, [&](auto k) {
+                a.share = share_vectors(ranks, tokens, width, v(), kCombineItems<k()>);
                 if (ranks * tokens * top_k * width * (int64_t)sizeof(T) > kStreamBytes)
                     combine_kernel<T, v(), k(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, static_cast<T*>(y));
                 else
@@ -301,12 +332,13 @@ int trivance_experts_combine_backward(const void* dy, const void* rows, const in
                         a, from, static_cast<T*>(drows), dweights);
             };
             with_slots(top_k, [&](auto k) {
-                // lanes of a token: a power of two that holds its vectors, at most a wave
+                // lanes of a token: a power of two that holds its vectors, or a wave; the workgroup for more than two of a wave's
                 const int64_t n = (width + v() - 1) / v();
                 if (n <= 8) launch(std::integral_constant<int, 8>{}, k);
                 else if (n <= 16) launch(std::integral_constant<int, 16>{}, k);
                 else if (n <= 32) launch(std::integral_constant<int, 32>{}, k);
-                else launch(std::integral_constant<int, 64>{}, k);
+                else if (n <= 128) launch(std::integral_constant<int, 64>{}, k);
+                else launch(std::integral_constant<int, 256>{}, k);
             });
             return launch_status();
         });

@@ -33,8 +33,20 @@ __device__ __forceinline__ int64_t used_of(const SortPass& a, int64_t r) {
     return a.ids ? a.slots : a.counts[r * a.count_stride];
 }
 
-__global__ __launch_bounds__(kHistThreads) void sort_count_kernel(SortPass a, int64_t per) {
+// A workgroup's block of zeros, for every rank of its grid row.
+template <int THREADS>
+__device__ __forceinline__ void fill_block(const SortPass& a, int64_t block) {
+    const int64_t begin = (a.zeros.first + block) * kZerosBlock;
+    const int64_t end = begin + kZerosBlock < a.zeros.values ? begin + kZerosBlock : a.zeros.values;
+    const float zero[4] = {};
+    for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y)
+        for (int64_t i = begin + threadIdx.x * 4; i < end; i += THREADS * 4)
+            store_row<float, 4, true>(a.zeros.at + r * a.zeros.rank_stride, i, end, zero);
+}
+
+__global__ __launch_bounds__(kHistThreads) void sort_count_kernel(SortPass a, int64_t per, int64_t chunks) {
     extern __shared__ int hist[];
+    if (blockIdx.x >= chunks) return fill_block<kHistThreads>(a, blockIdx.x - chunks);
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         for (int e = threadIdx.x; e < a.bins; e += kHistThreads) hist[e] = 0;
         __syncthreads();
@@ -44,7 +56,7 @@ __global__ __launch_bounds__(kHistThreads) void sort_count_kernel(SortPass a, in
             if (key >= 0) atomicAdd(&hist[digit_of(a, key)], 1);
         }
         __syncthreads();
-        int* to = a.hist + (r * gridDim.x + blockIdx.x) * a.bins;
+        int* to = a.hist + (r * chunks + blockIdx.x) * a.bins;
         for (int e = threadIdx.x; e < a.bins; e += kHistThreads) to[e] = hist[e];
         __syncthreads();
     }
@@ -61,24 +73,38 @@ __device__ __forceinline__ int wave_inclusive(int x) {
     return x;
 }
 
+constexpr int kRounds = 2;  // of 64 slots, whose keys a wave holds in registers
+
 template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int64_t per, int bits) {
+__global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int64_t per, int64_t chunks, int bits) {
     constexpr int kThreads = 64 * WAVES;
+    if (blockIdx.x >= chunks) return fill_block<kThreads>(a, blockIdx.x - chunks);
     extern __shared__ int shared[];
     int* first = shared;  // of each digit
     int* sums = shared + a.bins;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     int* own = sums + WAVES + wave * a.bins;  // this wave's counters
-    const int64_t chunks = gridDim.x, c = blockIdx.x;
+    const int64_t c = blockIdx.x;
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         const int64_t begin = c * per, end = begin + per < a.slots ? begin + per : a.slots, used = used_of(a, r);
         const int64_t from = begin + wave * (per / WAVES);
         const int64_t to = from + per / WAVES < end ? from + per / WAVES : end;
+        int key[kRounds];
+        const auto fetch = [&](int64_t base) {
+#pragma unroll
+            for (int q = 0; q < kRounds; ++q) {
+                const int64_t i = base + 64 * q + lane;
+                key[q] = i < to ? key_of(a, r, i, used) : -1;
+            }
+        };
+        fetch(from);
         for (int e = lane; e < a.bins; e += 64) own[e] = 0;
         __syncthreads();
-        for (int64_t i = from + lane; i < to; i += 64) {
-            const int key = key_of(a, r, i, used);
-            if (key >= 0) atomicAdd(&own[digit_of(a, key)], 1);
+        for (int64_t base = from; base < to; base += 64 * kRounds) {
+            if (base > from) fetch(base);
+#pragma unroll
+            for (int q = 0; q < kRounds; ++q)
+                if (key[q] >= 0) atomicAdd(&own[digit_of(a, key[q])], 1);
         }
         __syncthreads();
         // each digit's keys before this chunk, and in all chunks; a wave's counter becomes the number before the wave
@@ -86,7 +112,7 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
             int before = 0, all = 0;
             if (chunks > 1) {
                 const int* h = a.hist + r * chunks * a.bins + e;
-#pragma unroll 8
+#pragma unroll 16
                 for (int64_t k = 0; k < chunks; ++k) {
                     const int n = h[k * a.bins];
                     all += n;
@@ -125,33 +151,33 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
         }
         if (a.offsets && c == 0 && threadIdx.x == 0) a.offsets[r * (a.bins + 1) + a.bins] = total;
         __syncthreads();
-        constexpr int kAhead = 4;  // rounds of a wave whose keys are on their way at once
-        for (int64_t base = from; base < to; base += 64 * kAhead) {
-            int key[kAhead];
+        for (int64_t base = from; base < to; base += 64 * kRounds) {
+            if (to - from > 64 * kRounds) fetch(base);
+            // of each round the lanes with a lane's digit; the rounds' chains of steps are independent
+            uint64_t same[kRounds];
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
-                const int64_t i = base + 64 * q + lane;
-                key[q] = i < to ? key_of(a, r, i, used) : -1;
+            for (int q = 0; q < kRounds; ++q) same[q] = __ballot(key[q] >= 0);
+            for (int b = 0; b < bits; ++b) {
+#pragma unroll
+                for (int q = 0; q < kRounds; ++q) {
+                    const bool one = digit_of(a, key[q]) >> b & 1;  // of no key any will do
+                    const uint64_t set = __ballot(one);
+                    same[q] &= one ? set : ~set;
+                }
             }
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
+            for (int q = 0; q < kRounds; ++q) {
                 const int64_t i = base + 64 * q + lane;
                 const bool is = key[q] >= 0;
-                const int d = is ? digit_of(a, key[q]) : 0;
-                // the lanes with this lane's digit
-                uint64_t same = __ballot(is);
-                for (int b = 0; b < bits; ++b) {
-                    const uint64_t set = __ballot(is && (d >> b & 1));
-                    same &= d >> b & 1 ? set : ~set;
-                }
-                const int rank = (int)__popcll(same & ((1ull << lane) - 1));
+                const int rank = (int)__popcll(same[q] & ((1ull << lane) - 1));
                 int at = -1;
                 if (is) {
                     // all lanes read the counter before the last of them moves it on: a wave's accesses to local
                     // memory keep their order
+                    const int d = digit_of(a, key[q]);
                     const int n = __hip_atomic_load(&own[d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     at = first[d] + n + rank;
-                    if (rank + 1 == (int)__popcll(same))
+                    if (rank + 1 == (int)__popcll(same[q]))
                         __hip_atomic_store(&own[d], n + rank + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
                 if (i < to) {
@@ -170,17 +196,15 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
 
 }  // namespace
 
-// One workgroup for a rank's slots where its waves take at most eight rounds; otherwise chunks to fill the GPU, of one round of
-// each wave at least, and no more than it takes little time to add up the counters of.
+// Chunks of as many slots as a workgroup's waves hold keys of, one where that is all; at most 128, as each workgroup adds up the
+// counters of all of them, and fewer of many digits.
 SortShape sort_shape(int64_t ranks, int64_t slots, int bins) {
-    const auto rounded = [](int64_t n, int64_t to) { return (n + to - 1) / to * to; };
-    int waves = bins <= 512 ? 16 : bins <= 2048 ? 4 : 2;
-    if (slots <= waves * 64 * 8) return {waves, 1, rounded(slots > 0 ? slots : 1, waves * 64)};
-    waves = bins <= 2048 ? 4 : 2;
-    int64_t chunks = 1024 / ranks < 16 ? 16 : 1024 / ranks > 256 ? 256 : 1024 / ranks;
-    if (chunks * bins > 65536) chunks = 65536 / bins;
-    const int64_t per = rounded((slots + chunks - 1) / chunks, waves * 64);
-    return {waves, (slots + per - 1) / per, per};
+    const int waves = bins <= 2048 ? 4 : 2;
+    const int64_t unit = waves * 64, full = unit * kRounds, most = 65536 / bins < 128 ? 65536 / bins : 128;
+    int64_t per = full * ((slots + full * most - 1) / (full * most));
+    if (slots <= full) per = (slots + unit - 1) / unit * unit;
+    if (per == 0) per = unit;
+    return {waves, slots > per ? (slots + per - 1) / per : 1, per};
 }
 
 int64_t sort_hist_values(int64_t ranks, int64_t slots, int bins) {
@@ -188,19 +212,29 @@ int64_t sort_hist_values(int64_t ranks, int64_t slots, int bins) {
     return chunks > 1 ? ranks * chunks * bins : 0;
 }
 
-int run_sort_pass(const SortPass& a, hipStream_t stream) {
+int sort_launches(int64_t ranks, int64_t slots, int bins) { return sort_shape(ranks, slots, bins).chunks > 1 ? 2 : 1; }
+
+int run_sort_pass(SortPass a, hipStream_t stream, int launch, int launches) {
     const SortShape s = sort_shape(a.ranks, a.slots, a.bins);
-    const dim3 grid((unsigned)s.chunks, (unsigned)(a.ranks < kMaxGridY ? a.ranks : kMaxGridY));
+    // this launch's share of the blocks of zeros
+    const int64_t blocks = launches ? (a.zeros.values + kZerosBlock - 1) / kZerosBlock : 0;
+    const auto grid = [&]() {
+        a.zeros.first = launches ? blocks * launch / launches : 0;
+        a.zeros.blocks = launches ? blocks * (launch + 1) / launches - a.zeros.first : 0;
+        ++launch;
+        return dim3((unsigned)(s.chunks + a.zeros.blocks), (unsigned)(a.ranks < kMaxGridY ? a.ranks : kMaxGridY));
+    };
     int bits = 0;
     while ((1 << bits) < a.bins) ++bits;
     if (s.chunks > 1) {
-        sort_count_kernel<<<grid, kHistThreads, sizeof(int) * a.bins, stream>>>(a, s.per);
+        const dim3 g = grid();
+        sort_count_kernel<<<g, kHistThreads, sizeof(int) * a.bins, stream>>>(a, s.per, s.chunks);
         if (const int rc = launch_status()) return rc;
     }
     const size_t local = sizeof(int) * place_words(s.waves, a.bins);
-    if (s.waves == 16) sort_place_kernel<16><<<grid, 64 * 16, local, stream>>>(a, s.per, bits);
-    else if (s.waves == 4) sort_place_kernel<4><<<grid, 64 * 4, local, stream>>>(a, s.per, bits);
-    else sort_place_kernel<2><<<grid, 64 * 2, local, stream>>>(a, s.per, bits);
+    const dim3 g = grid();
+    if (s.waves == 4) sort_place_kernel<4><<<g, 64 * 4, local, stream>>>(a, s.per, s.chunks, bits);
+    else sort_place_kernel<2><<<g, 64 * 2, local, stream>>>(a, s.per, s.chunks, bits);
     return launch_status();
 }
 

@@ -15,7 +15,7 @@ constexpr int kShareThreads = 256;
 constexpr int64_t kShareMaxY = 65535;
 constexpr int64_t kShareMaxX = (int64_t)1 << 22;  // 2^30 lanes of a launch at most
 
-// A workgroup takes the vectors of `tokens` consecutive tokens of a rank: as many as its lanes hold, one at least.
+// A workgroup takes the vectors of `tokens` consecutive tokens of a rank.
 struct Share {
     uint32_t vectors;  // of a row
     FastDiv32 by_vectors;
@@ -23,9 +23,16 @@ struct Share {
     dim3 grid;
 };
 
-inline Share share_vectors(int64_t ranks, int64_t tokens, int64_t width, int vec) {
-    const int64_t n = (width + vec - 1) / vec;  // below 2^24
-    const int64_t each = n < kShareThreads ? kShareThreads / n : 1, blocks = (tokens + each - 1) / each;
+// As many tokens as the lanes hold with `times` vectors each, one at least; and where there are workgroups enough, up to three
+// times as many, if fewer lanes are then without a vector in the last round: 188 vectors are 73% of 256 lanes' work, four
+// times 188 are 98% of three rounds.
+inline Share share_vectors(int64_t ranks, int64_t tokens, int64_t width, int vec, int times = 1) {
+    const int64_t n = (width + vec - 1) / vec, lanes = (int64_t)kShareThreads * times;  // n below 2^24
+    int64_t each = n < lanes ? lanes / n : 1;
+    const auto rounds = [&](int64_t e) { return (e * n + lanes - 1) / lanes; };
+    for (int64_t e = each + 1, first = each; e <= 4 * first; ++e)
+        if ((double)ranks * tokens / e >= 4096 && 100 * rounds(e) * each < 95 * rounds(each) * e) each = e;
+    const int64_t blocks = (tokens + each - 1) / each;
     return Share{(uint32_t)n, make_fastdiv32((uint32_t)n), (uint32_t)each,
                  dim3((unsigned)(blocks < kShareMaxX ? blocks : kShareMaxX), (unsigned)(ranks < kShareMaxY ? ranks : kShareMaxY))};
 }
@@ -36,27 +43,31 @@ inline dim3 share_rows(int64_t ranks, int64_t tokens, int64_t rows) {
     return dim3((unsigned)(blocks < kShareMaxX ? blocks : kShareMaxX), (unsigned)(ranks < kShareMaxY ? ranks : kShareMaxY));
 }
 
-// run(rank, token, vector) for every vector of every row.
-template <typename F>
-__device__ __forceinline__ void for_blocks(const Share& s, int64_t ranks, int64_t tokens, F run) {
+// One of the vectors that a lane takes at once.
+struct Item {
+    bool is;  // whether there is one
+    int64_t token;
+    int64_t first;  // of its columns
+};
+
+// run(rank, items) for every vector of every row, U of them at once. A row that does not end with a vector of V values
+// lends its last one values of the one before: both write the same there. V is 1 for rows shorter than a vector.
+template <int V, int U, typename F>
+__device__ __forceinline__ void for_vectors(const Share& s, int64_t ranks, int64_t tokens, int64_t width, F run) {
     for (int64_t r = blockIdx.y; r < ranks; r += gridDim.y)
         for (int64_t t0 = (int64_t)blockIdx.x * s.tokens; t0 < tokens; t0 += (int64_t)gridDim.x * s.tokens) {
-            const uint32_t here = tokens - t0 < s.tokens ? (uint32_t)(tokens - t0) : s.tokens;
-            for (uint32_t i = threadIdx.x; i < here * s.vectors; i += kShareThreads) {
-                const uint32_t of = fdiv32(i, s.by_vectors);
-                run(r, t0 + of, i - of * s.vectors);
+            const uint32_t here = (tokens - t0 < s.tokens ? (uint32_t)(tokens - t0) : s.tokens) * s.vectors;
+            for (uint32_t i0 = threadIdx.x; i0 < here; i0 += U * kShareThreads) {
+                Item item[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t i = i0 + u * kShareThreads, of = fdiv32(i, s.by_vectors);
+                    const int64_t first = (int64_t)(i - of * s.vectors) * V;
+                    item[u] = Item{i < here, t0 + of, first + V <= width ? first : width - V};
+                }
+                run(r, item);
             }
         }
-}
-
-// run(rank, token, first column) for every vector of V values. A row that does not end with a vector lends its last one
-// values of the one before: both write the same there. V is 1 for rows shorter than a vector.
-template <int V, typename F>
-__device__ __forceinline__ void for_vectors(const Share& s, int64_t ranks, int64_t tokens, int64_t width, F run) {
-    for_blocks(s, ranks, tokens, [&](int64_t r, int64_t t, uint32_t vector) {
-        const int64_t first = (int64_t)vector * V;
-        run(r, t, first + V <= width ? first : width - V);
-    });
 }
 
 // run with the number of values of a row's vectors.
