@@ -63,8 +63,8 @@ __global__ __launch_bounds__(kShareThreads) void dropout_kernel(Dropout<T> a) {
         typename Packed<T>::type v[N], more[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            v[n] = load_packed<T, STREAM>(x, first + n * V, a.width, (T)0.0f);
-            if (a.residual) more[n] = load_packed<T, STREAM>(residual, first + n * V, a.width, (T)0.0f);
+            v[n] = load_columns<T, STREAM>(x, first + n * V, a.width);
+            if (a.residual) more[n] = load_columns<T, STREAM>(residual, first + n * V, a.width);
         }
         uint32_t c[4] = {(uint32_t)(first / kBlock), (uint32_t)t, (uint32_t)r, call};
         philox(c, (uint32_t)seed, (uint32_t)(seed >> 32));
@@ -110,7 +110,7 @@ extern "C" int trivance_dropout(const void* x, const void* residual, void* y, co
         const Dropout<T> a{static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<T*>(y), state, ranks,
                            tokens, width, x_rank_stride, x_token_stride, residual_rank_stride, residual_token_stride,
                            y_rank_stride, y_token_stride, limit, (float)(65536.0 / (65536.0 - limit)),
-                           share_vectors(ranks, tokens, width, kBlock)};
+                           share_vectors(ranks, tokens, width, kBlock, 1, true)};
         if ((double)ranks * tokens * width * sizeof(T) > kStreamBytes)
             dropout_kernel<T, true><<<a.share.grid, kShareThreads, 0, s>>>(a);
         else

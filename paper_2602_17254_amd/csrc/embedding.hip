@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void table_sums_kernel(Table<T> a) {
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q)
                     if (p + q < here)
-                        v[q] = load_packed<T, STREAM>(dy + of_lane<L>(token, p + q) * a.dy_token, col, a.width, (T)0.0f);
+                        v[q] = load_columns<T, STREAM>(dy + of_lane<L>(token, p + q) * a.dy_token, col, a.width);
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
                     if (p + q >= here) break;
@@ -294,7 +294,7 @@ int trivance_embedding_forward(const void* ids, const void* table, void* y, int6
         return with_vector<T>(width, [&](auto v) {
             const Lookup a{ids, table, ranks, tokens, vocab, width, table_row_stride, y_rank_stride, y_token_stride,
                            id_dtype == TRIVANCE_I64, table_dtype, (float)scale,
-                           share_vectors(ranks, tokens, width, v(), kLookupItems)};
+                           share_vectors(ranks, tokens, width, v(), kLookupItems, false)};
             if (ranks * tokens * width * (int64_t)sizeof(T) > kStreamBytes)
                 lookup_kernel<T, v(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, static_cast<T*>(y));
             else

@@ -261,7 +261,7 @@ int trivance_experts_dispatch(const void* x, const int32_t* places, void* rows, 
         return with_vector<T>(width, [&](auto v) {
             Slots<T> a{places, nullptr, static_cast<T*>(rows), ranks, tokens, width, capacity, rows_rank_stride,
                        rows_row_stride, x_rank_stride, x_token_stride, 0, 0, (int)top_k, 0,
-                       share_vectors(ranks, tokens, width, v())};
+                       share_vectors(ranks, tokens, width, v(), 1, false)};
             const T* from = static_cast<const T*>(x);
             if (ranks * tokens * top_k * width * (int64_t)sizeof(T) > kStreamBytes)
                 dispatch_kernel<T, v(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, from);
@@ -289,7 +289,7 @@ int trivance_experts_combine(const void* rows, const int32_t* places, const void
             Slots<T> a{places, weights, static_cast<T*>(const_cast<void*>(rows)), ranks, tokens, width, capacity,
                        rows_rank_stride, rows_row_stride, y_rank_stride, y_token_stride, 0, 0, (int)top_k, weight_dtype, Share{}};
             with_slots(top_k, [&](auto k) {
-                a.share = share_vectors(ranks, tokens, width, v(), kCombineItems<k()>);
+                a.share = share_vectors(ranks, tokens, width, v(), kCombineItems<k()>, false);
                 if (ranks * tokens * top_k * width * (int64_t)sizeof(T) > kStreamBytes)
                     combine_kernel<T, v(), k(), true><<<a.share.grid, kShareThreads, 0, s>>>(a, static_cast<T*>(y));
                 else

@@ -23,14 +23,15 @@ struct Share {
     dim3 grid;
 };
 
-// As many tokens as the lanes hold with `times` vectors each, one at least; and where there are workgroups enough, up to three
+// As many tokens as the lanes hold with `times` vectors each, one at least. With `fill`, where there are workgroups enough, up to four
 // times as many, if fewer lanes are then without a vector in the last round: 188 vectors are 73% of 256 lanes' work, four
 // times 188 are 98% of three rounds.
-inline Share share_vectors(int64_t ranks, int64_t tokens, int64_t width, int vec, int times = 1) {
+inline Share share_vectors(int64_t ranks, int64_t tokens, int64_t width, int vec, int times, bool fill) {
     const int64_t n = (width + vec - 1) / vec, lanes = (int64_t)kShareThreads * times;  // n below 2^24
-    int64_t each = n < lanes ? lanes / n : 1;
-    const auto rounds = [&](int64_t e) { return (e * n + lanes - 1) / lanes; };
-    for (int64_t e = each + 1, first = each; e <= 4 * first; ++e)
+    const int64_t fit = n < lanes ? lanes / n : 1;
+    const auto rounds = [&](int64_t tokens) { return (tokens * n + lanes - 1) / lanes; };
+    int64_t each = fit;
+    for (int64_t e = fit + 1; fill && e <= 4 * fit; ++e)
         if ((double)ranks * tokens / e >= 4096 && 100 * rounds(e) * each < 95 * rounds(each) * e) each = e;
     const int64_t blocks = (tokens + each - 1) / each;
     return Share{(uint32_t)n, make_fastdiv32((uint32_t)n), (uint32_t)each,
@@ -68,6 +69,21 @@ __device__ __forceinline__ void for_vectors(const Share& s, int64_t ranks, int64
                 run(r, item);
             }
         }
+}
+
+// A vector of a row where nothing may be lent, as y may be x: what lies behind the row's end is not read, and what
+// the result holds there does not matter. A row's last values come by single loads, all on their way at once.
+template <typename T, bool STREAM>
+__device__ __forceinline__ typename Packed<T>::type load_columns(const T* row, int64_t i, int64_t width) {
+    constexpr int V = kVec<T>;
+    typename Packed<T>::type x = {};
+    if (i + V <= width) {
+        x = load_vector<STREAM, V>(row + i);
+    } else if (i < width) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = row[i + k < width ? i + k : width - 1];
+    }
+    return x;
 }
 
 // run with the number of values of a row's vectors.
