@@ -106,9 +106,9 @@ def table_gradient(dy, ids, vocab, scale, piece):
 
 
 def piece_of(tokens):
-    """The smallest power of two from 32 on, the 16-fold of whose square is not less than the number of tokens."""
+    """The smallest power of two from 32 on, the 64-fold of whose square is not less than the number of tokens."""
     p = 32
-    while 16 * p * p < tokens:
+    while 64 * p * p < tokens:
         p *= 2
     return p
 
