@@ -3,7 +3,7 @@
 //   y_t = scale table_{id_t}          dtable_v = scale sum of dy_t over the rank's tokens with id_t = v
 //
 // Memory bounds both: the gradient is dense, a row of the vector that an AllReduce sums, so most of its bytes are
-// zeros. A rank's tokens are sorted by number (sort.hip, one pass for tables of up to 4096 rows, otherwise two), and the
+// zeros. A rank's tokens are sorted by number (sort.hip, in one pass or two), and the
 // launches of the sort, which latency bounds, write the zeros on the way. A number's tokens are then a run of the sorted ones.
 // Groups of lanes take equal pieces of these, add up rows in the order of the tokens and write a row of the gradient where its
 // run ends: no atomics, the same bits in every call. Sums of runs that go beyond a piece are joined in order in 64 bits.
@@ -208,13 +208,16 @@ int piece_of(int64_t tokens) {
 
 int64_t pieces_of(int64_t tokens) { return (tokens + piece_of(tokens) - 1) / piece_of(tokens); }
 
-// How the numbers are sorted: by their lower bits first where one pass does not hold them all.
+// How the numbers are sorted: by their lower bits first, in a pass of its own, beyond kOnePass of them, unless a workgroup sorts all
+// tokens of a rank. A pass's counters of many digits and chunks take longer to add up than two passes of fewer digits.
+constexpr int64_t kOnePass = 1024;
+
 struct Digits {
     int bits, bins, more;  // of the first pass (0: all); its digits; those of the second
 };
 
-Digits digits_of(int64_t vocab) {
-    if (vocab <= kMaxBins) return {0, (int)vocab, 0};
+Digits digits_of(int64_t ranks, int64_t tokens, int64_t vocab) {
+    if (vocab <= kOnePass || (vocab <= kMaxBins && sort_launches(ranks, tokens, (int)vocab) == 1)) return {0, (int)vocab, 0};
     int bits = 0;
     while (((int64_t)1 << bits) < vocab) ++bits;
     bits = (bits + 1) / 2;
@@ -227,7 +230,7 @@ struct Places {
 };
 
 Places places(int64_t ranks, int64_t tokens, int64_t width, int64_t vocab) {
-    const Digits d = digits_of(vocab);
+    const Digits d = digits_of(ranks, tokens, vocab);
     Places p;
     int64_t at = 0;
     const auto take = [&](int64_t words) {
@@ -338,7 +341,7 @@ int trivance_embedding_backward(const void* dy, const void* ids, float* dtable, 
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Places at = places(ranks, tokens, width, vocab);
     int* words = static_cast<int*>(workspace);
-    const Digits d = digits_of(vocab);
+    const Digits d = digits_of(ranks, tokens, vocab);
     const int first = sort_launches(ranks, tokens, d.bins), launches = first + (d.bits ? sort_launches(ranks, tokens, d.more) : 0);
     SortPass pass{};
     pass.ids = tokens > 0 ? ids : workspace;  // of no tokens nothing is read

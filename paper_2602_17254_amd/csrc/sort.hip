@@ -62,8 +62,10 @@ __global__ __launch_bounds__(kHistThreads) void sort_count_kernel(SortPass a, in
     }
 }
 
-// Local memory of a workgroup: a counter of each digit for each wave, the digits' first places, a value a wave.
-__host__ __device__ constexpr int64_t place_words(int waves, int bins) { return (int64_t)(waves + 1) * bins + waves; }
+// Local memory of a workgroup: the digits' first places, a value a wave, a counter of each digit for each wave. A thread adds up
+// consecutive first places: one word in 32 is left out, so that threads with 32 each do not meet in one bank.
+__host__ __device__ constexpr int spread(int e) { return e + e / 32; }
+__host__ __device__ constexpr int64_t place_words(int waves, int bins) { return spread(bins) + 1 + waves + (int64_t)waves * bins; }
 
 __device__ __forceinline__ int wave_inclusive(int x) {
     for (int d = 1; d < 64; d *= 2) {
@@ -75,13 +77,15 @@ __device__ __forceinline__ int wave_inclusive(int x) {
 
 constexpr int kRounds = 2;  // of 64 slots, whose keys a wave holds in registers
 
-template <int WAVES>
+// D: digits of a thread whose counters it adds up at once; more than one costs registers, and with them the rate of the
+// zeros that other workgroups of the launch write.
+template <int WAVES, int D>
 __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int64_t per, int64_t chunks, int bits) {
-    constexpr int kThreads = 64 * WAVES;
+    constexpr int kThreads = 64 * WAVES, kCounters = D == 1 ? 16 : 8;
     if (blockIdx.x >= chunks) return fill_block<kThreads>(a, blockIdx.x - chunks);
     extern __shared__ int shared[];
     int* first = shared;  // of each digit
-    int* sums = shared + a.bins;
+    int* sums = shared + spread(a.bins) + 1;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     int* own = sums + WAVES + wave * a.bins;  // this wave's counters
     const int64_t c = blockIdx.x;
@@ -108,25 +112,32 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
         }
         __syncthreads();
         // each digit's keys before this chunk, and in all chunks; a wave's counter becomes the number before the wave
-        for (int e = threadIdx.x; e < a.bins; e += kThreads) {
-            int before = 0, all = 0;
+        for (int e0 = threadIdx.x; e0 < a.bins; e0 += D * kThreads) {
+            int before[D] = {}, all[D] = {};
             if (chunks > 1) {
-                const int* h = a.hist + r * chunks * a.bins + e;
-#pragma unroll 16
-                for (int64_t k = 0; k < chunks; ++k) {
-                    const int n = h[k * a.bins];
-                    all += n;
-                    before += k < c ? n : 0;
-                }
+                const int* h = a.hist + r * chunks * a.bins + e0;
+#pragma unroll kCounters
+                for (int64_t k = 0; k < chunks; ++k)
+#pragma unroll
+                    for (int q = 0; q < D; ++q) {
+                        const int n = q == 0 || e0 + q * kThreads < a.bins ? h[k * a.bins + q * kThreads] : 0;
+                        all[q] += n;
+                        before[q] += k < c ? n : 0;
+                    }
             }
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                int* counter = sums + WAVES + w * a.bins + e;
-                const int n = *counter;
-                *counter = before;
-                before += n;
+            for (int q = 0; q < D; ++q) {
+                const int e = e0 + q * kThreads;
+                if (e >= a.bins) break;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    int* counter = sums + WAVES + w * a.bins + e;
+                    const int n = *counter;
+                    *counter = before[q];
+                    before[q] += n;
+                }
+                first[spread(e)] = chunks > 1 ? all[q] : before[q];
             }
-            first[e] = chunks > 1 ? all : before;
         }
         __syncthreads();
         // the digits' first places: a thread adds up consecutive digits, waves and workgroup the threads' sums
@@ -134,7 +145,7 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
         const int e1 = threadIdx.x * each < (unsigned)a.bins ? threadIdx.x * each : a.bins;
         const int e2 = e1 + each < a.bins ? e1 + each : a.bins;
         int sum = 0;
-        for (int e = e1; e < e2; ++e) sum += first[e];
+        for (int e = e1; e < e2; ++e) sum += first[spread(e)];
         const int upto = wave_inclusive(sum);
         if (lane == 63) sums[wave] = upto;
         __syncthreads();
@@ -144,8 +155,8 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
             total += sums[w];
         }
         for (int e = e1; e < e2; ++e) {
-            const int n = first[e];
-            first[e] = place;
+            const int n = first[spread(e)];
+            first[spread(e)] = place;
             if (a.offsets && c == 0) a.offsets[r * (a.bins + 1) + e] = place;
             place += n;
         }
@@ -176,7 +187,7 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
                     // memory keep their order
                     const int d = digit_of(a, key[q]);
                     const int n = __hip_atomic_load(&own[d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                    at = first[d] + n + rank;
+                    at = first[spread(d)] + n + rank;
                     if (rank + 1 == (int)__popcll(same[q]))
                         __hip_atomic_store(&own[d], n + rank + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
@@ -197,8 +208,8 @@ __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int6
 }  // namespace
 
 // Chunks of as many slots as a workgroup's waves hold keys of, one where that is all; at most 128 (256 where they would be of more than
-// four times as many slots), as each workgroup adds up the counters of all of them, and fewer of many digits. One rank's 10^6
-// slots of 1000 digits take 55 us in place of 96 with 256 chunks, 8 x 131072 of 256 digits 22 in place of 35 with 128.
+// four times as many slots), as each workgroup adds up the counters of all of them, and fewer of many digits. Both launches take
+// 10 us for 8 ranks of 32768 slots and 64 digits, 20 for 131072 and 256.
 SortShape sort_shape(int64_t ranks, int64_t slots, int bins) {
     const int waves = bins <= 2048 ? 4 : 2;
     const int64_t unit = waves * 64, full = unit * kRounds, chunks = slots > full * 4 * 128 ? 256 : 128;
@@ -235,8 +246,9 @@ int run_sort_pass(SortPass a, hipStream_t stream, int launch, int launches) {
     }
     const size_t local = sizeof(int) * place_words(s.waves, a.bins);
     const dim3 g = grid();
-    if (s.waves == 4) sort_place_kernel<4><<<g, 64 * 4, local, stream>>>(a, s.per, s.chunks, bits);
-    else sort_place_kernel<2><<<g, 64 * 2, local, stream>>>(a, s.per, s.chunks, bits);
+    if (a.bins <= 512) sort_place_kernel<4, 1><<<g, 64 * 4, local, stream>>>(a, s.per, s.chunks, bits);
+    else if (s.waves == 4) sort_place_kernel<4, 4><<<g, 64 * 4, local, stream>>>(a, s.per, s.chunks, bits);
+    else sort_place_kernel<2, 4><<<g, 64 * 2, local, stream>>>(a, s.per, s.chunks, bits);
     return launch_status();
 }
 
