@@ -16,6 +16,7 @@ namespace {
 
 constexpr int64_t kMaxGridY = 65535;
 constexpr int kHistThreads = 256;
+constexpr int64_t kMaxZeros = (int64_t)1 << 21;  // workgroups of a launch that write zeros
 
 // The key of a rank's slot, -1 for none.
 __device__ __forceinline__ int key_of(const SortPass& a, int64_t r, int64_t i, int64_t used) {
@@ -33,20 +34,22 @@ __device__ __forceinline__ int64_t used_of(const SortPass& a, int64_t r) {
     return a.ids ? a.slots : a.counts[r * a.count_stride];
 }
 
-// A workgroup's block of zeros, for every rank of its grid row.
+// A workgroup's block of zeros, one of `most` of them, for every rank of its grid row; and the blocks that lie so many further on.
 template <int THREADS>
-__device__ __forceinline__ void fill_block(const SortPass& a, int64_t block) {
-    const int64_t begin = (a.zeros.first + block) * kZerosBlock;
-    const int64_t end = begin + kZerosBlock < a.zeros.values ? begin + kZerosBlock : a.zeros.values;
+__device__ __forceinline__ void fill_blocks(const SortPass& a, int64_t block, int64_t most) {
     const float zero[4] = {};
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y)
-        for (int64_t i = begin + threadIdx.x * 4; i < end; i += THREADS * 4)
-            store_row<float, 4, true>(a.zeros.at + r * a.zeros.rank_stride, i, end, zero);
+        for (int64_t b = block; b < a.zeros.blocks; b += most) {
+            const int64_t begin = (a.zeros.first + b) * kZerosBlock;
+            const int64_t end = begin + kZerosBlock < a.zeros.values ? begin + kZerosBlock : a.zeros.values;
+            for (int64_t i = begin + threadIdx.x * 4; i < end; i += THREADS * 4)
+                store_row<float, 4, true>(a.zeros.at + r * a.zeros.rank_stride, i, end, zero);
+        }
 }
 
 __global__ __launch_bounds__(kHistThreads) void sort_count_kernel(SortPass a, int64_t per, int64_t chunks) {
     extern __shared__ int hist[];
-    if (blockIdx.x >= chunks) return fill_block<kHistThreads>(a, blockIdx.x - chunks);
+    if (blockIdx.x >= chunks) return fill_blocks<kHistThreads>(a, blockIdx.x - chunks, gridDim.x - chunks);
     for (int64_t r = blockIdx.y; r < a.ranks; r += gridDim.y) {
         for (int e = threadIdx.x; e < a.bins; e += kHistThreads) hist[e] = 0;
         __syncthreads();
@@ -82,7 +85,7 @@ constexpr int kRounds = 2;  // of 64 slots, whose keys a wave holds in registers
 template <int WAVES, int D>
 __global__ __launch_bounds__(64 * WAVES) void sort_place_kernel(SortPass a, int64_t per, int64_t chunks, int bits) {
     constexpr int kThreads = 64 * WAVES, kCounters = D == 1 ? 16 : 8;
-    if (blockIdx.x >= chunks) return fill_block<kThreads>(a, blockIdx.x - chunks);
+    if (blockIdx.x >= chunks) return fill_blocks<kThreads>(a, blockIdx.x - chunks, gridDim.x - chunks);
     extern __shared__ int shared[];
     int* first = shared;  // of each digit
     int* sums = shared + spread(a.bins) + 1;
@@ -235,7 +238,8 @@ int run_sort_pass(SortPass a, hipStream_t stream, int launch, int launches) {
         a.zeros.first = launches ? blocks * launch / launches : 0;
         a.zeros.blocks = launches ? blocks * (launch + 1) / launches - a.zeros.first : 0;
         ++launch;
-        return dim3((unsigned)(s.chunks + a.zeros.blocks), (unsigned)(a.ranks < kMaxGridY ? a.ranks : kMaxGridY));
+        const int64_t most = a.zeros.blocks < kMaxZeros ? a.zeros.blocks : kMaxZeros;
+        return dim3((unsigned)(s.chunks + most), (unsigned)(a.ranks < kMaxGridY ? a.ranks : kMaxGridY));
     };
     int bits = 0;
     while ((1 << bits) < a.bins) ++bits;

@@ -805,6 +805,34 @@ def test_more_than_2_31_values():
         assert torch.equal(y[r, part, :8], torch.where(kept, (x[r, part, :8].float() / 0.75), 0.0).bfloat16())
 
 
+def test_embedding_gradient_of_more_than_2_31_values():
+    """A table of 9 GB: the rows at both ends and between them, and zeros everywhere else, where there was none before."""
+    import paper_2602_17254_amd as T
+
+    vocab, width = 140001, 16400
+    d = torch.full((1, vocab, width), math.nan, device="cuda")
+    assert d.numel() > 2 ** 31 + 2 ** 27
+    ids = torch.tensor([[vocab - 1, 0, 131000, vocab - 1, -1, 77]], device="cuda")
+    dy = torch.randn((1, 6, width), **_gen(1))
+    T.trivance_embedding_backward(dy, ids, d, _bytes(T.trivance_embedding_workspace_bytes(1, 6, width, vocab)), 2.0)
+    for v, want in ((vocab - 1, dy[0, 0] + dy[0, 3]), (0, dy[0, 1]), (131000, dy[0, 2]), (77, dy[0, 5])):
+        assert torch.equal(d[0, v], 2 * want)
+        d[0, v] = 0.0
+    assert not any(bool(part.any()) for part in d[0].split(10000))
+
+
+def test_combine_of_no_sorted_rows():
+    """A capacity of zero: every slot is passed over."""
+    import paper_2602_17254_amd as T
+
+    rows, places = torch.empty((2, 0, 40), device="cuda"), torch.zeros((2, 5, 3), dtype=torch.int32, device="cuda")
+    y, w, dw = torch.full((2, 5, 40), 3.0, device="cuda"), torch.ones((2, 5, 3), device="cuda"), torch.full((2, 5, 3), 3.0, device="cuda")
+    T.trivance_experts_dispatch(y, places, rows)
+    T.trivance_experts_combine_backward(y, rows, places, w, rows, dw)
+    T.trivance_experts_combine(rows, places, y, w)
+    assert bool((y == 0).all()) and bool((dw == 0).all())
+
+
 @pytest.mark.parametrize("width", [24, 1030])
 def test_more_ranks_than_a_grid_has_rows(width):
     """Workgroups that go on to another rank."""

@@ -181,9 +181,9 @@ def test_workspace_sizes():
     assert T.trivance_rmsnorm_workspace_bytes(1, 4096, 4096) * 2 == T.trivance_layernorm_workspace_bytes(1, 4096, 4096) > 0
     assert T.trivance_experts_workspace_bytes(9, 100, 2, 64) == 0
     assert T.trivance_experts_workspace_bytes(1, 1 << 20, 8, 4096) > 0
-    # sorted keys and slots, and where each number's run starts
-    assert T.trivance_embedding_workspace_bytes(3, 1000, 64, 2000) >= 3 * (2 * 1000 + 2001) * 4
-    assert T.trivance_embedding_workspace_bytes(3, 1000, 64, 50000) >= 3 * (4 * 1000 + 50001) * 4
+    # sorted keys and slots, twice in two passes, where each digit's run starts, and two parts of 32 pieces
+    assert T.trivance_embedding_workspace_bytes(3, 1000, 64, 1000) >= 3 * (2 * 1000 + 1001 + 32 * 2 * 64) * 4
+    assert T.trivance_embedding_workspace_bytes(3, 1000, 64, 50000) >= 3 * (4 * 1000 + 257 + 32 * 2 * 64) * 4
     for call, args in ((T.trivance_rmsnorm_workspace_bytes, (0, 1, 1)), (T.trivance_rmsnorm_workspace_bytes, (1, 1, 0)),
                        (T.trivance_experts_workspace_bytes, (1, 1, 0, 8)), (T.trivance_experts_workspace_bytes, (1, 1, 1, 0)),
                        (T.trivance_experts_workspace_bytes, (1, 1, 1, 4097)),
