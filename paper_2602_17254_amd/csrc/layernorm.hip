@@ -355,22 +355,23 @@ __global__ __launch_bounds__(kWide) void norm_backward_long_kernel(Backward<T> a
 // 67 MB (6.2 TB/s).
 constexpr int kJoinWaves = 8;
 
+template <int SUMS>
 __global__ __launch_bounds__(64 * kJoinWaves) void join_chunks_kernel(
-    const float* parts, float* dgamma, float* dbeta, int sums_of_chunk, int64_t ranks, int64_t chunks,
-    int64_t width, int64_t grad_rank) {
+    const float* parts, float* dgamma, float* dbeta, int64_t ranks, int64_t chunks, int64_t width,
+    int64_t grad_rank) {
     __shared__ double sums[kJoinWaves][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane, columns = sums_of_chunk * width;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     for (int64_t r = blockIdx.y; r < ranks; r += gridDim.y) {
         double s = 0.0;
-        if (col < columns) {
-            const float* p = parts + r * chunks * columns + col;
+        if (col < SUMS * width) {
+            const float* p = parts + r * chunks * SUMS * width + col;
 #pragma unroll 8
-            for (int64_t c = wave; c < chunks; c += kJoinWaves) s += p[c * columns];
+            for (int64_t c = wave; c < chunks; c += kJoinWaves) s += p[c * SUMS * width];
         }
         sums[wave][lane] = s;
         __syncthreads();
-        if (wave == 0 && col < columns) {
+        if (wave == 0 && col < SUMS * width) {
 #pragma unroll
             for (int w = 1; w < kJoinWaves; ++w) s += sums[w][lane];
             float* out = col < width ? dgamma : dbeta;
@@ -424,8 +425,10 @@ int run_backward(const Backward<T>& a, hipStream_t stream) {
 int join_chunks(const float* parts, float* dgamma, float* dbeta, int sums, int64_t ranks, int64_t chunks,
                 int64_t width, int64_t grad_rank, hipStream_t stream) {
     const dim3 grid((unsigned)((sums * width + 63) / 64), (unsigned)imin(ranks, kMaxGridY));
-    join_chunks_kernel<<<grid, 64 * kJoinWaves, 0, stream>>>(parts, dgamma, dbeta, sums, ranks, chunks, width,
-                                                             grad_rank);
+    if (sums == 2)
+        join_chunks_kernel<2><<<grid, 64 * kJoinWaves, 0, stream>>>(parts, dgamma, dbeta, ranks, chunks, width, grad_rank);
+    else
+        join_chunks_kernel<1><<<grid, 64 * kJoinWaves, 0, stream>>>(parts, dgamma, dbeta, ranks, chunks, width, grad_rank);
     return launch_status();
 }
 

@@ -9,6 +9,9 @@
 
 #include "operators.h"
 
+// the norms' products and sums are fused, those in the functions here among them
+#pragma clang fp contract(fast)
+
 namespace trivance {
 
 constexpr int kThreads = 256;      // lanes of a workgroup whose rows take fewer
