@@ -569,8 +569,8 @@ int trivance_rmsnorm_forward(const void* x, const void* residual, const void* ga
                              int64_t y_rank_stride, int64_t y_token_stride, double eps, int dtype,
                              int y_dtype, int weight_dtype, void* stream);
 
-/* Workspace bytes of trivance_rmsnorm_backward for these sizes, for every dtype; 0 where a rank's
- * tokens are summed in one piece. EINVAL for sizes that the call refuses. */
+/* Workspace bytes of trivance_rmsnorm_backward for these sizes (others may need more, smaller ones
+ * too), for every dtype; 0 where a rank's tokens are summed in one piece. EINVAL for sizes that the call refuses. */
 int64_t trivance_rmsnorm_workspace_bytes(int64_t ranks, int64_t tokens, int64_t width);
 
 /*
@@ -601,8 +601,8 @@ int trivance_rmsnorm_backward(const void* dy, const void* total, const void* gam
                               int weight_dtype, void* workspace, int64_t workspace_bytes,
                               void* stream);
 
-/* Workspace bytes of trivance_experts_sort for these sizes, for both types of numbers. EINVAL or
- * EUNSUPPORTED for sizes that the call refuses. */
+/* Workspace bytes of trivance_experts_sort for these sizes (others may need more, smaller ones too),
+ * for both types of numbers. EINVAL or EUNSUPPORTED for sizes that the call refuses. */
 int64_t trivance_experts_workspace_bytes(int64_t ranks, int64_t tokens, int64_t top_k,
                                          int64_t experts);
 
@@ -703,8 +703,8 @@ int trivance_embedding_forward(const void* ids, const void* table, void* y, int6
                                int64_t y_rank_stride, int64_t y_token_stride, double scale, int dtype,
                                int table_dtype, int id_dtype, void* stream);
 
-/* Workspace bytes of trivance_embedding_backward for these sizes, for every type. EINVAL or EUNSUPPORTED
- * for sizes that the call refuses. */
+/* Workspace bytes of trivance_embedding_backward for these sizes (others may need more, smaller ones
+ * too), for every type. EINVAL or EUNSUPPORTED for sizes that the call refuses. */
 int64_t trivance_embedding_workspace_bytes(int64_t ranks, int64_t tokens, int64_t width,
                                            int64_t vocab);
 

@@ -50,7 +50,10 @@ __device__ __forceinline__ float weight_of(const Slots<T>& a, int64_t slot) {
     return (float)static_cast<const f16*>(a.weights)[slot];
 }
 
-// A lane reads a vector of a token's row once and writes it to each of the token's slots' rows.
+// A lane reads a vector of a token's row once and writes it to each of the token's slots' rows, one after another: 889 us for 8 x 16384
+// tokens of 2048 bf16 in 8 slots, 4.8 GB (5.4 TB/s; 5.7 where the rows follow one another, 6.8 a copy). Stores to many rows bound
+// it: all places first and then all stores took 955, a store a lane 1367 (latency), a wave for a row 965, fewer workgroups at
+// once 898 to 957, contiguous tokens for each XCD 923.
 template <typename T, int V, bool STREAM>
 __global__ __launch_bounds__(kShareThreads) void dispatch_kernel(Slots<T> a, const T* x) {
     for_vectors<V, 1>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, const Item(&item)[1]) {
@@ -64,7 +67,9 @@ __global__ __launch_bounds__(kShareThreads) void dispatch_kernel(Slots<T> a, con
     });
 }
 
-// A lane adds up vectors of U tokens' results, K slots at a time: all places, then all rows on their way at once.
+// A lane adds up vectors of U tokens' results, K slots at a time: all places, then all rows on their way at once. Bound by the bytes of the
+// rows: 219 us for 8 x 8192 tokens of 2048 bf16 in 4 slots, 1.34 GB, 6.1 TB/s (248 with a slot's place and row one after
+// the other, 226 with one token a lane); 20 us for 27 x 1003 tokens of 515 fp16 in 4 slots, half of them empty.
 template <int K>
 constexpr int kCombineItems = K <= 4 ? 2 : 1;
 
