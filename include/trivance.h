@@ -554,8 +554,9 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
  *   scales       device fp32 array [ranks][tokens], with TRIVANCE_E4M3 only: a row's largest |y| over
  *                448, or 2^-126 where that is less; the row stands for y times its scale.
  *
- * Sums are in fp32: rows with values of 1e19 or more give zeros. A row that holds a NaN gives NaN; an
- * infinity gives NaN in its place and zeros elsewhere, NaN throughout with TRIVANCE_E4M3.
+ * Sums are in fp32: rows whose squares add up to more than it holds (values near 1e19) give zeros, and
+ * with eps == 0 rows of less than 1e-18 lose precision and zeros give NaN. A row that holds a NaN gives
+ * NaN; an infinity gives NaN in its place and zeros elsewhere, NaN throughout with TRIVANCE_E4M3.
  * tokens == 0 does nothing.
  * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, width outside [1, 2^24], eps negative or
  * NaN, NULL x or y, y in total's place, scales without TRIVANCE_E4M3 or the other way round, bad

@@ -200,7 +200,7 @@ bool sizes_ok(int64_t ranks, int64_t tokens, int64_t top_k) {
     return ranks <= INT32_MAX && top_k <= INT32_MAX && (__int128)ranks * tokens * top_k <= INT32_MAX;
 }
 
-// The tokens' rows and the sorted ones; `written` says which of them a call writes.
+// Whether the rows of tokens and the sorted ones can be addressed.
 bool rows_ok(int64_t ranks, int64_t tokens, int64_t width, int64_t capacity, int64_t x_rank, int64_t x_token,
              int64_t rows_rank, int64_t rows_row) {
     if (width < 1 || width > ((int64_t)1 << 24) || capacity < 0 || capacity > INT32_MAX) return false;

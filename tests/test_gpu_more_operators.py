@@ -436,7 +436,7 @@ def test_experts_gradients_against_autograd(width):
 # Embedding.
 
 
-TABLE_SIZES = [(1, 1, 1, 1), (2, 3, 5, 7), (1, 1, 50000, 64), (3, 100, 10, 33), (2, 0, 20, 16), (1, 65, 1, 130), (2, 700, 1024, 40), (2, 700, 1025, 40), (2, 700, 4096, 40),
+TABLE_SIZES = [(1, 1, 1, 1), (5, 128, 40, 50), (5, 129, 40, 50), (2, 64, 900, 520), (2, 127, 3, 4097), (2, 3, 5, 7), (1, 1, 50000, 64), (3, 100, 10, 33), (2, 0, 20, 16), (1, 65, 1, 130), (2, 700, 1024, 40), (2, 700, 1025, 40), (2, 700, 4096, 40),
                (2, 700, 4097, 40), (1, 5000, 300, 257), (9, 333, 1000, 100), (1, 20000, 70000, 24), (3, 3000, 9, 515),
                (1, 300, 7, 9000), (2, 17000, 131, 64), (70, 40, 60, 8), (1, 40000, 2, 65)]
 
@@ -485,7 +485,7 @@ def test_embedding(size, dtype):
     assert bool((rows == PATTERN).all())
 
 
-@pytest.mark.parametrize("tokens", [64, 65, 128, 4096, 4097, 9000])
+@pytest.mark.parametrize("tokens", [64, 65, 128, 129, 192, 4096, 4097, 9000])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_embedding_runs_that_start_and_end_at_pieces(tokens, dtype):
     """Long runs of one number beside others, whose ends fall on, before and behind the ends of pieces."""
