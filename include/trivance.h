@@ -641,7 +641,7 @@ int trivance_experts_sort(const void* chosen, const uint8_t* mask, int32_t* offs
  *   rows    device rows [ranks][capacity][width]; those of no slot are left as they were. Not x.
  *
  * Errors: EINVAL for unknown types, sizes as in trivance_experts_sort, width outside [1, 2^24], capacity
- * outside [0, 2^31 - 1], NULL pointers, bad strides; EHIP.
+ * outside [0, 2^31 - 1], NULL pointers, rows in x's place, bad strides; EHIP.
  */
 int trivance_experts_dispatch(const void* x, const int32_t* places, void* rows, int64_t ranks,
                               int64_t tokens, int64_t top_k, int64_t width, int64_t capacity,
@@ -659,7 +659,7 @@ int trivance_experts_dispatch(const void* x, const int32_t* places, void* rows, 
  *                 rows.
  *
  * Sums are in fp32, in the order of j, rounded once.
- * Errors: as trivance_experts_dispatch.
+ * Errors: as trivance_experts_dispatch, y in rows' place.
  */
 int trivance_experts_combine(const void* rows, const int32_t* places, const void* weights, void* y,
                              int64_t ranks, int64_t tokens, int64_t top_k, int64_t width,
@@ -674,10 +674,10 @@ int trivance_experts_combine(const void* rows, const int32_t* places, const void
  *
  *   dy        device rows [ranks][tokens][width] of `dtype`.
  *   drows     device rows [ranks][capacity][width]; those of no slot are left as they were. It may be
- *             rows (with the same strides).
+ *             rows (with the same strides), not dy.
  *   dweights  device fp32 [ranks][tokens][top_k].
  *
- * Errors: as trivance_experts_dispatch.
+ * Errors: as trivance_experts_dispatch, drows in dy's place.
  */
 int trivance_experts_combine_backward(const void* dy, const void* rows, const int32_t* places,
                                       const void* weights, void* drows, float* dweights, int64_t ranks,

@@ -115,6 +115,14 @@ __global__ __launch_bounds__(kShareThreads) void combine_kernel(Slots<T> a, T* y
     });
 }
 
+// A product that is rounded to fp32 before it is to fewer bits, wherever it is stored: of some the compiler would make an
+// instruction that rounds once, so that two lanes that write the same value might not.
+__device__ __forceinline__ float product(float a, float b) {
+    float p = a * b;
+    asm("" : "+v"(p));
+    return p;
+}
+
 // L lanes take a token: each adds up its vectors' part of the slots' sums, K slots at a time. With a workgroup for a token,
 // whose lanes have a vector each or a few, 8 x 8192 tokens of 2048 bf16 in 4 slots take 427 us in place of a wave's 465.
 template <typename T, int V, int L, int K, bool STREAM>
@@ -150,10 +158,17 @@ __global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T
 #pragma unroll
                             for (int k = 0; k < V; ++k) {
                                 const float g = (float)d[k];
-                                o[k] = (T)(w[j] * g);
+                                o[k] = (T)product(w[j], g);
                                 sum[j] += k >= skip ? g * (float)v[j][k] : 0.0f;
                             }
-                            store_vector<STREAM, V>(drows + r * a.drows_rank + p[j] * a.drows_row + at, o);
+                            T* to = drows + r * a.drows_rank + p[j] * a.drows_row + at;
+                            if (skip == 0 || drows != a.rows) {
+                                store_vector<STREAM, V>(to, o);
+                            } else {  // in place: the wave of the vector before may not have read what is lent
+#pragma unroll
+                                for (int k = 1; k < V; ++k)
+                                    if (k >= skip) to[k] = o[k];
+                            }
                         }
                 }
 #pragma unroll
@@ -256,7 +271,7 @@ int trivance_experts_dispatch(const void* x, const int32_t* places, void* rows, 
     if (tokens == 0) return TRIVANCE_OK;
     if (!rows_ok(ranks, tokens, width, capacity, x_rank_stride, x_token_stride, rows_rank_stride, rows_row_stride))
         return TRIVANCE_EINVAL;
-    if (!x || !places || (capacity > 0 && !rows) ||
+    if (!x || !places || (capacity > 0 && !rows) || rows == x ||
         (capacity > 0 && !rows_distinct(ranks, capacity, width, rows_rank_stride, rows_row_stride)))
         return TRIVANCE_EINVAL;
     if (capacity == 0) return TRIVANCE_OK;
@@ -285,7 +300,8 @@ int trivance_experts_combine(const void* rows, const int32_t* places, const void
     if (tokens == 0) return TRIVANCE_OK;
     if (!rows_ok(ranks, tokens, width, capacity, y_rank_stride, y_token_stride, rows_rank_stride, rows_row_stride))
         return TRIVANCE_EINVAL;
-    if ((capacity > 0 && !rows) || !places || !y || !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride))
+    if ((capacity > 0 && !rows) || !places || !y || y == rows ||
+        !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride))
         return TRIVANCE_EINVAL;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return with_type(dtype, [&](auto type) {
@@ -314,7 +330,7 @@ int trivance_experts_combine_backward(const void* dy, const void* rows, const in
     if (tokens == 0) return TRIVANCE_OK;
     if (!rows_ok(ranks, tokens, width, capacity, dy_rank_stride, dy_token_stride, rows_rank_stride, rows_row_stride))
         return TRIVANCE_EINVAL;
-    if (!dy || !places || !dweights || (capacity > 0 && (!rows || !drows)) ||
+    if (!dy || !places || !dweights || drows == dy || (capacity > 0 && (!rows || !drows)) ||
         !rows_fit(ranks, capacity > 0 ? capacity : 1, width, drows_rank_stride, drows_row_stride) ||
         (capacity > 0 && !rows_distinct(ranks, capacity, width, drows_rank_stride, drows_row_stride)))
         return TRIVANCE_EINVAL;

@@ -356,6 +356,28 @@ def test_experts_rows(size, dtype):
     _gaps_kept(rows, base)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vectors,more_values", [(128, 1), (192, 2), (256, 3), (320, 1)])
+def test_experts_gradients_in_place_of_rows_that_end_inside_a_vector(vectors, more_values, dtype):
+    """drows in rows' place, where a row's last vector and the one before it are of different waves: the bits of a
+    call with rows of its own."""
+    import paper_2602_17254_amd as T
+
+    dt = ref.DTYPES[dtype]
+    width = vectors * (4 if dt == torch.float32 else 8) + more_values
+    dev = _gen(width)
+    for k in (1, 2, 4, 8):
+        ranks, tokens = 2, 1500
+        places, capacity = _sorted_rows((ranks, tokens, k, width), 64)
+        rows = torch.randn((ranks, capacity, width), **dev).to(dt)
+        dy, weights = torch.randn((ranks, tokens, width), **dev).to(dt), torch.randn((ranks, tokens, k), **dev)
+        drows, dweights, own = rows.clone(), torch.empty_like(weights), rows.clone()
+        T.trivance_experts_combine_backward(dy, rows, places, weights, drows, dweights)
+        again = torch.empty_like(dweights)
+        T.trivance_experts_combine_backward(dy, own, places, weights, own, again)
+        assert torch.equal(again, dweights) and torch.equal(own, drows), (width, k)
+
+
 def test_experts_empty_slots_are_neither_read_nor_added():
     """Rows of no slot, weights of empty slots and dy of tokens without one may hold anything."""
     import paper_2602_17254_amd as T

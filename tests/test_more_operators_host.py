@@ -57,7 +57,7 @@ def combine(**kw):
 
 
 def gradient(**kw):
-    a = dict(dy=P, rows=P, places=P, weights=P, drows=P, dweights=P, ranks=2, tokens=3, k=2, width=8, capacity=6,
+    a = dict(dy=P, rows=P, places=P, weights=P, drows=Q, dweights=P, ranks=2, tokens=3, k=2, width=8, capacity=6,
              yr=24, yt=8, rr=48, rs=8, dr=48, ds=8, dtype=T.F32, wtype=T.F32, stream=None)
     a.update(kw)
     return _lib().trivance_experts_combine_backward(*a.values())
@@ -121,18 +121,19 @@ BAD_ROWS = [dict(dtype=T.I32), dict(dtype=T.E4M3), dict(ranks=0), dict(tokens=-1
 
 
 @pytest.mark.parametrize("kw", BAD_ROWS + [dict(x=None), dict(xr=-1), dict(xt=-1), dict(rs=7), dict(rr=47),
-                                           dict(rr=0)], ids=str)
+                                           dict(rr=0), dict(rows=P)], ids=str)
 def test_experts_dispatch_refuses(kw):
     assert dispatch(**kw) == EINVAL
 
 
-@pytest.mark.parametrize("kw", BAD_ROWS + [dict(y=None), dict(yr=-1), dict(yt=7), dict(yr=8), dict(wtype=T.I32)], ids=str)
+@pytest.mark.parametrize("kw", BAD_ROWS + [dict(y=None), dict(yr=-1), dict(yt=7), dict(yr=8), dict(wtype=T.I32),
+                                           dict(y=P)], ids=str)
 def test_experts_combine_refuses(kw):
     assert combine(**kw) == EINVAL
 
 
 @pytest.mark.parametrize("kw", BAD_ROWS + [dict(dy=None), dict(yr=-1), dict(drows=None), dict(dweights=None), dict(dr=47),
-                                           dict(ds=7), dict(ds=-1), dict(wtype=9)], ids=str)
+                                           dict(ds=7), dict(ds=-1), dict(wtype=9), dict(drows=P)], ids=str)
 def test_experts_combine_backward_refuses(kw):
     assert gradient(**kw) == EINVAL
 
