@@ -14,6 +14,7 @@
 
 #include "operators.h"
 #include "sort.h"
+#include "strips.h"
 #include "vectors.h"
 
 #pragma clang fp contract(fast)
@@ -101,8 +102,8 @@ __global__ __launch_bounds__(kThreads) void table_sums_kernel(Table<T> a) {
         bool began = first == 0 || keys[first - 1] != keys[first];  // whether the run did in this piece
         float* part = a.parts + (r * a.pieces + piece) * 2 * a.width;
         float sum[V] = {};
-        for (int p0 = (int)first; p0 < end; p0 += L) {
-            const int here = end - p0 < L ? end - p0 : L, own = p0 + (lane < here ? lane : 0);
+        for_strips<L>((int)first, end, [&](int p0, int here) {
+            const int own = p0 + (lane < here ? lane : 0);
             const int token = order[own], key = keys[own], after = own + 1 < used ? keys[own + 1] : -1;
             const auto fetch = [&](int p, typename Packed<T>::type(&v)[kAhead]) {
 #pragma unroll
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void table_sums_kernel(Table<T> a) {
                 fetch(p + 2 * kAhead, even);
                 add(p + kAhead, odd);
             }
-        }
+        });
     }
 }
 
