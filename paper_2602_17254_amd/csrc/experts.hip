@@ -16,6 +16,7 @@
 #include "device.h"
 #include "operators.h"
 #include "sort.h"
+#include "strips.h"
 #include "vectors.h"
 
 #pragma clang fp contract(fast)
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(kShareThreads) void combine_kernel(Slots<T> a, T* y
     for_vectors<V, U>(a.share, a.ranks, a.tokens, a.width, [&](int64_t r, const Item(&item)[U]) {
         const T* rows = a.rows + r * a.rows_rank;
         float sum[U][V] = {};
-        for (int j0 = 0; j0 < a.top_k; j0 += K) {
+        for_strips<K>(0, a.top_k, [&](int j0, int here) {
             Some<T, V> v[U][K];
             int p[U][K];
             float w[U][K];
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(kShareThreads) void combine_kernel(Slots<T> a, T* y
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int j = 0; j < K; ++j)
-                    p[u][j] = item[u].is && j0 + j < a.top_k ? place_of(a, (r * a.tokens + item[u].token) * a.top_k + j0 + j) : -1;
+                    p[u][j] = item[u].is && j < here ? place_of(a, (r * a.tokens + item[u].token) * a.top_k + j0 + j) : -1;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(kShareThreads) void combine_kernel(Slots<T> a, T* y
 #pragma unroll
                         for (int k = 0; k < V; ++k) sum[u][k] += w[u][j] * (float)v[u][j][k];
                     }
-        }
+        });
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             Some<T, V> o;
@@ -135,12 +136,12 @@ __global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T
         for (int64_t t = (int64_t)blockIdx.x * G + group; t < a.tokens; t += (int64_t)gridDim.x * G) {
             const int64_t slot = (r * a.tokens + t) * a.top_k;
             const T* from = dy + r * a.x_rank + t * a.x_token;
-            for (int j0 = 0; j0 < a.top_k; j0 += K) {
+            for_strips<K>(0, a.top_k, [&](int j0, int here) {
                 int p[K];
                 float w[K], sum[K] = {};
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
-                    p[j] = j0 + j < a.top_k ? place_of(a, slot + j0 + j) : -1;
+                    p[j] = j < here ? place_of(a, slot + j0 + j) : -1;
                     w[j] = p[j] >= 0 ? weight_of(a, slot + j0 + j) : 0.0f;
                 }
                 for (int64_t i = lane * V; i < a.width; i += L * V) {
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T
                         for (int j = 0; j < K; ++j) sums[turn][threadIdx.x / 64][j] = sum[j];
                     }
                     __syncthreads();
-                    if (lane < K && j0 + lane < a.top_k) {
+                    if (lane < here) {
                         float s = 0.0f;
 #pragma unroll
                         for (int w = 0; w < L / 64; ++w) s += sums[turn][w][lane];
@@ -189,9 +190,9 @@ __global__ __launch_bounds__(kShareThreads) void combine_backward_kernel(Slots<T
                 } else if (lane == 0) {
 #pragma unroll
                     for (int j = 0; j < K; ++j)
-                        if (j0 + j < a.top_k) dweights[slot + j0 + j] = sum[j];
+                        if (j < here) dweights[slot + j0 + j] = sum[j];
                 }
-            }
+            });
         }
     }
 }

@@ -2,6 +2,7 @@
 numbers that the calls take."""
 
 import os
+import re
 import shutil
 import subprocess
 
@@ -19,3 +20,10 @@ def test_strips_end_at_the_largest_int(tmp_path):
     res = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert res.returncode == 0, res.stdout + res.stderr
     assert "strips ok" in res.stdout
+
+
+@pytest.mark.parametrize("name", ["embedding.hip", "experts.hip"])
+def test_kernels_count_by_strips(name):
+    """No kernel counts slots or tokens up by whole strips in an int, which may go beyond the largest one."""
+    with open(os.path.join(CSRC, name)) as f:
+        assert not re.findall(r"for \(int \w+ = [^;]*;[^;]*; \w+ \+= [KL]\)", f.read())
