@@ -387,7 +387,8 @@ int trivance_plan_with_dispatch_limit(const trivance_plan_t* plan, int64_t work_
  * Activations and logits are rows of `width` (or `experts`) consecutive values, one for each token
  * of each rank: value i of token t of rank r lies at data[r * rank_stride + t * token_stride + i].
  * Strides count elements, are not negative and need no alignment beyond an element's; rows that are
- * written must not overlap (EINVAL). Gradients and counts are one row per rank, `*_rank_stride`
+ * written must not overlap (EINVAL). Where an output may take an input's place, it does so from the first
+ * row on and with the same strides (EINVAL for others; those of a single rank or token do not matter). Gradients and counts are one row per rank, `*_rank_stride`
  * elements apart, so they can be written into (and read from) slices of the buffers of
  * trivance_allreduce_emulated. All calls are asynchronous on `stream`, enqueue kernel launches only
  * and can be captured into a HIP graph; sums are formed in a fixed order, so a call repeated on

@@ -103,7 +103,10 @@ extern "C" int trivance_dropout(const void* x, const void* residual, void* y, co
         !rows_fit(ranks, tokens, width, x_rank_stride, x_token_stride) ||
         !rows_fit(ranks, tokens, width, y_rank_stride, y_token_stride) ||
         !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride) ||
-        (residual && !rows_fit(ranks, tokens, width, residual_rank_stride, residual_token_stride)))
+        !rows_in_place(y, x, ranks, tokens, y_rank_stride, y_token_stride, x_rank_stride, x_token_stride) ||
+        (residual && (!rows_fit(ranks, tokens, width, residual_rank_stride, residual_token_stride) ||
+                      !rows_in_place(y, residual, ranks, tokens, y_rank_stride, y_token_stride, residual_rank_stride,
+                                     residual_token_stride))))
         return TRIVANCE_EINVAL;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const auto run = [&](auto type) {

@@ -333,7 +333,9 @@ int trivance_experts_combine_backward(const void* dy, const void* rows, const in
         return TRIVANCE_EINVAL;
     if (!dy || !places || !dweights || drows == dy || (capacity > 0 && (!rows || !drows)) ||
         !rows_fit(ranks, capacity > 0 ? capacity : 1, width, drows_rank_stride, drows_row_stride) ||
-        (capacity > 0 && !rows_distinct(ranks, capacity, width, drows_rank_stride, drows_row_stride)))
+        (capacity > 0 &&
+         (!rows_distinct(ranks, capacity, width, drows_rank_stride, drows_row_stride) ||
+          !rows_in_place(drows, rows, ranks, capacity, drows_rank_stride, drows_row_stride, rows_rank_stride, rows_row_stride))))
         return TRIVANCE_EINVAL;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return with_type(dtype, [&](auto type) {

@@ -215,6 +215,14 @@ inline bool rows_distinct(int64_t ranks, int64_t tokens, int64_t width, int64_t 
     return rank_stride >= width && token_stride >= (ranks - 1) * rank_stride + width;
 }
 
+// Whether rows that are written may lie where rows that are read do: elsewhere, or each in its own place. With other
+// strides they would overwrite rows that are still to be read. Strides of a single rank or token do not matter.
+inline bool rows_in_place(const void* out, const void* in, int64_t ranks, int64_t tokens, int64_t out_rank_stride,
+                          int64_t out_token_stride, int64_t in_rank_stride, int64_t in_token_stride) {
+    return out != in || ((ranks == 1 || out_rank_stride == in_rank_stride) &&
+                         (tokens == 1 || out_token_stride == in_token_stride));
+}
+
 inline int launch_status() {
     return hipGetLastError() == hipSuccess ? TRIVANCE_OK : TRIVANCE_EHIP;
 }

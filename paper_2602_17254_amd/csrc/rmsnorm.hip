@@ -525,6 +525,13 @@ int trivance_rmsnorm_forward(const void* x, const void* residual, const void* ga
         (residual && !fits(residual_rank_stride, residual_token_stride)) ||
         (total && !written(total_rank_stride, total_token_stride)))
         return TRIVANCE_EINVAL;
+    const auto in_place = [&](const void* out, int64_t rank, int64_t token) {
+        return rows_in_place(out, x, ranks, tokens, rank, token, x_rank_stride, x_token_stride) &&
+               (!residual ||
+                rows_in_place(out, residual, ranks, tokens, rank, token, residual_rank_stride, residual_token_stride));
+    };
+    if (!in_place(y, y_rank_stride, y_token_stride) || !in_place(total, total_rank_stride, total_token_stride))
+        return TRIVANCE_EINVAL;
     const bool out8 = y_dtype == TRIVANCE_E4M3;
     // scales go with 8 bits, whose rows cannot take the place of wider ones
     if (out8 ? !scales || y == x || y == residual : scales != nullptr) return TRIVANCE_EINVAL;
@@ -567,6 +574,12 @@ int trivance_rmsnorm_backward(const void* dy, const void* total, const void* gam
                        !fits(total_rank_stride, total_token_stride) || !fits(dx_rank_stride, dx_token_stride) ||
                        (dtotal && !fits(dtotal_rank_stride, dtotal_token_stride)) ||
                        !rows_distinct(ranks, tokens, width, dx_rank_stride, dx_token_stride)))
+        return TRIVANCE_EINVAL;
+    const auto in_place = [&](const void* in, int64_t rank, int64_t token) {
+        return rows_in_place(dx, in, ranks, tokens, dx_rank_stride, dx_token_stride, rank, token);
+    };
+    if (tokens > 0 && !(in_place(dy, dy_rank_stride, dy_token_stride) && in_place(total, total_rank_stride, total_token_stride) &&
+                        (!dtotal || in_place(dtotal, dtotal_rank_stride, dtotal_token_stride))))
         return TRIVANCE_EINVAL;
     const int64_t need = trivance_rmsnorm_workspace_bytes(ranks, tokens, width);
     if (dgamma && (workspace_bytes < need || (need > 0 && !workspace))) return TRIVANCE_ESIZE;

@@ -952,3 +952,30 @@ def test_tensors_beyond_the_caches(dtype):
     kept = torch.from_numpy(more.kept(x.shape, 2, 2, 0.5)).to("cuda")
     assert torch.equal(drop, torch.where(kept, x * 2, torch.zeros_like(x)))
     _gaps_kept(drop, base)
+
+
+@pytest.mark.parametrize("shape", [(1, 3, 40), (3, 1, 40), (1, 1, 700)], ids=_id)
+def test_in_place_strides_of_a_single_rank_or_token_do_not_matter(shape):
+    import paper_2602_17254_amd as T
+
+    ranks, tokens, width = shape
+    dev = _gen(width)
+    other = (width if ranks > 1 else 977, width if tokens > 1 else 1013, 1)
+    x, dy, state = torch.randn(shape, **dev), torch.randn(shape, **dev), _state(1, 2)
+    y, dx, rstd, drop = torch.empty_like(x), torch.empty_like(x), torch.empty(shape[:2], device="cuda"), torch.empty_like(x)
+    T.trivance_rmsnorm_forward(x, None, y, rstd)
+    T.trivance_rmsnorm_backward(dy, x, None, rstd, dx, None)
+    T.trivance_dropout(x, drop, state, 0.5)
+    for call, want in ((lambda t: T.trivance_rmsnorm_forward(t, None, t.as_strided(shape, other)), y),
+                       (lambda t: T.trivance_rmsnorm_backward(dy, t, None, rstd, t.as_strided(shape, other), None), dx),
+                       (lambda t: T.trivance_dropout(t, t.as_strided(shape, other), state, 0.5), drop)):
+        own = x.clone()
+        call(own)
+        assert torch.equal(own, want)
+    # one token and one sorted row a rank
+    if tokens == 1:
+        places, w = torch.zeros((ranks, 1, 1), dtype=torch.int32, device="cuda"), torch.rand((ranks, 1, 1), **dev)
+        drows, dw, own = torch.empty_like(x), torch.empty_like(w), x.clone()
+        T.trivance_experts_combine_backward(dy, x, places, w, drows, dw)
+        T.trivance_experts_combine_backward(dy, own, places, w, own.as_strided(shape, other), torch.empty_like(w))
+        assert torch.equal(own, drows)

@@ -243,3 +243,28 @@ def test_generator_keeps_the_share():
         assert abs(share - (1 - round(rate * 65536) / 65536)) <= 5 * math.sqrt(rate * (1 - rate) / n)
     a, b = more.kept((2, 9, 40), 5, 1, 0.5), more.kept((2, 9, 40), 5, 2, 0.5)
     assert (a != b).any() and np.array_equal(a, more.kept((2, 9, 40), 5, 1 + (1 << 32), 0.5))
+
+
+@pytest.mark.parametrize("kw", [dict(total=P, tr=48), dict(total=P, tt=12, tr=36), dict(residual=8 * P, total=P, tr=48),
+                                dict(x=8 * P, total=P, tr=48), dict(total=None, y=P, yr=48), dict(total=None, y=P, yt=9, yr=27),
+                                dict(total=8 * P, x=9 * P, y=P, yr=48), dict(total=8 * P, y=P, ranks=1, yt=9),
+                                dict(total=8 * P, y=P, tokens=1, yr=25)], ids=str)
+def test_rmsnorm_forward_refuses_other_strides_in_place(kw):
+    assert norm(**kw) == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(dxr=48), dict(dxt=9, dxr=27), dict(dx=Q, dy=Q, dxr=48), dict(dx=Q, total=Q, dxr=48),
+                                dict(dx=Q, dtotal=Q, dxr=48), dict(ranks=1, dxt=9), dict(tokens=1, dxr=25)], ids=str)
+def test_rmsnorm_backward_refuses_other_strides_in_place(kw):
+    assert norm_backward(**kw) == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(dr=96), dict(ds=9, dr=54), dict(ranks=1, ds=9), dict(capacity=1, dr=96)], ids=str)
+def test_experts_combine_backward_refuses_other_strides_in_place(kw):
+    assert gradient(drows=Q, rows=Q, **kw) == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(yr=48), dict(yt=9, yr=27), dict(x=P, residual=Q, yr=48), dict(x=Q, residual=P, yr=48),
+                                dict(x=Q, residual=None, yr=48), dict(ranks=1, yt=9), dict(tokens=1, yr=25)], ids=str)
+def test_dropout_refuses_other_strides_in_place(kw):
+    assert dropout(**{**dict(x=Q, residual=Q), **kw}) == EINVAL
