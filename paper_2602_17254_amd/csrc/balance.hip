@@ -487,7 +487,8 @@ int trivance_balance_backward(const void* logits, const int32_t* counts, const u
     if (!logits || !counts || !dlogits || !rows_fit(ranks, tokens, experts, rank_stride, token_stride) ||
         !rows_fit(ranks, 1, experts + 1, counts_rank_stride, 0) ||
         !rows_fit(ranks, tokens, experts, d_rank_stride, d_token_stride) ||
-        !rows_distinct(ranks, tokens, experts, d_rank_stride, d_token_stride))
+        !rows_distinct(ranks, tokens, experts, d_rank_stride, d_token_stride) ||
+        !rows_in_place(dlogits, logits, ranks, tokens, d_rank_stride, d_token_stride, rank_stride, token_stride))
         return TRIVANCE_EINVAL;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const auto run = [&](auto type) {

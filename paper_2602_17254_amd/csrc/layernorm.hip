@@ -448,7 +448,8 @@ int trivance_layernorm_forward(const void* x, const void* gamma, const void* bet
     if (tokens == 0) return TRIVANCE_OK;
     if (!x || !y || !rows_fit(ranks, tokens, width, x_rank_stride, x_token_stride) ||
         !rows_fit(ranks, tokens, width, y_rank_stride, y_token_stride) ||
-        !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride))
+        !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride) ||
+        !rows_in_place(y, x, ranks, tokens, y_rank_stride, y_token_stride, x_rank_stride, x_token_stride))
         return TRIVANCE_EINVAL;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const auto run = [&](auto type) {
@@ -491,7 +492,9 @@ int trivance_layernorm_backward(const void* dy, const void* x, const void* gamma
          !rows_fit(ranks, tokens, width, dy_rank_stride, dy_token_stride) ||
          !rows_fit(ranks, tokens, width, x_rank_stride, x_token_stride) ||
          !rows_fit(ranks, tokens, width, dx_rank_stride, dx_token_stride) ||
-         !rows_distinct(ranks, tokens, width, dx_rank_stride, dx_token_stride)))
+         !rows_distinct(ranks, tokens, width, dx_rank_stride, dx_token_stride) ||
+         !rows_in_place(dx, dy, ranks, tokens, dx_rank_stride, dx_token_stride, dy_rank_stride, dy_token_stride) ||
+         !rows_in_place(dx, x, ranks, tokens, dx_rank_stride, dx_token_stride, x_rank_stride, x_token_stride)))
         return TRIVANCE_EINVAL;
     const int64_t need = trivance_layernorm_workspace_bytes(ranks, tokens, width);
     if ((dgamma || dbeta) && (workspace_bytes < need || (need > 0 && !workspace)))

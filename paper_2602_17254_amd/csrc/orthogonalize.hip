@@ -1187,7 +1187,8 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
     if (batch == 0 || rows == 0 || cols == 0) return TRIVANCE_OK;
     if (!x || !out || !rows_fit(batch, rows, cols, x_batch_stride, x_row_stride) ||
         !rows_fit(batch, rows, cols, out_batch_stride, out_row_stride) ||
-        !rows_distinct(batch, rows, cols, out_batch_stride, out_row_stride))
+        !rows_distinct(batch, rows, cols, out_batch_stride, out_row_stride) ||
+        !rows_in_place(out, x, batch, rows, out_batch_stride, out_row_stride, x_batch_stride, x_row_stride))
         return TRIVANCE_EINVAL;
     if (workspace_bytes < need || (need > 0 && !workspace)) return TRIVANCE_ESIZE;
     const Layout w = layout_of(batch, rows, cols);

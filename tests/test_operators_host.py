@@ -180,3 +180,13 @@ def test_orthogonalize_workspace_holds_what_the_call_uses(size, shared):
     need = b * (16 * m * n + 8 * m * m) + 4 * shared * 128 * 128
     got = T.trivance_orthogonalize_workspace_bytes(*size)
     assert need <= got <= need + b * (1024 * 8 + 16) + 4096
+
+
+@pytest.mark.parametrize("call,kw", [
+    (forward, dict(yr=48)), (forward, dict(yt=9, yr=27)), (forward, dict(ranks=1, yt=9)), (forward, dict(tokens=1, yr=25)),
+    (backward, dict(dxr=48)), (backward, dict(dxt=9, dxr=27)), (backward, dict(dy=2 * P, dxr=48)), (backward, dict(x=2 * P, dxr=48)),
+    (backward, dict(tokens=1, dxr=25)), (gradient, dict(dr=48)), (gradient, dict(dt=9, dr=27)), (gradient, dict(ranks=1, dt=9)),
+    (orthogonalize, dict(ob=5700)), (orthogonalize, dict(orow=81, ob=5670)), (orthogonalize, dict(batch=1, orow=81)),
+    (orthogonalize, dict(rows=1, ob=81))], ids=lambda v: getattr(v, "__name__", None) or str(v))
+def test_other_strides_in_place_are_refused(call, kw):
+    assert call(**kw) == EINVAL
