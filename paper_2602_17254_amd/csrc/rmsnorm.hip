@@ -10,8 +10,9 @@
 // sum (and one maximum with it: that of |s gamma|, as rstd is the same for the whole row), so one barrier where
 // several waves hold it. A lane holds the same columns of every row: the weight gradients of a workgroup's rows add
 // up in registers, go to the workspace, and are joined in a fixed order in 64 bits, as those of the layer norm.
-// Squares are positive: their sum in fp32 loses nothing by cancelling. y comes from the sum before it is rounded to
-// the stored type; total, y and dx are rounded once.
+// A lane adds up at most 32 values of a row in fp32, then lanes and waves their sums in some 22 steps: a sum is off by at most
+// 54 roundings of the sum of its terms' sizes. The lanes of longer rows have many vectors, whose sums meet in 64 bits. y comes from the
+// sum before it is rounded to the stored type; total, y and dx are rounded once.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -179,7 +180,8 @@ __global__ __launch_bounds__(kBlock<LANES>) void rms_forward_kernel(Forward<T> a
     }
 }
 
-// Rows beyond what a workgroup's registers hold: read twice, the second time from the caches.
+// Rows beyond what a workgroup's registers hold: read twice, the second time from the caches. A lane adds up to 4096 vectors: one
+// after another in fp32, rstd was off by 5e-5 of itself at 2^24 equal values.
 template <typename T, bool OUT8>
 __global__ __launch_bounds__(kWide) void rms_forward_long_kernel(Forward<T> a) {
     constexpr int V = kVec<T>;
@@ -200,17 +202,21 @@ __global__ __launch_bounds__(kWide) void rms_forward_long_kernel(Forward<T> a) {
                     for (int k = 0; k < V; ++k) v[k] += w[k];
                 }
             };
-            float v[V], gamma[V], square = 0.0f, most = 0.0f;
+            float v[V], gamma[V], most = 0.0f;
+            double squares = 0.0;
             for (int64_t i = i0; i < a.width; i += kWide * V) {
                 fetch(i, v);
+                float part = 0.0f;
 #pragma unroll
-                for (int k = 0; k < V; ++k) square += v[k] * v[k];
+                for (int k = 0; k < V; ++k) part += v[k] * v[k];
+                squares += part;
                 if constexpr (OUT8) {
                     load_weights<V>(a.gamma, a.weight_type, i, a.width, 1.0f, gamma);
 #pragma unroll
                     for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[k] * gamma[k]));
                 }
             }
+            float square = (float)squares;
             row_sum_max<kWide, OUT8>(square, most, slots[turn]);
             turn ^= 1;
             const float rstd = 1.0f / sqrtf(square * inv + a.eps);
@@ -383,12 +389,12 @@ __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1))
     }
 }
 
-// Rows beyond what a workgroup's registers hold: read twice, the second time from the caches, and the chunk's
-// sums of the weight gradients added up where they go.
+// Rows beyond what a workgroup's registers hold: read twice, the second time from the caches, the sum of their vectors' sums
+// in 64 bits, and the chunk's sums of the weight gradients added up where they go.
 template <typename T>
 __global__ __launch_bounds__(kWide) void rms_backward_long_kernel(Backward<T> a) {
     constexpr int V = kVec<T>;
-    __shared__ float slots[2][kWide / 64];
+    __shared__ double slots[2][kWide / 64];
     const float inv = 1.0f / (float)a.width;
     const int64_t i0 = (int64_t)threadIdx.x * V;
     int turn = 0;  // goes on from one rank to the next
@@ -406,15 +412,18 @@ __global__ __launch_bounds__(kWide) void rms_backward_long_kernel(Backward<T> a)
             const T* dtotal = a.dtotal + r * a.dtotal_rank + t * a.dtotal_token;
             T* dx = a.dx + r * a.dx_rank + t * a.dx_token;
             const float rstd = a.rstd[r * a.tokens + t];
-            float h[V], g[V], gamma[V], along = 0.0f;
+            float h[V], g[V], gamma[V];
+            double sum = 0.0;
             for (int64_t i = i0; i < a.width; i += kWide * V) {
                 load_row<T>(total, i, a.width, 0.0f, h);
                 load_row<T>(dy, i, a.width, 0.0f, g);
                 load_weights<V>(a.gamma, a.weight_type, i, a.width, 1.0f, gamma);
+                float part = 0.0f;
 #pragma unroll
-                for (int k = 0; k < V; ++k) along += g[k] * gamma[k] * (h[k] * rstd);
+                for (int k = 0; k < V; ++k) part += g[k] * gamma[k] * (h[k] * rstd);
+                sum += part;
             }
-            along = inv * row_sum<kWide>(along, slots[turn]);
+            const float along = inv * (float)row_sum<kWide>(sum, slots[turn]);
             turn ^= 1;
             for (int64_t i = i0; i < a.width; i += kWide * V) {
                 float o[V], more[V] = {};

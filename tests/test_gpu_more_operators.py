@@ -979,3 +979,35 @@ def test_in_place_strides_of_a_single_rank_or_token_do_not_matter(shape):
         T.trivance_experts_combine_backward(dy, x, places, w, drows, dw)
         T.trivance_experts_combine_backward(dy, own, places, w, own.as_strided(shape, other), torch.empty_like(w))
         assert torch.equal(own, drows)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [100003, 1 << 20, (1 << 24) - 1, 1 << 24])
+def test_rmsnorm_sums_of_the_longest_rows(width, dtype):
+    """Rows of values whose sums round the same way at every step, and of any: the bounds of short rows hold. A lane's sum
+    of a vector passes 8 roundings, 64 lanes' 6, the waves' 16, which SUM covers whatever the width."""
+    import paper_2602_17254_amd as T
+
+    _say("rmsnorm long", width, dtype)
+    dt, dev = ref.DTYPES[dtype], _gen(width)
+    x = torch.randn((1, 3, width), **dev)
+    x[0, 0] = 1.1
+    x[0, 1] = x[0, 1].abs() + 0.3
+    dy = torch.randn((1, 3, width), **dev)
+    dy[0, :2] = 0.7
+    x, dy, gamma = x.to(dt), dy.to(dt), 1 + 0.1 * torch.rand(width, **dev)
+    y, rstd = torch.empty_like(x), torch.empty((1, 3), device="cuda")
+    T.trivance_rmsnorm_forward(x, gamma, y, rstd)
+    (want, by), (wr, br) = more.rmsnorm_forward(x.double(), gamma.double(), 1e-5)
+    ref.assert_within(rstd, wr, br, "rstd")
+    ref.assert_within(y, want, by + ref.rounding(want, dt) * 1.01, "y")
+    q, scales = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty_like(rstd)
+    T.trivance_rmsnorm_forward(x, gamma, q, scales=scales)
+    (wq, bq), (ws, bs) = more.eight_bits(want)
+    ref.assert_within(scales, ws, bs, "scales")
+    ref.assert_within(q.float(), wq, bq, "8 bits")
+    dx, dg = torch.empty_like(x), torch.empty((1, width), device="cuda")
+    T.trivance_rmsnorm_backward(dy, x, gamma, rstd, dx, dg, _bytes(T.trivance_rmsnorm_workspace_bytes(1, 3, width)))
+    (wx, bx), (wg, bg) = more.rmsnorm_backward(dy.double(), x.double(), gamma.double(), rstd.double(), None)
+    ref.assert_within(dx, wx, bx + ref.rounding(wx, dt) * 1.01, "dx")
+    ref.assert_within(dg, wg, bg, "dgamma")
