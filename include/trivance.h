@@ -698,7 +698,7 @@ int trivance_experts_combine_backward(const void* dy, const void* rows, const in
  *
  * scale is used as an fp32 number.
  * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, more than 2^31 - 1 tokens over all ranks,
- * width outside [1, 2^24], vocab < 1, NULL pointers, bad strides; EHIP.
+ * width outside [1, 2^24], vocab < 1, scale not finite as an fp32 number, NULL pointers, bad strides; EHIP.
  */
 int trivance_embedding_forward(const void* ids, const void* table, void* y, int64_t ranks,
                                int64_t tokens, int64_t width, int64_t vocab, int64_t table_row_stride,

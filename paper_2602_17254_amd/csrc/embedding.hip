@@ -9,6 +9,7 @@
 // run ends: no atomics, the same bits in every call. Sums of runs that go beyond a piece are joined in order in 64 bits.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -401,7 +402,7 @@ int trivance_embedding_forward(const void* ids, const void* table, void* y, int6
                                void* stream) {
     if (!is_float_type(dtype) || !is_float_type(table_dtype) || (id_dtype != TRIVANCE_I32 && id_dtype != TRIVANCE_I64))
         return TRIVANCE_EINVAL;
-    if (!sizes_ok(ranks, tokens, width, vocab)) return TRIVANCE_EINVAL;
+    if (!sizes_ok(ranks, tokens, width, vocab) || !std::isfinite((float)scale)) return TRIVANCE_EINVAL;
     if (tokens == 0) return TRIVANCE_OK;
     if (!ids || !table || !y || !rows_fit(1, vocab, width, 0, table_row_stride) ||
         !rows_fit(ranks, tokens, width, y_rank_stride, y_token_stride) ||
@@ -437,6 +438,7 @@ int trivance_embedding_backward(const void* dy, const void* ids, float* dtable, 
     if (!is_float_type(dtype) || (id_dtype != TRIVANCE_I32 && id_dtype != TRIVANCE_I64)) return TRIVANCE_EINVAL;
     const int64_t need = trivance_embedding_workspace_bytes(ranks, tokens, width, vocab);
     if (need < 0) return (int)need;
+    if (!std::isfinite((float)scale)) return TRIVANCE_EINVAL;  // of zeros it would make no zeros
     if (!dtable || !rows_fit(ranks, 1, vocab * width, dtable_rank_stride, 0) ||
         !rows_distinct(ranks, 1, vocab * width, dtable_rank_stride, 0))
         return TRIVANCE_EINVAL;

@@ -268,3 +268,10 @@ def test_experts_combine_backward_refuses_other_strides_in_place(kw):
                                 dict(x=Q, residual=None, yr=48), dict(ranks=1, yt=9), dict(tokens=1, yr=25)], ids=str)
 def test_dropout_refuses_other_strides_in_place(kw):
     assert dropout(**{**dict(x=Q, residual=Q), **kw}) == EINVAL
+
+
+@pytest.mark.parametrize("scale", [math.inf, -math.inf, math.nan, 1e39, -3.5e38], ids=str)
+def test_embedding_refuses_scales_that_are_no_numbers(scale):
+    """They would make NaN of the zeros of padding, and of sums that are zero."""
+    assert lookup(scale=scale) == EINVAL
+    assert table(scale=scale) == EINVAL
