@@ -694,11 +694,12 @@ int trivance_experts_combine_backward(const void* dy, const void* rows, const in
  *   ids    device array [ranks][tokens] of id_dtype (TRIVANCE_I32 or TRIVANCE_I64); a value outside
  *          [0, vocab) is padding and gives zeros.
  *   table  device rows [vocab][width] of table_dtype, table_row_stride elements apart.
- *   y      device rows [ranks][tokens][width] of `dtype`.
+ *   y      device rows [ranks][tokens][width] of `dtype`. Not table.
  *
  * scale is used as an fp32 number.
  * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, more than 2^31 - 1 tokens over all ranks,
- * width outside [1, 2^24], vocab < 1, scale not finite as an fp32 number, NULL pointers, bad strides; EHIP.
+ * width outside [1, 2^24], vocab < 1, scale not finite as an fp32 number, NULL pointers, y in table's
+ * place, bad strides; EHIP.
  */
 int trivance_embedding_forward(const void* ids, const void* table, void* y, int64_t ranks,
                                int64_t tokens, int64_t width, int64_t vocab, int64_t table_row_stride,
@@ -716,12 +717,12 @@ int64_t trivance_embedding_workspace_bytes(int64_t ranks, int64_t tokens, int64_
  *
  *   dy, ids    as y and ids of the forward pass; padding adds nothing, and its dy is not read.
  *   dtable     device fp32 [vocab][width] of each rank, dtable_rank_stride elements apart; all of it is
- *              written, not added to (zeros for numbers that no token has).
+ *              written, not added to (zeros for numbers that no token has). Not dy.
  *   workspace  4-byte aligned, at least trivance_embedding_workspace_bytes.
  *
  * Sums go in the order of the tokens, in fp32, those of numbers that many tokens have in pieces that are
  * joined in 64 bits.
- * Errors: those of the forward pass; EUNSUPPORTED for vocab above 2^24; ESIZE for the workspace.
+ * Errors: those of the forward pass, dtable in dy's place; EUNSUPPORTED for vocab above 2^24; ESIZE for the workspace.
  */
 int trivance_embedding_backward(const void* dy, const void* ids, float* dtable, int64_t ranks,
                                 int64_t tokens, int64_t width, int64_t vocab, int64_t dy_rank_stride,

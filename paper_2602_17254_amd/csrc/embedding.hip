@@ -404,7 +404,7 @@ int trivance_embedding_forward(const void* ids, const void* table, void* y, int6
         return TRIVANCE_EINVAL;
     if (!sizes_ok(ranks, tokens, width, vocab) || !std::isfinite((float)scale)) return TRIVANCE_EINVAL;
     if (tokens == 0) return TRIVANCE_OK;
-    if (!ids || !table || !y || !rows_fit(1, vocab, width, 0, table_row_stride) ||
+    if (!ids || !table || !y || y == table || !rows_fit(1, vocab, width, 0, table_row_stride) ||
         !rows_fit(ranks, tokens, width, y_rank_stride, y_token_stride) ||
         !rows_distinct(ranks, tokens, width, y_rank_stride, y_token_stride))
         return TRIVANCE_EINVAL;
@@ -442,7 +442,7 @@ int trivance_embedding_backward(const void* dy, const void* ids, float* dtable, 
     if (!dtable || !rows_fit(ranks, 1, vocab * width, dtable_rank_stride, 0) ||
         !rows_distinct(ranks, 1, vocab * width, dtable_rank_stride, 0))
         return TRIVANCE_EINVAL;
-    if (tokens > 0 && (!dy || !ids || !rows_fit(ranks, tokens, width, dy_rank_stride, dy_token_stride)))
+    if (tokens > 0 && (!dy || !ids || dtable == dy || !rows_fit(ranks, tokens, width, dy_rank_stride, dy_token_stride)))
         return TRIVANCE_EINVAL;
     if (workspace_bytes < need || !workspace) return TRIVANCE_ESIZE;
     if (reinterpret_cast<uintptr_t>(workspace) % sizeof(int)) return TRIVANCE_EINVAL;

@@ -275,3 +275,10 @@ def test_embedding_refuses_scales_that_are_no_numbers(scale):
     """They would make NaN of the zeros of padding, and of sums that are zero."""
     assert lookup(scale=scale) == EINVAL
     assert table(scale=scale) == EINVAL
+
+
+def test_embedding_refuses_outputs_in_place():
+    """Rows of the table, or of dy, would be overwritten before they are read."""
+    assert lookup(y=P, ttype=T.F32) == EINVAL
+    assert table(dtable=P) == EINVAL
+    assert table(dtable=P, ranks=1, tokens=200, dyr=1600) == EINVAL
