@@ -707,7 +707,8 @@ int trivance_embedding_forward(const void* ids, const void* table, void* y, int6
                                int table_dtype, int id_dtype, void* stream);
 
 /* Workspace bytes of trivance_embedding_backward for these sizes (others may need more, smaller ones
- * too), for every type. EINVAL or EUNSUPPORTED for sizes that the call refuses. */
+ * too), for every type; up to 128 tokens of a rank leave it untouched. EINVAL or EUNSUPPORTED for sizes that
+ * the call refuses. */
 int64_t trivance_embedding_workspace_bytes(int64_t ranks, int64_t tokens, int64_t width,
                                            int64_t vocab);
 

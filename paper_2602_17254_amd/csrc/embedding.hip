@@ -333,7 +333,7 @@ Places places(int64_t ranks, int64_t tokens, int64_t width, int64_t vocab) {
         p.order[i] = i == 0 || d.bits ? take(ranks * tokens) : p.order[0];
     }
     p.hist = take(imax(sort_hist_values(ranks, tokens, d.bins), d.bits ? sort_hist_values(ranks, tokens, d.more) : 0));
-    p.parts = take(ranks * pieces_of(tokens) * 2 * width);
+    p.parts = take(tokens > kFewTokens ? ranks * pieces_of(tokens) * 2 * width : 0);  // few tokens have no pieces
     p.end = at;
     return p;
 }

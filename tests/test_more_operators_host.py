@@ -282,3 +282,10 @@ def test_embedding_refuses_outputs_in_place():
     assert lookup(y=P, ttype=T.F32) == EINVAL
     assert table(dtable=P) == EINVAL
     assert table(dtable=P, ranks=1, tokens=200, dyr=1600) == EINVAL
+
+
+def test_few_tokens_ask_for_no_parts():
+    """The sums of pieces, two rows for each, are most of a workspace; up to 128 tokens of a rank have no pieces."""
+    few = T.trivance_embedding_workspace_bytes(243, 128, 8192, 1000)
+    assert 0 < few < 2 * 4 * (243 * (1000 + 1 + 2 * 128) + 12)
+    assert T.trivance_embedding_workspace_bytes(243, 129, 8192, 1000) > 243 * 5 * 2 * 8192 * 4
