@@ -1011,3 +1011,31 @@ def test_rmsnorm_sums_of_the_longest_rows(width, dtype):
     (wx, bx), (wg, bg) = more.rmsnorm_backward(dy.double(), x.double(), gamma.double(), rstd.double(), None)
     ref.assert_within(dx, wx, bx + ref.rounding(wx, dt) * 1.01, "dx")
     ref.assert_within(dg, wg, bg, "dgamma")
+
+
+def test_more_than_2_31_values_leave_no_row_and_no_column_out():
+    """Weights' gradients of whole numbers, whose sums fp32 holds, are equal to the last one; dropout's places of whole
+    rows, the last block of columns, which is not full, among them."""
+    import paper_2602_17254_amd as T
+
+    ranks, tokens, width = 8, 65537, 4100
+    dev = _gen(5)
+    x, dy, dx = (torch.empty((ranks, tokens, width), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    assert x.numel() > 2 ** 31 and tokens * 9 < 2 ** 24
+    for r in range(ranks):
+        for t in (x, dy):
+            t[r] = torch.randint(-3, 4, (tokens, width), dtype=torch.int8, **dev)
+    rstd, dg = torch.ones((ranks, tokens), device="cuda"), torch.empty((ranks, width), device="cuda")
+    T.trivance_rmsnorm_backward(dy, x, None, rstd, dx, dg, _bytes(T.trivance_rmsnorm_workspace_bytes(*x.shape)))
+    for r in range(ranks):
+        assert torch.equal(dg[r].double(), (x[r].double() * dy[r].double()).sum(0)), r
+
+    seed, call, rate = 7, 9, 0.25
+    T.trivance_dropout(x, dx, _state(seed, call), rate)
+    blocks = -(-width // 8)
+    for r in (0, 3, ranks - 1):
+        for t in (0, 1, tokens // 2, tokens - 1):
+            words = more.philox((range(blocks), [t] * blocks, [r] * blocks, [call] * blocks), (seed, 0))
+            halves = torch.tensor([[int(w[b]) >> s & 0xFFFF for w in words for s in (0, 16)] for b in range(blocks)])
+            kept = (halves.flatten()[:width] >= round(rate * 65536)).to("cuda")
+            assert torch.equal(dx[r, t], torch.where(kept, x[r, t].float() / 0.75, 0.0).bfloat16()), (r, t)
