@@ -557,7 +557,8 @@ int trivance_orthogonalize(const void* x, void* out, int64_t batch, int64_t rows
  *
  * Sums are in fp32: rows whose squares add up to more than it holds (values near 1e19) give zeros, and
  * with eps == 0 rows of less than 1e-18 lose precision and zeros give NaN. A row that holds a NaN gives
- * NaN; an infinity gives NaN in its place and zeros elsewhere, NaN throughout with TRIVANCE_E4M3.
+ * NaN; an infinity gives NaN in its place and zeros elsewhere, NaN throughout with TRIVANCE_E4M3, where
+ * |s gamma| has to be a number of fp32, too.
  * tokens == 0 does nothing.
  * Errors: EINVAL for unknown types, ranks < 1, tokens < 0, width outside [1, 2^24], eps negative or
  * NaN, NULL x or y, y in total's place, scales without TRIVANCE_E4M3 or the other way round, bad
@@ -676,7 +677,8 @@ int trivance_experts_combine(const void* rows, const int32_t* places, const void
  *   dy        device rows [ranks][tokens][width] of `dtype`.
  *   drows     device rows [ranks][capacity][width]; those of no slot are left as they were. It may be
  *             rows (with the same strides), not dy.
- *   dweights  device fp32 [ranks][tokens][top_k].
+ *   dweights  device fp32 [ranks][tokens][top_k]. Sums are in fp32, at most 16 terms, or width / 256 + 8
+ *             of them, one after another.
  *
  * Errors: as trivance_experts_dispatch, drows in dy's place.
  */

@@ -6,8 +6,10 @@
 //              of a dispatch: dx_t = sum_j drows_{p_tj}, a combine without weights
 //
 // Memory bounds all three. Every kernel goes by token: a token's row is read (or written) once and its slots' rows,
-// which lie anywhere, in whole runs of consecutive lanes. A slot without a row (a place outside the sorted rows) is passed over and neither
-// read nor written; sums are in fp32, in the order of the slots, rounded once.
+// which lie anywhere, in whole runs of consecutive lanes. A slot without a row (a place outside the sorted rows) is passed over: no sorted
+// row is read or written for it. Its token's own row is read all the same, by the dispatch as its load goes before the places, by the
+// gradient once for the token: with half of 8 x 8192 tokens of 2048 bf16 masked and a slot each they take 60 and 99 us, where 79 and
+// 133 are those of all tokens and the bytes in use would take 40 and 59. Sums are in fp32, in the order of the slots, rounded once.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

@@ -172,7 +172,8 @@ inline int64_t imax(int64_t a, int64_t b) { return a > b ? a : b; }
 // enough for that, 19 sizes between the two took 2% more in all: 8 x 1200 x 16000 bf16 262 us in place of 219,
 // 8 x 5000 x 768 bf16 51 in place of 44, 1 x 9000 x 4000 bf16 59 in place of 54; 1 x 16000 x 1100 bf16 46 in
 // place of 54 and 8 x 1500 x 1536 bf16 35 in place of 39, whose lanes' second vectors are void. A few
-// workgroups above a multiple of what the CUs hold would cost a round.
+// workgroups above a multiple of what the CUs hold would cost a round. All these are the layer norm's times; the RMS
+// norm's backward pass follows the same rule, which was not measured against others for it.
 inline int64_t chunk_tokens(int64_t ranks, int64_t tokens, Shape s) {
     const int64_t rows = group_rows(s), wide = block_lanes(s) / kThreads;
     const int64_t many = imax(1, 1024 / ranks), few = imax(1, 512 / wide / ranks);

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void rms_forward_kernel(Forward<T> a
 }
 
 // Rows beyond what a workgroup's registers hold: read twice, the second time from the caches. A lane adds up to 4096 vectors: one
-// after another in fp32, rstd was off by 5e-5 of itself at 2^24 equal values.
+// after another in fp32, rstd was off by 5e-5 of itself at 2^24 equal values. 8 x 1024 x 20001 bf16 223 us, of which the bytes take 96.
 template <typename T, bool OUT8>
 __global__ __launch_bounds__(kWide) void rms_forward_long_kernel(Forward<T> a) {
     constexpr int V = kVec<T>;
@@ -277,7 +277,9 @@ __device__ __forceinline__ float* sums_of(const Backward<T>& a, int64_t r, int64
 // Bound by the bytes of its rows: 376 us at 8 x 4096 x 8192 bf16 with dtotal, 2.15 GB, 5.7 TB/s (and 7 us to join the workgroups' sums). The rows
 // of a rank go to its workgroups in turn, so that those at work read neighbouring rows: with consecutive rows of its own for each it
 // took 390, and 5 to 13% more on 8 of 10 sizes (2 to 9% less on 8 x 4096 x 2048 and 8 x 16384 x 512). Loads a row ahead make no difference there,
-// but 5% at 9 x 777 x 1283 fp16, 16 us and 4 to join.
+// but 5% at 9 x 777 x 1283 fp16, 16 us and 4 to join. Rows of 8193 to 16384 values leave no registers for all of it: 20 to 100 bytes of
+// a lane go to scratch memory. 8 x 4096 x 16384 bf16 takes 770 us, 5.6 TB/s, 8 x 1024 x 16384 fp32 385, 5.6, but 8 x 1024 x 8200 bf16,
+// whose lanes' third and fourth vectors are void but for one, 112, 4.8.
 template <typename T, int V, int LANES, int NV, bool STREAM>
 __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1)) void rms_backward_kernel(Backward<T> a) {
     constexpr int G = kBlock<LANES> / LANES;
@@ -390,7 +392,8 @@ __global__ __launch_bounds__(kBlock<LANES>, (kLocalGamma<V, LANES, NV> ? 4 : 1))
 }
 
 // Rows beyond what a workgroup's registers hold: read twice, the second time from the caches, the sum of their vectors' sums
-// in 64 bits, and the chunk's sums of the weight gradients added up where they go.
+// in 64 bits, and the chunk's sums of the weight gradients added up where they go. 8 x 1024 x 20001 bf16 863 us, 651 without
+// dgamma, where the bytes take 145: a lane's loads wait for those before.
 template <typename T>
 __global__ __launch_bounds__(kWide) void rms_backward_long_kernel(Backward<T> a) {
     constexpr int V = kVec<T>;
